@@ -310,6 +310,94 @@ int nvfp4_linear_backward(const void* dy, int64_t tokens, int64_t d_out, int64_t
 int nvfp4_dequantize(const nvfp4_qtensor* q, int which_copy, int undo_rht, void* out, int out_dtype,
                      int64_t ld_out, nvfp4_stream_t stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Around the linear layers: what stands in front of and behind them in a transformer block's MLP, and what is kept of
+ * it for the backward pass.  Rules that all of these calls share:
+ *   - Element types are NVFP4_OUT_F32 and NVFP4_OUT_BF16.  All arithmetic, sums and statistics are FP32; an output is
+ *     rounded once, to nearest even.
+ *   - Rows may be any number, 0 included (nothing to do; sums over no rows are 0); columns are a positive multiple of
+ *     16; leading dimensions are in elements, at least the columns and multiples of 8 -- else NVFP4_ERR_BAD_SHAPE.
+ *     Pointers are 16-byte aligned (rstd 4, checkpoint scales 1), else NVFP4_ERR_INVALID_ARG; those of a tensor
+ *     without rows may be NULL.
+ *   - An output may be the very tensor that an input of the same type and leading dimension is (x or residual and h or
+ *     y; dy or dres and dx; da and dz; residual and D); other overlaps are not allowed.
+ *   - Sums over rows are added in a fixed order: the same inputs give the same bits.
+ */
+enum { NVFP4_ACT_NONE = 0, NVFP4_ACT_RELU2 = 1, NVFP4_ACT_GELU = 2, NVFP4_ACT_SILU = 3 };
+/* RELU2: max(z, 0)^2.  SILU: z / (1 + exp(-z)).  GELU: z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))). */
+
+/*
+ * An activation kept in 8 bits: every 16 consecutive columns of a row have one scale 2^e, e the smallest integer with
+ * max |v| <= 448 * 2^e (-127 <= e <= 127), and a value is an E4M3 code, round-to-nearest-even of v / 2^e.
+ *   codes [rows, cols] bytes, scales [rows, cols / 16] bytes e + 127 (0 for a block of zeros); 1.0625 bytes an element.
+ * A value is off by at most 1/16 of itself, or 2^(e - 10) where it is below 2^(e - 6).  A block that holds an infinity or a
+ * NaN has the byte 255 and reads back as 16 NaNs.  Caller-owned plain struct like nvfp4_qtensor.
+ */
+typedef struct nvfp4_checkpoint {
+  int64_t rows, cols;
+  void* codes;
+  void* scales;
+} nvfp4_checkpoint;
+
+/* Byte counts of a checkpoint (host pointers, any may be NULL). */
+int nvfp4_checkpoint_sizes(int64_t rows, int64_t cols, size_t* codes_bytes, size_t* scales_bytes);
+
+/* Keep x (type x_dtype, [rows, cols] as the descriptor says, leading dimension ldx) in 8 bits. */
+int nvfp4_checkpoint_save(const void* x, int x_dtype, int64_t ldx, const nvfp4_checkpoint* out, nvfp4_stream_t stream);
+
+/*
+ * out[i, j] = act(v[i, j]) * col_scale[j], v the checkpoint's values: with an activation, its output made again from what went into it; with
+ * col_scale = a norm's gamma (NULL: ones), that norm's output from its normalised rows.  Ready for nvfp4_quantize.
+ */
+int nvfp4_checkpoint_load(const nvfp4_checkpoint* c, int activation, const float* col_scale, void* out, int out_dtype, int64_t ld_out,
+                          nvfp4_stream_t stream);
+
+/*
+ * Residual addition and root-mean-square norm:
+ *   h = x + residual;  rstd = 1 / sqrt(mean over the row of h^2 + eps);  xhat = h rstd;  y = xhat gamma
+ *   x         [rows, cols] of type x_dtype, cols <= 32768
+ *   residual  of type h_dtype, or NULL (h = x)
+ *   gamma     FP32 [cols], or NULL (ones);  eps >= 0
+ *   h, y      outputs of types h_dtype, y_dtype, each may be NULL
+ *   rstd      FP32 [rows], or NULL
+ *   keep      8 bits of xhat (keep_kind NVFP4_NORM_KEEP_NORMALIZED: what nvfp4_rmsnorm_backward reads) or of y
+ *             (NVFP4_NORM_KEEP_OUTPUT), or NULL
+ * The norm is taken of the FP32 sum, before it is rounded for h.  Every tensor is read or written once.
+ */
+enum { NVFP4_NORM_KEEP_NORMALIZED = 0, NVFP4_NORM_KEEP_OUTPUT = 1 };
+int nvfp4_rmsnorm_forward(const void* x, int x_dtype, int64_t ldx, const void* residual, int64_t ldr, const float* gamma, float eps, int64_t rows,
+                          int64_t cols, void* h, int h_dtype, int64_t ldh, void* y, int y_dtype, int64_t ldy, float* rstd, const nvfp4_checkpoint* keep,
+                          int keep_kind, nvfp4_stream_t stream);
+
+/*
+ * Its gradient: g = dy gamma;  dx = rstd (g - xhat mean over the row of (g xhat)) + dres;  dgamma = sum over rows of dy xhat
+ *   dy        [rows, cols] of type dy_dtype
+ *   h         the norm's input, of type s_dtype: xhat = h rstd; or NULL and
+ *   saved     the 8 bits of xhat that the forward pass kept (exactly one of the two)
+ *   rstd      FP32 [rows], as the forward pass gave it
+ *   dres      the gradient that reaches h on the residual's way, of type s_dtype, or NULL
+ *   dx        of type s_dtype, the gradient of x and of residual alike; or NULL
+ *   dgamma    FP32 [cols], stored, or added into with accumulate; or NULL
+ *   workspace device, 16-byte aligned, nvfp4_rowsum_workspace_bytes; only with dgamma
+ */
+int nvfp4_rmsnorm_backward(const void* dy, int dy_dtype, int64_t lddy, const void* h, int64_t ldh, const nvfp4_checkpoint* saved, const float* rstd,
+                           const float* gamma, const void* dres, int64_t lddr, int64_t rows, int64_t cols, void* dx, int s_dtype, int64_t lddx,
+                           float* dgamma, int accumulate, void* workspace, size_t workspace_bytes, nvfp4_stream_t stream);
+
+/*
+ * Gradient through an activation whose input was kept in 8 bits, and of the bias that was added to it:
+ *   dz = da act'(z);  dbias = sum over rows of dz (before dz is rounded)
+ *   da, dz    [rows, cols] of one type; dz may be NULL (dbias alone)
+ *   saved     the checkpoint of z; NULL with NVFP4_ACT_NONE (dz = da: the sum is the gradient of a plain layer's bias)
+ *   dbias     FP32 [cols], stored, or added into with accumulate; or NULL
+ *   workspace as for nvfp4_rmsnorm_backward; only with dbias
+ */
+int nvfp4_activation_backward(const void* da, int dtype, int64_t ldda, int64_t rows, int64_t cols, const nvfp4_checkpoint* saved, int activation, void* dz,
+                              int64_t lddz, float* dbias, int accumulate, void* workspace, size_t workspace_bytes, nvfp4_stream_t stream);
+
+/* Bytes of the workspace that either backward call needs for its sums over rows (host pointer out); may be 0. */
+int nvfp4_rowsum_workspace_bytes(int64_t rows, int64_t cols, size_t* workspace_bytes);
+
 /* 16-bit sign diagonal for a seed: bit i set means s_i = -1 (App. C). */
 uint32_t nvfp4_rht_sign_mask(uint64_t rht_seed);
 

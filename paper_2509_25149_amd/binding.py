@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes
 import os
 from dataclasses import dataclass
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -24,11 +24,15 @@ ROUND_RNE, ROUND_SR = 0, 1
 OP_FPROP, OP_DGRAD, OP_WGRAD = 0, 1, 2
 OUT_F32, OUT_BF16, OUT_F32_ACCUMULATE = 0, 1, 2
 COPY_ROW, COPY_COL = 0, 1
+ACT_NONE, ACT_RELU2, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+NORM_KEEP_NORMALIZED, NORM_KEEP_OUTPUT = 0, 1
 
 EXPORTS = ["nvfp4_quantized_sizes", "nvfp4_quantize", "nvfp4_gemm", "nvfp4_gemm_workspace_bytes", "nvfp4_dequantize",
            "nvfp4_rht_sign_mask", "nvfp4_selftest_conversions", "nvfp4_status_string", "nvfp4_version",
            "nvfp4_linear_workspace_bytes", "nvfp4_linear_forward", "nvfp4_linear_backward",
-           "nvfp4_amax", "nvfp4_quantize_with_amax", "nvfp4_quantize_static", "nvfp4_predecode"]
+           "nvfp4_amax", "nvfp4_quantize_with_amax", "nvfp4_quantize_static", "nvfp4_predecode",
+           "nvfp4_checkpoint_sizes", "nvfp4_checkpoint_save", "nvfp4_checkpoint_load", "nvfp4_rmsnorm_forward", "nvfp4_rmsnorm_backward",
+           "nvfp4_activation_backward", "nvfp4_rowsum_workspace_bytes"]
 STATIC_SCRATCH_BYTES = 1 << 20
 
 
@@ -43,6 +47,11 @@ class QTensorStruct(ctypes.Structure):
                 ("rounding", ctypes.c_int32), ("col_has_rht", ctypes.c_int32),
                 ("rht_seed", ctypes.c_uint64), ("row_has_rht", ctypes.c_int32), ("scale_per_row", ctypes.c_int32),
                 ("row_fp16", ctypes.c_void_p), ("col_fp16", ctypes.c_void_p)]
+
+
+class CheckpointStruct(ctypes.Structure):
+    """Mirror of ``nvfp4_checkpoint``."""
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
 
 
 _lib = None
@@ -89,6 +98,21 @@ def load_library() -> ctypes.CDLL:
         L.nvfp4_rht_sign_mask.argtypes = [u64]
         L.nvfp4_selftest_conversions.restype = ci
         L.nvfp4_selftest_conversions.argtypes = [vp, vp]
+        cp, cf = ctypes.POINTER(CheckpointStruct), ctypes.c_float
+        L.nvfp4_checkpoint_sizes.restype = ci
+        L.nvfp4_checkpoint_sizes.argtypes = [i64, i64, vp, vp]
+        L.nvfp4_checkpoint_save.restype = ci
+        L.nvfp4_checkpoint_save.argtypes = [vp, ci, i64, cp, vp]
+        L.nvfp4_checkpoint_load.restype = ci
+        L.nvfp4_checkpoint_load.argtypes = [cp, ci, vp, vp, ci, i64, vp]
+        L.nvfp4_rmsnorm_forward.restype = ci
+        L.nvfp4_rmsnorm_forward.argtypes = [vp, ci, i64, vp, i64, vp, cf, i64, i64, vp, ci, i64, vp, ci, i64, vp, cp, ci, vp]
+        L.nvfp4_rmsnorm_backward.restype = ci
+        L.nvfp4_rmsnorm_backward.argtypes = [vp, ci, i64, vp, i64, cp, vp, vp, vp, i64, i64, i64, vp, ci, i64, vp, ci, vp, ctypes.c_size_t, vp]
+        L.nvfp4_activation_backward.restype = ci
+        L.nvfp4_activation_backward.argtypes = [vp, ci, i64, i64, i64, cp, ci, vp, i64, vp, ci, vp, ctypes.c_size_t, vp]
+        L.nvfp4_rowsum_workspace_bytes.restype = ci
+        L.nvfp4_rowsum_workspace_bytes.argtypes = [i64, i64, vp]
         L.nvfp4_status_string.restype = ctypes.c_char_p
         L.nvfp4_status_string.argtypes = [ci]
         L.nvfp4_version.restype = ci
@@ -339,6 +363,192 @@ def nvfp4_dequantize(q: QTensor, which_copy: int, undo_rht: bool = False, out_dt
     _check(load_library().nvfp4_dequantize(ctypes.byref(q.desc), which_copy, int(undo_rht), out.data_ptr(),
                                            out_dtype, out.stride(0), _stream()))
     return out
+
+
+# ---------------------------------------------------------------- around the linear layers
+
+_DTYPES = {torch.float32: OUT_F32, torch.bfloat16: OUT_BF16}
+_TORCH = {OUT_F32: torch.float32, OUT_BF16: torch.bfloat16}
+
+
+class Checkpoint8:
+    """An activation kept in 8 bits: `codes` uint8 [rows, cols], `scales` uint8 [rows, cols // 16], and the C descriptor."""
+    __slots__ = ("codes", "scales", "rows", "cols", "desc", "ref")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        if codes.dim() != 2 or codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or not codes.is_cuda or not scales.is_cuda or \
+                not codes.is_contiguous() or not scales.is_contiguous() or scales.shape != (codes.shape[0], codes.shape[1] // 16):
+            raise ValueError("codes and scales must be contiguous uint8 CUDA tensors [rows, cols] and [rows, cols // 16]")
+        self.codes, self.scales = codes, scales
+        self.rows, self.cols = codes.shape
+        self.desc = CheckpointStruct(self.rows, self.cols, codes.data_ptr(), scales.data_ptr())
+        self.ref = ctypes.byref(self.desc)
+
+
+class NormResult(NamedTuple):
+    y: Optional[torch.Tensor]
+    h: torch.Tensor                       # x + residual; x itself where there is no residual
+    rstd: torch.Tensor
+    checkpoint: Optional[Checkpoint8]
+
+
+def alloc_checkpoint(rows: int, cols: int, device="cuda") -> Checkpoint8:
+    _check(load_library().nvfp4_checkpoint_sizes(rows, cols, None, None))
+    return Checkpoint8(torch.empty((rows, cols), dtype=torch.uint8, device=device), torch.empty((rows, cols // 16), dtype=torch.uint8, device=device))
+
+
+def _matrix(t: torch.Tensor, what: str, shape=None) -> int:
+    """Element type of a 2-D FP32 or bf16 CUDA tensor whose rows are contiguous."""
+    dt = _DTYPES.get(t.dtype)
+    if dt is None or not t.is_cuda or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] != 1) or (shape is not None and t.shape != shape):
+        raise ValueError(f"{what} must be a 2-D float32 or bf16 CUDA tensor with unit inner stride" + (f" of shape {tuple(shape)}" if shape is not None else ""))
+    return dt
+
+
+def _ld(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])     # (torch leaves the stride of a single row open)
+
+
+def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous float32 CUDA tensor of {n} elements")
+    return t.data_ptr()
+
+
+def rowsum_workspace_bytes(rows: int, cols: int) -> int:
+    w = ctypes.c_size_t()
+    _check(load_library().nvfp4_rowsum_workspace_bytes(rows, cols, ctypes.addressof(w)))
+    return w.value
+
+
+def _rowsum_workspace(workspace: Optional[torch.Tensor], rows: int, cols: int, device):
+    if workspace is None:
+        workspace = _workspace(device, rowsum_workspace_bytes(rows, cols))
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def nvfp4_checkpoint_save(x: torch.Tensor, out: Optional[Checkpoint8] = None) -> Checkpoint8:
+    """Keep x (float32 or bf16, [rows, cols]) in 8 bits."""
+    dt = _matrix(x, "x")
+    if out is None:
+        out = alloc_checkpoint(*x.shape, x.device)
+    elif (out.rows, out.cols) != tuple(x.shape):
+        raise ValueError("out must have the shape of x")
+    _check(load_library().nvfp4_checkpoint_save(x.data_ptr(), dt, _ld(x), out.ref, _stream()))
+    return out
+
+
+def nvfp4_checkpoint_load(checkpoint: Checkpoint8, activation: int = ACT_NONE, col_scale: Optional[torch.Tensor] = None, out_dtype: int = OUT_BF16,
+                          out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """act(values) * col_scale."""
+    shape = (checkpoint.rows, checkpoint.cols)
+    if out is None:
+        out = torch.empty(shape, dtype=_TORCH[out_dtype], device=checkpoint.codes.device)
+    dt = _matrix(out, "out", shape)
+    _check(load_library().nvfp4_checkpoint_load(checkpoint.ref, activation, _vector(col_scale, shape[1], "col_scale"), out.data_ptr(), dt, _ld(out), _stream()))
+    return out
+
+
+def nvfp4_rmsnorm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                          y_dtype: Optional[int] = OUT_BF16, h_dtype: Optional[int] = None, checkpoint=False,
+                          keep_kind: int = NORM_KEEP_NORMALIZED, h: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                          rstd: Optional[torch.Tensor] = None) -> NormResult:
+    """y = norm(x + residual) * gamma.  h_dtype: type of x + residual (default: the residual's, which has to have it).  y_dtype None: no y.
+    checkpoint: True or a Checkpoint8 to keep the normalised rows (or, NORM_KEEP_OUTPUT, y) in 8 bits."""
+    xt = _matrix(x, "x")
+    rows, cols = x.shape
+    ht, rp, ldr, hp, ldh = xt, None, 0, None, 0
+    if residual is not None:
+        ht = _matrix(residual, "residual", x.shape)
+        if h_dtype is not None and h_dtype != ht:
+            raise ValueError("residual must be of type h_dtype")
+        if h is None:
+            h = torch.empty((rows, cols), dtype=residual.dtype, device=x.device)
+        elif _matrix(h, "h", x.shape) != ht:
+            raise ValueError("h must be of the residual's type")
+        rp, ldr, hp, ldh = residual.data_ptr(), _ld(residual), h.data_ptr(), _ld(h)
+    elif h is not None:
+        raise ValueError("h without a residual is x itself")
+    yt, yp, ldy = OUT_BF16, None, 0
+    if y is not None or y_dtype is not None:
+        if y is None:
+            y = torch.empty((rows, cols), dtype=_TORCH[y_dtype], device=x.device)
+        yt, yp, ldy = _matrix(y, "y", x.shape), y.data_ptr(), _ld(y)
+    if rstd is None:
+        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+    keep = None
+    if checkpoint is not None and checkpoint is not False:
+        keep = checkpoint if isinstance(checkpoint, Checkpoint8) else alloc_checkpoint(rows, cols, x.device)
+    _check(load_library().nvfp4_rmsnorm_forward(x.data_ptr(), xt, _ld(x), rp, ldr, _vector(gamma, cols, "gamma"), eps, rows, cols, hp, ht, ldh, yp, yt, ldy,
+                                                _vector(rstd, rows, "rstd"), None if keep is None else keep.ref, keep_kind, _stream()))
+    return NormResult(y, x if residual is None else h, rstd, keep)
+
+
+def nvfp4_rmsnorm_backward(dy: torch.Tensor, saved, rstd: torch.Tensor, gamma: Optional[torch.Tensor] = None, dres: Optional[torch.Tensor] = None,
+                           dx_dtype: Optional[int] = None, dx: Optional[torch.Tensor] = None, dgamma: Optional[torch.Tensor] = None,
+                           accumulate_dgamma: bool = False, workspace: Optional[torch.Tensor] = None):
+    """saved: the norm's input h, or the Checkpoint8 of the normalised rows.  h, dres and dx are of one type (dx_dtype; default: h's, dres's or dy's).
+    dgamma: float32 [cols], added into with accumulate_dgamma.  Returns (dx, dgamma)."""
+    dt = _matrix(dy, "dy")
+    rows, cols = dy.shape
+    st = dx_dtype
+    hp, ldh, sp, rp, ldr = None, 0, None, None, 0
+    if isinstance(saved, Checkpoint8):
+        sp = saved.ref
+    else:
+        st = _one_type(st, _matrix(saved, "saved", dy.shape))
+        hp, ldh = saved.data_ptr(), _ld(saved)
+    if dres is not None:
+        st = _one_type(st, _matrix(dres, "dres", dy.shape))
+        rp, ldr = dres.data_ptr(), _ld(dres)
+    if dx is not None:
+        st = _one_type(st, _matrix(dx, "dx", dy.shape))
+    else:
+        st = dt if st is None else st
+        dx = torch.empty((rows, cols), dtype=_TORCH[st], device=dy.device)
+    if dgamma is None:
+        if accumulate_dgamma:
+            raise ValueError("accumulate_dgamma needs dgamma")
+        dgamma = torch.empty(cols, dtype=torch.float32, device=dy.device)
+    ws, ws_bytes = _rowsum_workspace(workspace, rows, cols, dy.device)
+    _check(load_library().nvfp4_rmsnorm_backward(dy.data_ptr(), dt, _ld(dy), hp, ldh, sp, _vector(rstd, rows, "rstd"), _vector(gamma, cols, "gamma"), rp, ldr,
+                                                 rows, cols, dx.data_ptr(), st, _ld(dx), _vector(dgamma, cols, "dgamma"), int(accumulate_dgamma), ws, ws_bytes,
+                                                 _stream()))
+    return dx, dgamma
+
+
+def _one_type(a: Optional[int], b: int) -> int:
+    if a is not None and a != b:
+        raise ValueError("saved, dres and dx must be of one type")
+    return b
+
+
+def nvfp4_activation_backward(da: torch.Tensor, saved: Optional[Checkpoint8] = None, activation: int = ACT_NONE, bias_grad: bool = True, want_dz: bool = True,
+                              dz: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None, accumulate_dbias: bool = False,
+                              workspace: Optional[torch.Tensor] = None):
+    """dz = da * act'(z) from z's checkpoint, dbias = the sum of dz over rows (float32 [cols], added into with accumulate_dbias).
+    Returns (dz, dbias), None for what is not asked for."""
+    dt = _matrix(da, "da")
+    rows, cols = da.shape
+    zp, ldz = None, 0
+    if want_dz:
+        if dz is None:
+            dz = torch.empty((rows, cols), dtype=da.dtype, device=da.device)
+        elif _matrix(dz, "dz", da.shape) != dt:
+            raise ValueError("dz must be of the type of da")
+        zp, ldz = dz.data_ptr(), _ld(dz)
+    ws, ws_bytes = None, 0
+    if bias_grad:
+        if dbias is None:
+            if accumulate_dbias:
+                raise ValueError("accumulate_dbias needs dbias")
+            dbias = torch.empty(cols, dtype=torch.float32, device=da.device)
+        ws, ws_bytes = _rowsum_workspace(workspace, rows, cols, da.device)
+    _check(load_library().nvfp4_activation_backward(da.data_ptr(), dt, _ld(da), rows, cols, None if saved is None else saved.ref, activation, zp, ldz,
+                                                    _vector(dbias, cols, "dbias") if bias_grad else None, int(accumulate_dbias), ws, ws_bytes, _stream()))
+    return dz if want_dz else None, dbias if bias_grad else None
 
 
 def nvfp4_selftest_conversions() -> list:

@@ -487,6 +487,141 @@ int nvfp4_dequantize(const nvfp4_qtensor* q, int which_copy, int undo_rht, void*
   return e == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
 }
 
+// ---------------------------------------------------------------- around the linear layers
+
+namespace {
+
+bool element_type(int t) { return t == NVFP4_OUT_F32 || t == NVFP4_OUT_BF16; }
+bool activation(int a) { return a >= NVFP4_ACT_NONE && a <= NVFP4_ACT_SILU; }
+// (the kernels number the rows' workgroups with 31 bits)
+bool good_shape(int64_t rows, int64_t cols) { return rows >= 0 && rows <= 0x7fffffff && cols > 0 && cols <= 0x7fffffff && cols % 16 == 0; }
+bool good_ld(int64_t ld, int64_t cols) { return ld >= cols && ld % 8 == 0; }
+constexpr int64_t kMostNormCols = 32768;
+
+// A tensor that has to be there (unless it has no rows), or one that may be absent.
+int check_tensor(const void* p, int64_t rows, int64_t cols, int64_t ld, bool may_be_null) {
+  if (!p) return may_be_null || rows == 0 ? NVFP4_OK : NVFP4_ERR_INVALID_ARG;
+  if (!good_ld(ld, cols)) return NVFP4_ERR_BAD_SHAPE;
+  return aligned(p, 16) ? NVFP4_OK : NVFP4_ERR_INVALID_ARG;
+}
+
+int check_checkpoint(const nvfp4_checkpoint* c, int64_t rows, int64_t cols) {
+  if (c->rows != rows || c->cols != cols) return NVFP4_ERR_MISMATCH;
+  if (rows && (!c->codes || !c->scales)) return NVFP4_ERR_INVALID_ARG;
+  return aligned(c->codes, 16) ? NVFP4_OK : NVFP4_ERR_INVALID_ARG;
+}
+
+size_t rowsum_workspace(int64_t rows, int64_t cols) {
+  const size_t norm = cols <= kMostNormCols ? rmsnorm_partial_bytes(rows, cols) : 0, act = activation_partial_bytes(rows, cols);
+  return norm > act ? norm : act;
+}
+
+}  // namespace
+
+int nvfp4_checkpoint_sizes(int64_t rows, int64_t cols, size_t* codes_bytes, size_t* scales_bytes) {
+  if (!good_shape(rows, cols)) return NVFP4_ERR_BAD_SHAPE;
+  if (codes_bytes) *codes_bytes = static_cast<size_t>(rows) * static_cast<size_t>(cols);
+  if (scales_bytes) *scales_bytes = static_cast<size_t>(rows) * static_cast<size_t>(cols) / 16;
+  return NVFP4_OK;
+}
+
+int nvfp4_rowsum_workspace_bytes(int64_t rows, int64_t cols, size_t* workspace_bytes) {
+  if (!good_shape(rows, cols)) return NVFP4_ERR_BAD_SHAPE;
+  if (!workspace_bytes) return NVFP4_ERR_INVALID_ARG;
+  *workspace_bytes = rowsum_workspace(rows, cols);
+  return NVFP4_OK;
+}
+
+int nvfp4_checkpoint_save(const void* x, int x_dtype, int64_t ldx, const nvfp4_checkpoint* out, nvfp4_stream_t stream) {
+  if (!out || !element_type(x_dtype)) return NVFP4_ERR_INVALID_ARG;
+  if (!good_shape(out->rows, out->cols)) return NVFP4_ERR_BAD_SHAPE;
+  int rc = check_tensor(x, out->rows, out->cols, ldx, false);
+  if (rc == NVFP4_OK) rc = check_checkpoint(out, out->rows, out->cols);
+  if (rc != NVFP4_OK) return rc;
+  const hipError_t e = launch_checkpoint_save(x, x_dtype == NVFP4_OUT_BF16, out->rows, out->cols, ldx, static_cast<uint8_t*>(out->codes),
+                                              static_cast<uint8_t*>(out->scales), static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
+}
+
+int nvfp4_checkpoint_load(const nvfp4_checkpoint* c, int act, const float* col_scale, void* out, int out_dtype, int64_t ld_out, nvfp4_stream_t stream) {
+  if (!c || !element_type(out_dtype) || !activation(act)) return NVFP4_ERR_INVALID_ARG;
+  if (!good_shape(c->rows, c->cols)) return NVFP4_ERR_BAD_SHAPE;
+  int rc = check_checkpoint(c, c->rows, c->cols);
+  if (rc == NVFP4_OK) rc = check_tensor(out, c->rows, c->cols, ld_out, false);
+  if (rc != NVFP4_OK) return rc;
+  if (!aligned(col_scale, 16)) return NVFP4_ERR_INVALID_ARG;
+  const hipError_t e = launch_checkpoint_load(static_cast<const uint8_t*>(c->codes), static_cast<const uint8_t*>(c->scales), c->rows, c->cols, act, col_scale,
+                                              out, out_dtype == NVFP4_OUT_BF16, ld_out, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
+}
+
+int nvfp4_rmsnorm_forward(const void* x, int x_dtype, int64_t ldx, const void* residual, int64_t ldr, const float* gamma, float eps, int64_t rows,
+                          int64_t cols, void* h, int h_dtype, int64_t ldh, void* y, int y_dtype, int64_t ldy, float* rstd, const nvfp4_checkpoint* keep,
+                          int keep_kind, nvfp4_stream_t stream) {
+  if (!element_type(x_dtype) || !element_type(h_dtype) || !element_type(y_dtype) || !(eps >= 0.0f)) return NVFP4_ERR_INVALID_ARG;
+  if (keep_kind != NVFP4_NORM_KEEP_NORMALIZED && keep_kind != NVFP4_NORM_KEEP_OUTPUT) return NVFP4_ERR_INVALID_ARG;
+  if (!good_shape(rows, cols) || cols > kMostNormCols) return NVFP4_ERR_BAD_SHAPE;
+  int rc = check_tensor(x, rows, cols, ldx, false);
+  if (rc == NVFP4_OK) rc = check_tensor(residual, rows, cols, ldr, true);
+  if (rc == NVFP4_OK) rc = check_tensor(h, rows, cols, ldh, true);
+  if (rc == NVFP4_OK) rc = check_tensor(y, rows, cols, ldy, true);
+  if (rc == NVFP4_OK && keep) rc = check_checkpoint(keep, rows, cols);
+  if (rc != NVFP4_OK) return rc;
+  if (!aligned(gamma, 16) || !aligned(rstd, 4)) return NVFP4_ERR_INVALID_ARG;
+  RmsNormForward a{};
+  a.x = x, a.residual = residual, a.gamma = gamma;
+  a.rows = rows, a.cols = cols, a.ldx = ldx, a.ldr = ldr, a.ldh = ldh, a.ldy = ldy;
+  a.eps = eps;
+  a.x_bf16 = x_dtype == NVFP4_OUT_BF16, a.h_bf16 = h_dtype == NVFP4_OUT_BF16, a.y_bf16 = y_dtype == NVFP4_OUT_BF16;
+  a.codes_of_y = keep_kind == NVFP4_NORM_KEEP_OUTPUT;
+  a.h = h, a.y = y, a.rstd = rstd;
+  if (keep) a.codes = static_cast<uint8_t*>(keep->codes), a.scales = static_cast<uint8_t*>(keep->scales);
+  return launch_rmsnorm_forward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
+}
+
+int nvfp4_rmsnorm_backward(const void* dy, int dy_dtype, int64_t lddy, const void* h, int64_t ldh, const nvfp4_checkpoint* saved, const float* rstd,
+                           const float* gamma, const void* dres, int64_t lddr, int64_t rows, int64_t cols, void* dx, int s_dtype, int64_t lddx,
+                           float* dgamma, int accumulate, void* workspace, size_t workspace_bytes, nvfp4_stream_t stream) {
+  if (!element_type(dy_dtype) || !element_type(s_dtype) || (h && saved) || (!h && !saved && rows != 0)) return NVFP4_ERR_INVALID_ARG;
+  if (!good_shape(rows, cols) || cols > kMostNormCols) return NVFP4_ERR_BAD_SHAPE;
+  int rc = check_tensor(dy, rows, cols, lddy, false);
+  if (rc == NVFP4_OK) rc = check_tensor(h, rows, cols, ldh, true);
+  if (rc == NVFP4_OK && saved) rc = check_checkpoint(saved, rows, cols);
+  if (rc == NVFP4_OK) rc = check_tensor(dres, rows, cols, lddr, true);
+  if (rc == NVFP4_OK) rc = check_tensor(dx, rows, cols, lddx, true);
+  if (rc != NVFP4_OK) return rc;
+  if ((!rstd && rows) || !aligned(rstd, 4) || !aligned(gamma, 16) || !aligned(dgamma, 16)) return NVFP4_ERR_INVALID_ARG;
+  if (dgamma && rowsum_workspace(rows, cols) && (!workspace || !aligned(workspace, 16) || workspace_bytes < rowsum_workspace(rows, cols)))
+    return NVFP4_ERR_WORKSPACE;
+  RmsNormBackward a{};
+  a.dy = dy, a.h = h, a.rstd = rstd, a.gamma = gamma, a.dres = dres, a.dx = dx;
+  if (saved) a.codes = static_cast<const uint8_t*>(saved->codes), a.scales = static_cast<const uint8_t*>(saved->scales);
+  a.rows = rows, a.cols = cols, a.lddy = lddy, a.ldh = ldh, a.lddr = lddr, a.lddx = lddx;
+  a.dy_bf16 = dy_dtype == NVFP4_OUT_BF16, a.s_bf16 = s_dtype == NVFP4_OUT_BF16;
+  a.dgamma = dgamma, a.accumulate = accumulate != 0, a.partials = static_cast<float*>(workspace);
+  return launch_rmsnorm_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
+}
+
+int nvfp4_activation_backward(const void* da, int dtype, int64_t ldda, int64_t rows, int64_t cols, const nvfp4_checkpoint* saved, int act, void* dz,
+                              int64_t lddz, float* dbias, int accumulate, void* workspace, size_t workspace_bytes, nvfp4_stream_t stream) {
+  if (!element_type(dtype) || !activation(act) || (act != NVFP4_ACT_NONE && !saved)) return NVFP4_ERR_INVALID_ARG;
+  if (!good_shape(rows, cols)) return NVFP4_ERR_BAD_SHAPE;
+  int rc = check_tensor(da, rows, cols, ldda, false);
+  if (rc == NVFP4_OK && saved) rc = check_checkpoint(saved, rows, cols);
+  if (rc == NVFP4_OK) rc = check_tensor(dz, rows, cols, lddz, true);
+  if (rc != NVFP4_OK) return rc;
+  if (!aligned(dbias, 16)) return NVFP4_ERR_INVALID_ARG;
+  if (dbias && rowsum_workspace(rows, cols) && (!workspace || !aligned(workspace, 16) || workspace_bytes < rowsum_workspace(rows, cols)))
+    return NVFP4_ERR_WORKSPACE;
+  ActivationBackward a{};
+  a.da = da, a.dz = dz, a.act = act;
+  if (saved) a.codes = static_cast<const uint8_t*>(saved->codes), a.scales = static_cast<const uint8_t*>(saved->scales);
+  a.rows = rows, a.cols = cols, a.ldda = ldda, a.lddz = lddz;
+  a.bf16 = dtype == NVFP4_OUT_BF16;
+  a.dbias = dbias, a.accumulate = accumulate != 0, a.partials = static_cast<float*>(workspace);
+  return launch_activation_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
+}
+
 int nvfp4_selftest_conversions(uint64_t* mismatches, nvfp4_stream_t stream) {
   if (!mismatches || !aligned(mismatches, 8)) return NVFP4_ERR_INVALID_ARG;
   return run_selftest(mismatches, static_cast<hipStream_t>(stream)) == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;

@@ -1,0 +1,38 @@
+// Sums over rows, second half: a backward kernel leaves partial sums [parts, cols] in its workspace, one row per workgroup, and this launch adds
+// them in a fixed order.  No atomics: the same inputs give the same bits.
+#include "nvfp4_internal.h"
+#include "nvfp4_device.h"
+
+namespace nvfp4 {
+
+namespace {
+
+// 64 columns per workgroup: 16 lanes of four columns each, 16 of which share the parts.
+__global__ __launch_bounds__(256) void colsum_kernel(const float* __restrict__ partials, int parts, int64_t cols, float* __restrict__ out, bool accumulate) {
+  __shared__ float4v sums[16][16];
+  const int c = threadIdx.x & 15, p0 = threadIdx.x >> 4;
+  const int64_t col = static_cast<int64_t>(blockIdx.x) * 64 + c * 4;
+  float4v s = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (col < cols) {
+#pragma unroll 8
+    for (int p = p0; p < parts; p += 16) s += *reinterpret_cast<const float4v*>(partials + p * cols + col);
+  }
+  sums[p0][c] = s;
+  __syncthreads();
+  if (p0 == 0 && col < cols) {
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s += sums[i][c];
+    float4v* to = reinterpret_cast<float4v*>(out + col);
+    *to = accumulate ? *to + s : s;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_colsum(const float* partials, int parts, int64_t cols, float* out, bool accumulate, hipStream_t s) {
+  if (parts == 0 && accumulate) return hipSuccess;
+  hipLaunchKernelGGL(colsum_kernel, dim3(static_cast<unsigned>((cols + 63) / 64)), dim3(256), 0, s, partials, parts, cols, out, accumulate);
+  return hipGetLastError();
+}
+
+}  // namespace nvfp4

@@ -150,6 +150,53 @@ struct DequantArgs {
 hipError_t launch_dequantize(const DequantArgs& d, hipStream_t s);
 hipError_t launch_dequantize_mx(const DequantArgs& d, hipStream_t s);   // scales are UE8M0 per 32
 
+// ---------------------------------------------------------------- around the linear layers: norm, 8-bit checkpoints, activations
+struct RmsNormForward {
+  const void* x;
+  const void* residual;    // or null; of h's type
+  const float* gamma;      // or null
+  int64_t rows, cols, ldx, ldr, ldh, ldy;
+  float eps;
+  bool x_bf16, h_bf16, y_bf16, codes_of_y;
+  void *h, *y;             // each may be null
+  float* rstd;             // or null
+  uint8_t *codes, *scales; // or both null
+};
+hipError_t launch_rmsnorm_forward(const RmsNormForward& a, hipStream_t s);
+struct RmsNormBackward {
+  const void* dy;
+  const void* h;                  // the norm's input, or
+  const uint8_t *codes, *scales;  // 8 bits of the normalised rows
+  const float *rstd, *gamma;      // gamma may be null
+  const void* dres;               // or null
+  void* dx;                       // or null
+  int64_t rows, cols, lddy, ldh, lddr, lddx;
+  bool dy_bf16, s_bf16;           // s: h, dres and dx
+  float* dgamma;                  // or null
+  bool accumulate;
+  float* partials;
+};
+hipError_t launch_rmsnorm_backward(const RmsNormBackward& a, hipStream_t s);
+size_t rmsnorm_partial_bytes(int64_t rows, int64_t cols);
+hipError_t launch_checkpoint_save(const void* x, bool bf16, int64_t rows, int64_t cols, int64_t ldx, uint8_t* codes, uint8_t* scales, hipStream_t s);
+hipError_t launch_checkpoint_load(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, int act, const float* col_scale, void* out, bool bf16,
+                                  int64_t ld_out, hipStream_t s);
+struct ActivationBackward {
+  const void* da;
+  const uint8_t *codes, *scales;  // null without an activation
+  int act;
+  void* dz;                       // or null
+  int64_t rows, cols, ldda, lddz;
+  bool bf16;                      // da and dz
+  float* dbias;                   // or null
+  bool accumulate;
+  float* partials;
+};
+hipError_t launch_activation_backward(const ActivationBackward& a, hipStream_t s);
+size_t activation_partial_bytes(int64_t rows, int64_t cols);
+// out <- (out +) the sum of `parts` rows of partial sums, in a fixed order
+hipError_t launch_colsum(const float* partials, int parts, int64_t cols, float* out, bool accumulate, hipStream_t s);
+
 hipError_t run_selftest(uint64_t* mismatches_dev, hipStream_t s);
 
 // Host Philox4x32-10, used only to derive the sign diagonal from a seed (16 bits, or 32 for the MXFP4 mode).
