@@ -395,6 +395,30 @@ int nvfp4_rmsnorm_backward(const void* dy, int dy_dtype, int64_t lddy, const voi
 int nvfp4_activation_backward(const void* da, int dtype, int64_t ldda, int64_t rows, int64_t cols, const nvfp4_checkpoint* saved, int activation, void* dz,
                               int64_t lddz, float* dbias, int accumulate, void* workspace, size_t workspace_bytes, nvfp4_stream_t stream);
 
+/*
+ * nvfp4_gemm with what follows a linear layer done to its result before it is stored:
+ *   z = A B + bias;  8 bits of z are kept;  D = act(z) + residual
+ * or, on the way back (Dgrad through a layer whose input came out of an activation),
+ *   D = (A B) act'(z), z from the 8 bits that the forward pass kept.
+ *   bias      FP32 [N], 16-byte aligned, or NULL
+ *   residual  [M, N] of type residual_dtype, leading dimension ldr, or NULL
+ *   keep      the checkpoint that z goes to, or NULL
+ *   grad_of   the checkpoint of z for the second form; then bias, residual and keep are NULL
+ * a, b, op, D, ldd, workspace as in nvfp4_gemm (either format, tensor-level scales of either granularity); out_dtype
+ * NVFP4_OUT_F32 or NVFP4_OUT_BF16.  All of it happens to the FP32 result, D is rounded once.
+ */
+typedef struct nvfp4_epilogue {
+  const float* bias;
+  const void* residual;
+  int64_t ldr;
+  const nvfp4_checkpoint* keep;
+  const nvfp4_checkpoint* grad_of;
+  int32_t residual_dtype;
+  int32_t activation;
+} nvfp4_epilogue;
+int nvfp4_gemm_epilogue(const nvfp4_qtensor* a, const nvfp4_qtensor* b, int op, const nvfp4_epilogue* epilogue, void* d, int out_dtype, int64_t ldd,
+                        void* workspace, size_t workspace_bytes, nvfp4_stream_t stream);
+
 /* Bytes of the workspace that either backward call needs for its sums over rows (host pointer out); may be 0. */
 int nvfp4_rowsum_workspace_bytes(int64_t rows, int64_t cols, size_t* workspace_bytes);
 

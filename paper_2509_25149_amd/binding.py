@@ -32,7 +32,7 @@ EXPORTS = ["nvfp4_quantized_sizes", "nvfp4_quantize", "nvfp4_gemm", "nvfp4_gemm_
            "nvfp4_linear_workspace_bytes", "nvfp4_linear_forward", "nvfp4_linear_backward",
            "nvfp4_amax", "nvfp4_quantize_with_amax", "nvfp4_quantize_static", "nvfp4_predecode",
            "nvfp4_checkpoint_sizes", "nvfp4_checkpoint_save", "nvfp4_checkpoint_load", "nvfp4_rmsnorm_forward", "nvfp4_rmsnorm_backward",
-           "nvfp4_activation_backward", "nvfp4_rowsum_workspace_bytes"]
+           "nvfp4_activation_backward", "nvfp4_rowsum_workspace_bytes", "nvfp4_gemm_epilogue"]
 STATIC_SCRATCH_BYTES = 1 << 20
 
 
@@ -52,6 +52,12 @@ class QTensorStruct(ctypes.Structure):
 class CheckpointStruct(ctypes.Structure):
     """Mirror of ``nvfp4_checkpoint``."""
     _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class EpilogueStruct(ctypes.Structure):
+    """Mirror of ``nvfp4_epilogue``."""
+    _fields_ = [("bias", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64), ("keep", ctypes.POINTER(CheckpointStruct)),
+                ("grad_of", ctypes.POINTER(CheckpointStruct)), ("residual_dtype", ctypes.c_int32), ("activation", ctypes.c_int32)]
 
 
 _lib = None
@@ -111,6 +117,8 @@ def load_library() -> ctypes.CDLL:
         L.nvfp4_rmsnorm_backward.argtypes = [vp, ci, i64, vp, i64, cp, vp, vp, vp, i64, i64, i64, vp, ci, i64, vp, ci, vp, ctypes.c_size_t, vp]
         L.nvfp4_activation_backward.restype = ci
         L.nvfp4_activation_backward.argtypes = [vp, ci, i64, i64, i64, cp, ci, vp, i64, vp, ci, vp, ctypes.c_size_t, vp]
+        L.nvfp4_gemm_epilogue.restype = ci
+        L.nvfp4_gemm_epilogue.argtypes = [qp, qp, ci, ctypes.POINTER(EpilogueStruct), vp, ci, i64, vp, ctypes.c_size_t, vp]
         L.nvfp4_rowsum_workspace_bytes.restype = ci
         L.nvfp4_rowsum_workspace_bytes.argtypes = [i64, i64, vp]
         L.nvfp4_status_string.restype = ctypes.c_char_p
@@ -549,6 +557,34 @@ def nvfp4_activation_backward(da: torch.Tensor, saved: Optional[Checkpoint8] = N
     _check(load_library().nvfp4_activation_backward(da.data_ptr(), dt, _ld(da), rows, cols, None if saved is None else saved.ref, activation, zp, ldz,
                                                     _vector(dbias, cols, "dbias") if bias_grad else None, int(accumulate_dbias), ws, ws_bytes, _stream()))
     return dz if want_dz else None, dbias if bias_grad else None
+
+
+def nvfp4_gemm_epilogue(a: QTensor, b: QTensor, op: int, bias: Optional[torch.Tensor] = None, activation: int = ACT_NONE,
+                        residual: Optional[torch.Tensor] = None, keep: Optional[Checkpoint8] = None, grad_of: Optional[Checkpoint8] = None,
+                        out_dtype: int = OUT_BF16, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """act(A B + bias) + residual, what goes into act kept in 8 bits in `keep`; or, with grad_of, (A B) * act'(values of grad_of).  Operands and workspace
+    as for nvfp4_gemm."""
+    m = a.cols if op == OP_WGRAD else a.rows
+    n = b.rows if op == OP_DGRAD else b.cols
+    e = EpilogueStruct(activation=activation)
+    if bias is not None:
+        e.bias = _vector(bias, n, "bias")
+    if residual is not None:
+        e.residual_dtype = _matrix(residual, "residual", (m, n))
+        e.residual, e.ldr = residual.data_ptr(), _ld(residual)
+    if keep is not None:
+        e.keep = ctypes.pointer(keep.desc)
+    if grad_of is not None:
+        e.grad_of = ctypes.pointer(grad_of.desc)
+    if out is None:
+        dev = (a.row_codes if a.row_codes is not None else a.col_codes).device
+        out = torch.empty((m, n), dtype=_TORCH[out_dtype], device=dev)
+    elif _matrix(out, "out", (m, n)) != out_dtype:
+        raise ValueError("out must be of type out_dtype")
+    ws_ptr, ws_bytes = (workspace.data_ptr(), workspace.numel()) if workspace is not None else (None, 0)
+    _check(load_library().nvfp4_gemm_epilogue(ctypes.byref(a.desc), ctypes.byref(b.desc), op, ctypes.byref(e), out.data_ptr(), out_dtype, _ld(out), ws_ptr, ws_bytes,
+                                              _stream()))
+    return out
 
 
 def nvfp4_selftest_conversions() -> list:

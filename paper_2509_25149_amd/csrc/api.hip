@@ -622,6 +622,58 @@ int nvfp4_activation_backward(const void* da, int dtype, int64_t ldda, int64_t r
   return launch_activation_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
 }
 
+// A validated nvfp4_gemm_epilogue call.
+static int plan_epilogue(const nvfp4_epilogue* p, int out_dtype, GemmArgs* g, GemmEpilogue* e) {
+  if (!p || !element_type(out_dtype) || !activation(p->activation)) return NVFP4_ERR_INVALID_ARG;
+  const int64_t M = g->a.outer, N = g->b.outer;
+  *e = GemmEpilogue{};
+  if (p->grad_of) {
+    if (p->bias || p->residual || p->keep) return NVFP4_ERR_INVALID_ARG;
+    const int rc = check_checkpoint(p->grad_of, M, N);
+    if (rc != NVFP4_OK) return rc;
+    e->grad_codes = static_cast<const uint8_t*>(p->grad_of->codes), e->grad_scales = static_cast<const uint8_t*>(p->grad_of->scales);
+  }
+  if (!aligned(p->bias, 16)) return NVFP4_ERR_INVALID_ARG;
+  if (p->residual) {
+    if (!element_type(p->residual_dtype)) return NVFP4_ERR_INVALID_ARG;
+    const int rc = check_tensor(p->residual, M, N, p->ldr, false);
+    if (rc != NVFP4_OK) return rc;
+  }
+  if (p->keep) {
+    const int rc = check_checkpoint(p->keep, M, N);
+    if (rc != NVFP4_OK) return rc;
+    e->keep_codes = static_cast<uint8_t*>(p->keep->codes), e->keep_scales = static_cast<uint8_t*>(p->keep->scales);
+  }
+  e->bias = p->bias, e->residual = p->residual, e->ldr = p->ldr;
+  e->cols = N, e->act = p->activation;
+  e->residual_bf16 = p->residual_dtype == NVFP4_OUT_BF16, e->out_bf16 = out_dtype == NVFP4_OUT_BF16;
+  g->epilogue = e;
+  return NVFP4_OK;
+}
+
+int nvfp4_gemm_epilogue(const nvfp4_qtensor* a, const nvfp4_qtensor* b, int op, const nvfp4_epilogue* epilogue, void* d, int out_dtype, int64_t ldd,
+                        void* workspace, size_t workspace_bytes, nvfp4_stream_t stream) {
+  GemmArgs g;
+  GemmEpilogue e;
+  int rc = plan_gemm(a, b, op, d, out_dtype, ldd, workspace, workspace_bytes, &g);
+  if (rc == NVFP4_OK) rc = plan_epilogue(epilogue, out_dtype, &g, &e);
+  if (rc != NVFP4_OK) return rc;
+  const hipError_t err = g.mx ? launch_gemm_mx(g, static_cast<hipStream_t>(stream)) : launch_gemm(g, static_cast<hipStream_t>(stream));
+  return err == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
+}
+
+// For the tests, not part of the ABI: as nvfp4_internal_gemm_direct.
+int nvfp4_internal_gemm_epilogue_direct(const nvfp4_qtensor* a, const nvfp4_qtensor* b, int op, const nvfp4_epilogue* epilogue, void* d, int out_dtype,
+                                        int64_t ldd, int shape, nvfp4_stream_t stream) {
+  GemmArgs g;
+  GemmEpilogue e;
+  int rc = plan_gemm(a, b, op, d, out_dtype, ldd, nullptr, 0, &g);
+  if (rc == NVFP4_OK) rc = plan_epilogue(epilogue, out_dtype, &g, &e);
+  if (rc != NVFP4_OK) return rc;
+  if (g.mx) return NVFP4_ERR_INVALID_ARG;
+  return launch_gemm_direct(g, shape, static_cast<hipStream_t>(stream)) == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
+}
+
 int nvfp4_selftest_conversions(uint64_t* mismatches, nvfp4_stream_t stream) {
   if (!mismatches || !aligned(mismatches, 8)) return NVFP4_ERR_INVALID_ARG;
   return run_selftest(mismatches, static_cast<hipStream_t>(stream)) == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;

@@ -88,8 +88,15 @@ __device__ __forceinline__ void checkpoint_values4(uint32_t codes, uint32_t byte
 // Numbers of include/nvfp4.h's NVFP4_ACT_*.
 enum { kActNone = 0, kActRelu2 = 1, kActGelu = 2, kActSilu = 3 };
 
-__device__ __forceinline__ float exp_minus(float p) { return __builtin_amdgcn_exp2f(-1.4426950408889634f * p); }
-__device__ __forceinline__ float logistic(float p) { return __builtin_amdgcn_rcpf(1.0f + exp_minus(p)); }
+// s(p) and s (1 - s) from q = exp(-|p|): 1 / (1 + q), or q / (1 + q) below zero, and q / (1 + q)^2.  q is a square because the exponential instruction has no
+// subnormal results and a product has: nothing is flushed to zero before it is below the smallest number.
+struct Logistic {
+  float s, t;
+};
+__device__ __forceinline__ Logistic logistic(float p) {
+  const float w = __builtin_amdgcn_exp2f(__builtin_fabsf(p) * -0.72134752044448170f), q = w * w, r = __builtin_amdgcn_rcpf(1.0f + q), qr = q * r;
+  return {p < 0.0f ? qr : r, qr * r};
+}
 
 template <int kN>
 __device__ __forceinline__ void activate(float (&v)[kN], int act) {
@@ -102,11 +109,11 @@ __device__ __forceinline__ void activate(float (&v)[kN], int act) {
   } else if (act != kActNone) {
     const float c1 = act == kActSilu ? 1.0f : 1.5957691216057308f, c3 = act == kActSilu ? 0.0f : 0.07135481282988394f;
 #pragma unroll
-    for (int i = 0; i < kN; ++i) v[i] *= logistic(v[i] * __builtin_fmaf(c3 * v[i], v[i], c1));
+    for (int i = 0; i < kN; ++i) v[i] *= logistic(v[i] * __builtin_fmaf(c3 * v[i], v[i], c1)).s;
   }
 }
 
-// v <- derivative at v.  With p the logistic function's argument, e = exp(-p) and s its value, (z s)' = s + z s (1 - s) p', and 1 - s = e s.
+// v <- derivative at v: (z s(p))' = s + z s (1 - s) p'.
 template <int kN>
 __device__ __forceinline__ void activation_slope(float (&v)[kN], int act) {
   if (act == kActRelu2) {
@@ -119,8 +126,9 @@ __device__ __forceinline__ void activation_slope(float (&v)[kN], int act) {
     const float c1 = act == kActSilu ? 1.0f : 1.5957691216057308f, c3 = act == kActSilu ? 0.0f : 0.07135481282988394f;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const float z = v[i], e = exp_minus(z * __builtin_fmaf(c3 * z, z, c1)), s = __builtin_amdgcn_rcpf(1.0f + e), t = s * (e * s);
-      v[i] = s + (t > 0.0f ? z * t * __builtin_fmaf(3.0f * c3 * z, z, c1) : 0.0f);   // (far out t is 0, or infinity times 0, and the polynomial infinite)
+      const float z = v[i];
+      const Logistic l = logistic(z * __builtin_fmaf(c3 * z, z, c1));
+      v[i] = l.s + (l.t > 0.0f ? z * l.t * __builtin_fmaf(3.0f * c3 * z, z, c1) : 0.0f);   // (far out t is 0 and the polynomial infinite)
     }
   }
 }

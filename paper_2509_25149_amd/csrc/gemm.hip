@@ -57,9 +57,10 @@ __device__ __forceinline__ void stage_row(const Operand& op, int64_t K, int64_t 
   dst[3] = decode8_f16(c23.y, h1);
 }
 
-template <bool kBf16Out>
+// kKind: kNoEpilogue, or kForward for an epilogue of any kind (then the output type is the epilogue's).
+template <bool kBf16Out, int kKind>
 __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(Operand A, Operand B, int64_t K,
-                                                            void* __restrict__ Dv, int64_t ldd, bool accumulate) {
+                                                            void* __restrict__ Dv, int64_t ldd, bool accumulate, EpilogueArg<kKind> epilogue) {
   __shared__ __attribute__((aligned(16))) _Float16 As[BM * LDS_LD];
   __shared__ __attribute__((aligned(16))) _Float16 Bs[BN * LDS_LD];
 
@@ -110,6 +111,25 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(Operand A, Operand B
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int m = wm * 64 + i * 32 + l32;
+    if constexpr (kKind != kNoEpilogue) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {   // a 16-column block
+          const int n = wn * 64 + j * 32 + q * 8, first = (lane >> 5) * 4;
+          if (n >= N) continue;            // (alike in all lanes)
+          float4v v[2];
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            const float4v sc = scale4(ts, out_scale, vec, m < M, m0 + m, n0 + n + first + 8 * g);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) v[g][t] = acc[i][j][(q + g) * 4 + t] * sc[t];
+          }
+          finish_block<2>(v, epilogue, Dv, ldd, m0 + m, n0 + n, first, m < M);
+        }
+      }
+      continue;
+    }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
 #pragma unroll
@@ -229,10 +249,10 @@ __device__ __forceinline__ void mma_tile(float4v (&acc)[8][4], const char* at, c
   mma_step(acc, f1);
 }
 
-template <bool kBf16Out>
+template <bool kBf16Out, int kKind>
 __global__ __launch_bounds__(kBigThreads) void gemm_kernel_256(Operand A, Operand B, int64_t K,
                                                                void* __restrict__ Dv, int64_t ldd, bool accumulate,
-                                                               int tiles_m, int tiles_n) {
+                                                               int tiles_m, int tiles_n, EpilogueArg<kKind> epilogue) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
 
   // Workgroup -> output tile.  Consecutive workgroup ids land on different XCDs
@@ -310,7 +330,10 @@ __global__ __launch_bounds__(kBigThreads) void gemm_kernel_256(Operand A, Operan
       const int n = wn * 64 + j * 16 + lq * 4;
       if (m < M && n < N) {  // N is a multiple of 16, so the 4 columns are in or out together
         float4v v = acc[i][j] * scale4(ts, out_scale, vec, true, m0 + m, n0 + n);
-        if (kBf16Out) {
+        if constexpr (kKind != kNoEpilogue) {   // (rows and columns come in multiples of 16: all lanes are here)
+          float4v block[1] = {v};
+          finish_block<1>(block, epilogue, Dv, ldd, m0 + m, n0 + n - lq * 4, lq * 4, true);
+        } else if (kBf16Out) {
           uint16_t* d = static_cast<uint16_t*>(Dv) + (m0 + m) * ldd + n0 + n;
           uint2 o;
           o.x = f32x2_to_bf16(v[0], v[1]);
@@ -338,27 +361,30 @@ static double fused_us(int64_t M, int64_t N, int64_t K) {
 // The 128 x 128 kernel, in the same terms (steps of 64 k; three workgroups fit a CU).
 static constexpr SmallTileCost kTile128Cost{3, 1.49, 1.37, 0.817};
 
-static hipError_t launch_tile128(const GemmArgs& g, hipStream_t s) {
+template <bool kBf16Out, int kKind>
+static hipError_t launch_tile128_as(const GemmArgs& g, const EpilogueArg<kKind>& e, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>((g.b.outer + BN - 1) / BN), static_cast<unsigned>((g.a.outer + BM - 1) / BM));
-  if (g.out_bf16)
-    hipLaunchKernelGGL(gemm_kernel<true>, grid, dim3(kGemmThreads), 0, s, g.a, g.b, g.K, g.d, g.ldd, g.accumulate);
-  else
-    hipLaunchKernelGGL(gemm_kernel<false>, grid, dim3(kGemmThreads), 0, s, g.a, g.b, g.K, g.d, g.ldd, g.accumulate);
+  hipLaunchKernelGGL((gemm_kernel<kBf16Out, kKind>), grid, dim3(kGemmThreads), 0, s, g.a, g.b, g.K, g.d, g.ldd, g.accumulate, e);
   return hipGetLastError();
 }
+static hipError_t launch_tile128(const GemmArgs& g, hipStream_t s) {
+  if (g.epilogue) return launch_tile128_as<false, kForward>(g, *g.epilogue, s);
+  return g.out_bf16 ? launch_tile128_as<true, kNoEpilogue>(g, {}, s) : launch_tile128_as<false, kNoEpilogue>(g, {}, s);
+}
 
-static hipError_t launch_fused256(const GemmArgs& g, hipStream_t s) {
-  static PerDeviceOnce once_bf16, once_f32;
-  const hipError_t e = g.out_bf16 ? ensure_dynamic_lds(reinterpret_cast<const void*>(&gemm_kernel_256<true>), 2 * kStageBytes, once_bf16)
-                                  : ensure_dynamic_lds(reinterpret_cast<const void*>(&gemm_kernel_256<false>), 2 * kStageBytes, once_f32);
+template <bool kBf16Out, int kKind>
+static hipError_t launch_fused256_as(const GemmArgs& g, const EpilogueArg<kKind>& epilogue, hipStream_t s) {
+  static PerDeviceOnce once;
+  const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&gemm_kernel_256<kBf16Out, kKind>), 2 * kStageBytes, once);
   if (e != hipSuccess) return e;
   const int tiles_m = static_cast<int>((g.a.outer + TM - 1) / TM), tiles_n = static_cast<int>((g.b.outer + TN - 1) / TN);
   const dim3 grid(static_cast<unsigned>(tiles_m * tiles_n));
-  if (g.out_bf16)
-    hipLaunchKernelGGL(gemm_kernel_256<true>, grid, dim3(kBigThreads), 2 * kStageBytes, s, g.a, g.b, g.K, g.d, g.ldd, g.accumulate, tiles_m, tiles_n);
-  else
-    hipLaunchKernelGGL(gemm_kernel_256<false>, grid, dim3(kBigThreads), 2 * kStageBytes, s, g.a, g.b, g.K, g.d, g.ldd, g.accumulate, tiles_m, tiles_n);
+  hipLaunchKernelGGL((gemm_kernel_256<kBf16Out, kKind>), grid, dim3(kBigThreads), 2 * kStageBytes, s, g.a, g.b, g.K, g.d, g.ldd, g.accumulate, tiles_m, tiles_n, epilogue);
   return hipGetLastError();
+}
+static hipError_t launch_fused256(const GemmArgs& g, hipStream_t s) {
+  if (g.epilogue) return launch_fused256_as<false, kForward>(g, *g.epilogue, s);
+  return g.out_bf16 ? launch_fused256_as<true, kNoEpilogue>(g, {}, s) : launch_fused256_as<false, kNoEpilogue>(g, {}, s);
 }
 
 // Which kernel a product takes.

@@ -99,10 +99,10 @@ struct Shape {
   static constexpr int kLdsBytes = kWaves * kWaveBytes;
 };
 
-// Tile number pid of a product of tiles_m x tiles_n of them.  bf16_out: the output type, a constant where a kernel serves one.
-template <int MB, int NB, int WK, int Steps>
+// Tile number pid of a product of tiles_m x tiles_n of them.  bf16_out: the output type, a constant where a kernel serves one (an epilogue has its own).
+template <int MB, int NB, int WK, int Steps, int kKind>
 __device__ __forceinline__ void direct_tile(const Operand& A, const Operand& B, const int K, void* __restrict__ Dv, const int64_t ldd, const bool accumulate,
-                                            const bool bf16_out, const int tiles_m, const int tiles_n, int pid) {
+                                            const bool bf16_out, const int tiles_m, const int tiles_n, int pid, const EpilogueArg<kKind>& epilogue) {
   using S = Shape<MB, NB, WK, Steps>;
   constexpr int kSteps = Steps, kWindowK = S::kWindowK, kCodeBytes = S::kCodeBytes, kScaleBytes = S::kScaleBytes;
   constexpr int kChunks = 4 * kSteps, kLoadRows = 64 / kChunks, kRowBytes = 16 * kChunks;   // of a row of a window; rows that a load instruction covers
@@ -347,10 +347,15 @@ __device__ __forceinline__ void direct_tile(const Operand& A, const Operand& B, 
   const bool vec = ts.a_per_row || ts.b_per_row;
   const float out_scale = vec ? 0.0f : A.ts[0] * B.ts[0];
   auto store = [&](float4v v, int i, int j) {
-    const uint32_t m = m0 + i * 16 + l16, n = n0 + j * 16 + q * 4;
+    int row = l16;
+    if constexpr (kKind != kNoEpilogue) asm volatile("" : "+v"(row));   // (no instruction; otherwise every row's addresses are kept)
+    const uint32_t m = m0 + i * 16 + row, n = n0 + j * 16 + q * 4;
     if (m < M && n < N) {
       v *= scale4(ts, out_scale, vec, true, m, n);
-      if (bf16_out) {
+      if constexpr (kKind != kNoEpilogue) {   // (rows and columns come in multiples of 16: all lanes are here)
+        float4v block[1] = {v};
+        finish_block<1>(block, epilogue, Dv, ldd, m, n - q * 4, q * 4, true);
+      } else if (bf16_out) {
         uint2 o;
         o.x = f32x2_to_bf16(v[0], v[1]);
         o.y = f32x2_to_bf16(v[2], v[3]);
@@ -383,10 +388,10 @@ __device__ __forceinline__ void direct_tile(const Operand& A, const Operand& B, 
   }
 }
 
-template <int MB, int NB, int WK, int Steps, bool kBf16Out>
+template <int MB, int NB, int WK, int Steps, bool kBf16Out, int kKind>
 __global__ __launch_bounds__((WK == 1 ? 4 : WK) * 64, MB * NB > 16 ? 1 : 2) void gemm_direct_kernel(
-    Operand A, Operand B, int K, void* __restrict__ Dv, int64_t ldd, bool accumulate, int tiles_m, int tiles_n) {
-  direct_tile<MB, NB, WK, Steps>(A, B, K, Dv, ldd, accumulate, kBf16Out, tiles_m, tiles_n, static_cast<int>(blockIdx.x));
+    Operand A, Operand B, int K, void* __restrict__ Dv, int64_t ldd, bool accumulate, int tiles_m, int tiles_n, EpilogueArg<kKind> epilogue) {
+  direct_tile<MB, NB, WK, Steps, kKind>(A, B, K, Dv, ldd, accumulate, kBf16Out, tiles_m, tiles_n, static_cast<int>(blockIdx.x), epilogue);
 }
 
 // Two products that do not depend on each other in one launch (a layer's Dgrad and Wgrad): the first `tiles` workgroups take the first one's tiles.  Apart, a small layer's
@@ -405,9 +410,9 @@ __global__ __launch_bounds__(256, 2) void gemm_direct_pair_kernel(DirectProduct 
   const int tiles = first.tiles_m * first.tiles_n, id = static_cast<int>(blockIdx.x);
   const DirectProduct& p = id < tiles ? first : second;
   const int pid = id < tiles ? id : id - tiles;
-  if (p.shape == 0) direct_tile<4, 4, 4, 1>(p.a, p.b, p.K, p.d, p.ldd, p.accumulate, p.bf16_out, p.tiles_m, p.tiles_n, pid);
-  else if (p.shape == 1) direct_tile<4, 3, 4, 1>(p.a, p.b, p.K, p.d, p.ldd, p.accumulate, p.bf16_out, p.tiles_m, p.tiles_n, pid);
-  else direct_tile<4, 4, 1, 1>(p.a, p.b, p.K, p.d, p.ldd, p.accumulate, p.bf16_out, p.tiles_m, p.tiles_n, pid);
+  if (p.shape == 0) direct_tile<4, 4, 4, 1, kNoEpilogue>(p.a, p.b, p.K, p.d, p.ldd, p.accumulate, p.bf16_out, p.tiles_m, p.tiles_n, pid, {});
+  else if (p.shape == 1) direct_tile<4, 3, 4, 1, kNoEpilogue>(p.a, p.b, p.K, p.d, p.ldd, p.accumulate, p.bf16_out, p.tiles_m, p.tiles_n, pid, {});
+  else direct_tile<4, 4, 1, 1, kNoEpilogue>(p.a, p.b, p.K, p.d, p.ldd, p.accumulate, p.bf16_out, p.tiles_m, p.tiles_n, pid, {});
 }
 
 }  // namespace
@@ -507,24 +512,24 @@ bool direct_shape(int shape, int* out) {
   return true;
 }
 
-template <int I, bool kBf16Out>
-static hipError_t launch_shape(const GemmArgs& g, hipStream_t s) {
+template <int I, bool kBf16Out, int kKind>
+static hipError_t launch_shape(const GemmArgs& g, const EpilogueArg<kKind>& epilogue, hipStream_t s) {
   constexpr DirectShape d = kDirectShapes[I];
   using S = Shape<d.mb, d.nb, d.wk, d.steps>;
-  constexpr auto kernel = &gemm_direct_kernel<d.mb, d.nb, d.wk, d.steps, kBf16Out>;
+  constexpr auto kernel = &gemm_direct_kernel<d.mb, d.nb, d.wk, d.steps, kBf16Out, kKind>;
   static PerDeviceOnce once;
   const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), S::kLdsBytes, once);
   if (e != hipSuccess) return e;
   const int tiles_m = static_cast<int>((g.a.outer + S::kTM - 1) / S::kTM), tiles_n = static_cast<int>((g.b.outer + S::kTN - 1) / S::kTN);
   hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tiles_m * tiles_n)), dim3(S::kThreads), S::kLdsBytes, s, g.a, g.b, static_cast<int>(g.K), g.d,
-                     g.ldd, g.accumulate, tiles_m, tiles_n);
+                     g.ldd, g.accumulate, tiles_m, tiles_n, epilogue);
   return hipGetLastError();
 }
 
-template <bool kBf16Out, int... I>
-static hipError_t launch_direct(const GemmArgs& g, int shape, hipStream_t s, std::integer_sequence<int, I...>) {
+template <bool kBf16Out, int kKind, int... I>
+static hipError_t launch_direct(const GemmArgs& g, const EpilogueArg<kKind>& epilogue, int shape, hipStream_t s, std::integer_sequence<int, I...>) {
   hipError_t e = hipErrorInvalidValue;
-  ((shape == I ? void(e = launch_shape<I, kBf16Out>(g, s)) : void()), ...);
+  ((shape == I ? void(e = launch_shape<I, kBf16Out, kKind>(g, epilogue, s)) : void()), ...);
   return e;
 }
 
@@ -582,7 +587,8 @@ hipError_t launch_gemm_direct_pair(const GemmArgs& g, int shape, const GemmArgs&
 
 hipError_t launch_gemm_direct(const GemmArgs& g, int shape, hipStream_t s) {
   if (!direct_shape_fits(g, shape)) return hipErrorInvalidValue;
-  return g.out_bf16 ? launch_direct<true>(g, shape, s, AllShapes{}) : launch_direct<false>(g, shape, s, AllShapes{});
+  if (g.epilogue) return launch_direct<false, kForward>(g, *g.epilogue, shape, s, AllShapes{});
+  return g.out_bf16 ? launch_direct<true, kNoEpilogue>(g, {}, shape, s, AllShapes{}) : launch_direct<false, kNoEpilogue>(g, {}, shape, s, AllShapes{});
 }
 
 }  // namespace nvfp4

@@ -5,7 +5,11 @@
 // Device code only.
 #pragma once
 
+#include <type_traits>
+
+#include "checkpoint8.h"
 #include "nvfp4_device.h"
+#include "nvfp4_internal.h"
 
 namespace nvfp4 {
 
@@ -166,6 +170,281 @@ template <bool kBf16Out, int kNB = 8>
 __device__ __forceinline__ void store_wave_block(float4v (&acc)[8][kNB], const TensorScales ts, void* __restrict__ Dv, int64_t ldd,
                                                  bool accumulate, int64_t row0, int64_t col0, int rows, int cols, int lane) {
   store_wave_block_impl<kBf16Out, false, 8, kNB>(acc, ts, Dv, ldd, accumulate, row0, col0, rows, cols, lane);
+}
+
+
+// ---------------------------------------------------------------- what nvfp4_gemm_epilogue does to the scaled sums
+//   z = sum + bias;  8 bits of z are kept;  D = act(z) + residual             (kForward; kResidual: with a residual)
+//   D = sum * act'(z), z from its 8 bits                                       (kGrad)
+// All of it in FP32 in registers, D rounded once.  The kinds are instances of their own because two of them load as much as they store; bias, activation,
+// what is kept and the types are decided at run time, alike for the whole launch.
+enum EpilogueKind { kNoEpilogue = 0, kForward = 1, kResidual = 2, kGrad = 3 };
+template <int kKind>
+struct EpilogueArg : GemmEpilogue {
+  __host__ __device__ EpilogueArg(const GemmEpilogue& e) : GemmEpilogue(e) {}
+};
+template <>
+struct EpilogueArg<kNoEpilogue> {};
+inline EpilogueKind epilogue_kind(const GemmEpilogue* e) { return !e ? kNoEpilogue : e->grad_codes ? kGrad : e->residual ? kResidual : kForward; }
+
+// Lanes 16 apart hold the rows of a 4 x 4 matrix of words, each lane a row: lane group q gets column q (its own inverse).
+__device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
+  const auto a = __builtin_amdgcn_permlane16_swap(w[0], w[1], false, false), b = __builtin_amdgcn_permlane16_swap(w[2], w[3], false, false);
+  const auto c = __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false), d = __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false);
+  w[0] = c[0], w[1] = d[0], w[2] = c[1], w[3] = d[1];
+}
+// The words of the four lane groups, in every lane.
+__device__ __forceinline__ void gather4(uint32_t v, uint32_t (&w)[4]) {
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  const auto c = __builtin_amdgcn_permlane32_swap(a[0], a[0], false, false), d = __builtin_amdgcn_permlane32_swap(a[1], a[1], false, false);
+  w[0] = c[0], w[1] = d[0], w[2] = c[1], w[3] = d[1];
+}
+// Largest of the lane groups' values (16x16 results), or of the two halves' (32x32 results), in all of them.
+__device__ __forceinline__ uint32_t max_over_halves(uint32_t v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max(a[0], a[1]);
+}
+__device__ __forceinline__ uint32_t max_over_groups(uint32_t v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return max_over_halves(max(a[0], a[1]));
+}
+
+__device__ __forceinline__ float4v load4(const void* base, bool bf16, int64_t at) {
+  if (!bf16) return *reinterpret_cast<const float4v*>(static_cast<const float*>(base) + at);
+  const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + at);
+  return float4v{bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
+}
+
+// One 16-column block, for the kernels that store block by block: the lane holds kGroups groups of four columns of row m, n0 + first + 8 g .. + 3 (one
+// group for 16x16 results, first = 4 (lane >> 4); two for 32x32, first = 4 (lane >> 5)).  The lanes that share a row's block come together; `in`: the row
+// exists.  Stores D too.
+template <int kGroups>
+__device__ __forceinline__ void finish_block(float4v (&v)[kGroups], const GemmEpilogue& e, void* __restrict__ Dv, int64_t ldd, int64_t m, int64_t n0, int first, bool in) {
+  float z[kGroups * 4];
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) {
+    float4v b = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (e.bias) b = *reinterpret_cast<const float4v*>(e.bias + n0 + first + 8 * g);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) z[4 * g + r] = v[g][r] + b[r];
+  }
+  const int64_t at = m * e.cols + n0;
+  if (e.grad_codes) {
+    float slope[kGroups * 4];
+    const uint32_t byte = in ? e.grad_scales[at / 16] : 0u;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const uint32_t codes = in ? *reinterpret_cast<const uint32_t*>(e.grad_codes + at + first + 8 * g) : 0u;
+      checkpoint_values4(codes, byte, slope + 4 * g);
+    }
+    activation_slope(slope, e.act);
+#pragma unroll
+    for (int i = 0; i < kGroups * 4; ++i) z[i] *= slope[i];
+  } else {
+    if (e.keep_codes) {
+      const uint32_t byte = checkpoint_scale(kGroups == 1 ? max_over_groups(max_magnitude(z)) : max_over_halves(max_magnitude(z)));
+      if (in) {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g)
+          *reinterpret_cast<uint32_t*>(e.keep_codes + at + first + 8 * g) = checkpoint_codes4(z[4 * g], z[4 * g + 1], z[4 * g + 2], z[4 * g + 3], byte);
+        if (first == 0) e.keep_scales[at / 16] = static_cast<uint8_t>(byte);
+      }
+    }
+    activate(z, e.act);
+  }
+  if (!in) return;
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) {
+    const int64_t n = n0 + first + 8 * g;
+    float4v d = {z[4 * g], z[4 * g + 1], z[4 * g + 2], z[4 * g + 3]};
+    if (e.residual) d += load4(e.residual, e.residual_bf16, m * e.ldr + n);
+    if (e.out_bf16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(Dv) + m * ldd + n) = make_uint2(f32x2_to_bf16(d[0], d[1]), f32x2_to_bf16(d[2], d[3]));
+    else *reinterpret_cast<float4v*>(static_cast<float*>(Dv) + m * ldd + n) = d;
+  }
+}
+
+// A wavefront's whole block of kMB x kNB 16x16 results, 16 rows of four blocks (64 columns) at a time, column group by column group.  What such a unit
+// loads (residual, or 8 bits) is asked for kAhead units before it is needed; addresses past the end are replaced by the last in range rather than
+// skipped, so that the number of loads in flight is known to the compiler.  The 8 bits move as 16 bytes of one block to a lane, D as in WaveBlockStore.
+// first_unit, units: a part of the block (see splitk_sum_kernel).
+template <int kKind, int kMB, int kNB>
+struct EpilogueBlock {
+  static constexpr int kGroups = (kNB + 3) / 4, kUnits = kGroups * kMB, kAhead = kKind == kResidual ? 3 : 4;
+  struct Loads {
+    float4v f[kKind == kResidual ? 4 : 1];   // residual, as loaded (bf16: in the first two words)
+    uint4 codes;
+    uint32_t byte;
+  };
+  const GemmEpilogue& e;
+  const TensorScales& ts;
+  void* d;
+  int64_t ldd, row0, col0;
+  int rows, cols, l16, lq;
+
+  __device__ __forceinline__ EpilogueBlock(const GemmEpilogue& e_, const TensorScales& ts_, void* Dv, int64_t ldd_, int64_t row0_, int64_t col0_, int rows_, int cols_, int lane)
+      : e(e_), ts(ts_), d(Dv), ldd(ldd_), row0(row0_), col0(col0_), rows(rows_), cols(cols_), l16(lane & 15), lq(lane >> 4) {}
+
+  // The lane's row in 16-row block i, counted from the first.  Opaque (no instruction): the compiler would keep every block's addresses from one column
+  // group to the next, in more registers than there are.
+  __device__ __forceinline__ int row_of(int i) const {
+    int r = i * 16 + l16;
+    asm volatile("" : "+v"(r));
+    return r;
+  }
+  __device__ __forceinline__ int64_t row_at(int i) const { return row0 + min(row_of(i), rows - 1); }
+  __device__ __forceinline__ int64_t col_at(int j) const { return col0 + min(16 * j, cols - 16); }   // first column of block j
+
+  __device__ __forceinline__ void fetch(Loads& l, int i, int jg) const {
+    const int64_t row = row_at(i);
+    if constexpr (kKind == kResidual) {
+      if (e.residual_bf16) {
+        const uint16_t* p = static_cast<const uint16_t*>(e.residual) + row * e.ldr + 4 * lq;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (4 * jg + k < kNB) {
+            const uint2 w = *reinterpret_cast<const uint2*>(p + col_at(4 * jg + k));
+            l.f[k][0] = __uint_as_float(w.x), l.f[k][1] = __uint_as_float(w.y);
+          }
+        }
+      } else {
+        const float* p = static_cast<const float*>(e.residual) + row * e.ldr + 4 * lq;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (4 * jg + k < kNB) l.f[k] = *reinterpret_cast<const float4v*>(p + col_at(4 * jg + k));
+      }
+    }
+    if constexpr (kKind == kGrad) {
+      const int64_t at = row * e.cols + col_at(min(4 * jg + lq, kNB - 1));
+      l.codes = *reinterpret_cast<const uint4*>(e.grad_codes + at);
+      l.byte = e.grad_scales[at / 16];
+    }
+  }
+
+  // Factors and bias of the lane's columns in a group of four blocks.
+  __device__ __forceinline__ void columns(int jg, float4v (&sb)[4], float4v (&bias)[4]) const {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (4 * jg + k >= kNB) continue;
+      const int64_t n = col_at(4 * jg + k) + 4 * lq;
+      if (ts.b_per_row) {
+        sb[k] = *reinterpret_cast<const float4v*>(ts.b + n);
+      } else {
+        const float b0 = ts.b[0];
+        sb[k] = float4v{b0, b0, b0, b0};
+      }
+      bias[k] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+      if (kKind != kGrad && e.bias) bias[k] = *reinterpret_cast<const float4v*>(e.bias + n);
+    }
+  }
+
+  // sums: the unit's four blocks, unscaled.
+  __device__ __forceinline__ void finish(const float4v (&sums)[4], const Loads& l, int i, int jg, float sa, const float4v (&sb)[4], const float4v (&bias)[4]) const {
+    constexpr int kLast = kNB % 4 ? kNB % 4 : 4;
+    const int blocks = jg == kGroups - 1 ? kLast : 4;   // (a constant where it is unrolled)
+    const int r_in = row_of(i);
+    const bool row_in = r_in < rows;
+    const int64_t row = row0 + r_in;
+    float z[16];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) z[4 * k + r] = k < blocks ? sums[k][r] * (sb[k][r] * sa) + bias[k][r] : 0.0f;
+    if constexpr (kKind == kGrad) {
+      uint32_t codes[4] = {l.codes.x, l.codes.y, l.codes.z, l.codes.w}, bytes[4];
+      transpose4(codes);
+      gather4(l.byte, bytes);
+      float slope[16];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) checkpoint_values4(codes[k], bytes[k], slope + 4 * k);
+      activation_slope(slope, e.act);
+#pragma unroll
+      for (int t = 0; t < 16; ++t) z[t] *= slope[t];
+    } else {
+      if (e.keep_codes) {
+        uint32_t m[4], w[4], bytes[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) m[k] = max(max(magnitude(z[4 * k]), magnitude(z[4 * k + 1])), max(magnitude(z[4 * k + 2]), magnitude(z[4 * k + 3])));
+        transpose4(m);
+        const uint32_t byte = checkpoint_scale(max(max(m[0], m[1]), max(m[2], m[3])));   // of block 4 jg + lq
+        gather4(byte, bytes);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = checkpoint_codes4(z[4 * k], z[4 * k + 1], z[4 * k + 2], z[4 * k + 3], bytes[k]);
+        transpose4(w);
+        const int c = 16 * (4 * jg + lq);
+        if (row_in && lq < blocks && c < cols) {
+          const int64_t at = row * e.cols + col0 + c;
+          *reinterpret_cast<u32x4v*>(e.keep_codes + at) = u32x4v{w[0], w[1], w[2], w[3]};
+          e.keep_scales[at / 16] = static_cast<uint8_t>(byte);
+        }
+      }
+      activate(z, e.act);
+      if constexpr (kKind == kResidual) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float4v f = l.f[k];
+          const uint32_t w0 = __float_as_uint(f[0]), w1 = __float_as_uint(f[1]);
+          if (k < blocks) {
+            z[4 * k] += e.residual_bf16 ? bf16_lo(w0) : f[0];
+            z[4 * k + 1] += e.residual_bf16 ? bf16_hi(w0) : f[1];
+            z[4 * k + 2] += e.residual_bf16 ? bf16_lo(w1) : f[2];
+            z[4 * k + 3] += e.residual_bf16 ? bf16_hi(w1) : f[3];
+          }
+        }
+      }
+    }
+    if (e.out_bf16) {
+      const int nl = (lq & 1) * 16 + (lq >> 1) * 8;   // (see WaveBlockStore)
+      uint16_t* to = static_cast<uint16_t*>(d) + row * ldd + col0 + nl;
+#pragma unroll
+      for (int k = 0; k < 4; k += 2) {
+        if (k >= blocks) continue;
+        const auto s0 = __builtin_amdgcn_permlane16_swap(f32x2_to_bf16(z[4 * k], z[4 * k + 1]), f32x2_to_bf16(z[4 * k + 4], z[4 * k + 5]), false, false);
+        const auto s1 = __builtin_amdgcn_permlane16_swap(f32x2_to_bf16(z[4 * k + 2], z[4 * k + 3]), f32x2_to_bf16(z[4 * k + 6], z[4 * k + 7]), false, false);
+        const int c = 16 * (4 * jg + k);
+        if (row_in && c + nl < cols && (k + 1 < blocks || nl < 16)) *reinterpret_cast<u32x4v*>(to + c) = u32x4v{s0[0], s1[0], s0[1], s1[1]};
+      }
+    } else {
+      float* to = static_cast<float*>(d) + row * ldd + col0 + 4 * lq;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int c = 16 * (4 * jg + k);
+        if (k < blocks && row_in && c < cols) *reinterpret_cast<float4v*>(to + c) = float4v{z[4 * k], z[4 * k + 1], z[4 * k + 2], z[4 * k + 3]};
+      }
+    }
+  }
+};
+
+template <int kBegin, int kEnd, class F>
+__device__ __forceinline__ void each(F&& f) {
+  if constexpr (kBegin < kEnd) {
+    f(std::integral_constant<int, kBegin>{});
+    each<kBegin + 1, kEnd>(f);
+  }
+}
+
+template <int kKind, int kMB, int kNB>
+__device__ __forceinline__ void store_wave_block_epilogue(float4v (&acc)[kMB][kNB], const TensorScales ts, const GemmEpilogue& e, void* __restrict__ Dv, int64_t ldd,
+                                                          int64_t row0, int64_t col0, int rows, int cols, int lane) {
+  using Block = EpilogueBlock<kKind, kMB, kNB>;
+  const Block b(e, ts, Dv, ldd, row0, col0, rows, cols, lane);
+  constexpr int kAhead = Block::kAhead, kUnits = Block::kUnits;
+  constexpr bool kLoads = kKind == kResidual || kKind == kGrad;
+  typename Block::Loads ring[kLoads ? kAhead : 1];
+  if constexpr (kLoads) each<0, (kAhead < kUnits ? kAhead : kUnits)>([&](auto u) { b.fetch(ring[decltype(u)::value], decltype(u)::value % kMB, decltype(u)::value / kMB); });
+  float sa[kMB];
+#pragma unroll
+  for (int i = 0; i < kMB; ++i) sa[i] = ts.a[ts.a_per_row ? b.row_at(i) : 0];
+  float4v sb[4], bias[4];
+  each<0, kUnits>([&](auto uc) {
+    constexpr int u = decltype(uc)::value, i = u % kMB, jg = u / kMB;
+    if constexpr (i == 0) b.columns(jg, sb, bias);
+    float4v sums[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sums[k] = 4 * jg + k < kNB ? acc[i][4 * jg + k < kNB ? 4 * jg + k : 0] : float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    b.finish(sums, ring[kLoads ? u % kAhead : 0], i, jg, sa[i], sb, bias);
+    if constexpr (kLoads && u + kAhead < kUnits) b.fetch(ring[u % kAhead], (u + kAhead) % kMB, (u + kAhead) / kMB);
+    __builtin_amdgcn_sched_barrier(0);
+  });
 }
 
 }  // namespace nvfp4

@@ -229,13 +229,14 @@ struct Schedule {
 // kRowScales: an operand carries a tensor-level scale per row (uniform over a launch, and a different output stage).
 // kSplit: k_splits > 1; the output stage is the store of the partial tile (kBf16Out and kRowScales are false then).
 // kMB, kNB: 16-row and 16-column blocks per wavefront; which tile a product takes: pick_tile.
-template <bool kBf16Out, bool kRowScales, bool kSplit, int kMB, int kNB>
+// kKind: the kind of epilogue; with one, kBf16Out and kRowScales are false and both are decided at run time.
+template <bool kBf16Out, bool kRowScales, bool kSplit, int kMB, int kNB, int kKind = kNoEpilogue>
 __global__ __launch_bounds__(kThreads) void gemm_f16_kernel(const _Float16* __restrict__ A, const _Float16* __restrict__ B,
                                                             int64_t M, int64_t N, int64_t K, const float* __restrict__ a_ts,
                                                             const float* __restrict__ b_ts, void* __restrict__ Dv,
                                                             int64_t ldd, bool accumulate, int tiles_m, int tiles_n,
                                                             int tile_begin, int tile_count, int k_splits, float* partials,
-                                                            bool a_ts_per_row, bool b_ts_per_row) {
+                                                            bool a_ts_per_row, bool b_ts_per_row, EpilogueArg<kKind> epilogue) {
   using S = Schedule<kMB, kNB>;
   constexpr int kTM = 32 * kMB, kTN = 32 * kNB, kStageBytes = stage_bytes(kMB, kNB);
   constexpr int kR = S::kR, kHalf = S::kHalf, kALoads = S::kALoads, kBLoads = S::kBLoads, kLoads = S::kLoads, kEarly = S::kEarly;
@@ -368,7 +369,7 @@ __global__ __launch_bounds__(kThreads) void gemm_f16_kernel(const _Float16* __re
       // Memory operations complete in issue order.  Behind the loads of stage g + 1 this wavefront has issued those of
       // g + 2 and g + 3, kLoads each, and, across a tile boundary, the stores of the tile before.
       // (The reads are waited for on every path, whatever is known of the stores.)
-      constexpr int kBehind = 2 * kLoads + (kRelaxed ? kTileStores<kBf16Out, kMB, kNB> : 0);
+      constexpr int kBehind = 2 * kLoads + (kRelaxed ? kTileStores<kBf16Out || kKind != kNoEpilogue, kMB, kNB> : 0);   // (with an epilogue at least as many)
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kBehind > 63 ? 63 : kBehind) : "memory");
       if (kRelaxed && !stores_behind) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
       __builtin_amdgcn_s_barrier();
@@ -440,6 +441,9 @@ __global__ __launch_bounds__(kThreads) void gemm_f16_kernel(const _Float16* __re
 #pragma unroll
         for (int j = 0; j < kNB; ++j) mine[(i * kNB + j) * kThreads] = acc[i][j];
       return;
+    } else if constexpr (kKind != kNoEpilogue) {
+      store_wave_block_epilogue<kKind, kMB, kNB>(acc, out_scale, epilogue, Dv, ldd, m0 + wm * (16 * kMB), n0 + wn * (16 * kNB), Mt - wm * (16 * kMB),
+                                                 Nt - wn * (16 * kNB), lane);
     } else {
       store_wave_block_impl<kBf16Out, kRowScales, kMB, kNB>(acc, out_scale, Dv, ldd, accumulate, m0 + wm * (16 * kMB), n0 + wn * (16 * kNB),
                                                             Mt - wm * (16 * kMB), Nt - wn * (16 * kNB), lane);
@@ -459,11 +463,11 @@ __global__ __launch_bounds__(kThreads) void gemm_f16_kernel(const _Float16* __re
 // in) and 16 rows of that, sum = ((p0 + p1) + p2) + ... in split order, then the same output stage.  Many small
 // workgroups: the partial tiles were written by other XCDs and every load of them is a long trip, so what counts is
 // how many are in flight over the chip (with a wavefront per 128 x 128 block the sum of 64 tiles x 4 splits took 57 us).
-template <bool kBf16Out, bool kRowScales>
+template <bool kBf16Out, bool kRowScales, int kKind = kNoEpilogue>
 __global__ __launch_bounds__(64) void splitk_sum_kernel(const float* __restrict__ partials, int k_splits, int64_t M, int64_t N,
                                                         const float* __restrict__ a_ts, const float* __restrict__ b_ts,
                                                         void* __restrict__ Dv, int64_t ldd, bool accumulate, int tiles_m,
-                                                        int tiles_n, int tile_begin, bool a_ts_per_row, bool b_ts_per_row) {
+                                                        int tiles_n, int tile_begin, bool a_ts_per_row, bool b_ts_per_row, EpilogueArg<kKind> epilogue) {
   const int tile_local = static_cast<int>(blockIdx.x) >> 5, wave = (static_cast<int>(blockIdx.x) >> 3) & 3;
   const int i = static_cast<int>(blockIdx.x) & 7;
   const int lane = static_cast<int>(threadIdx.x), wm = wave >> 1, wn = wave & 1;
@@ -487,6 +491,17 @@ __global__ __launch_bounds__(64) void splitk_sum_kernel(const float* __restrict_
   const int64_t m0 = static_cast<int64_t>(tm) * TM, n0 = static_cast<int64_t>(tn) * TN;
   const int Mt = static_cast<int>(M - m0 < TM ? M - m0 : TM);
   const int Nt = static_cast<int>(N - n0 < TN ? N - n0 : TN);
+  if constexpr (kKind != kNoEpilogue) {
+    // the rows as a block of 16 of their own
+    const int64_t row0 = m0 + wm * 128 + i * 16, col0 = n0 + wn * 128;
+    const int rows = Mt - wm * 128 - i * 16, cols = Nt - wn * 128;
+    if (rows <= 0 || cols <= 0) return;
+    float4v block[1][8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) block[0][j] = sums[j];
+    store_wave_block_epilogue<kKind, 1, 8>(block, ts, epilogue, Dv, ldd, row0, col0, rows, cols, lane);
+    return;
+  }
   const WaveBlockStore<kBf16Out, kRowScales> out(ts, Dv, ldd, accumulate, m0 + wm * 128, n0 + wn * 128, Mt - wm * 128,
                                                  Nt - wn * 128, lane);
   out.store_rows(sums, i, kRowScales ? out.row_scale(ts, m0 + wm * 128, i) : 0.0f);
@@ -560,7 +575,7 @@ static double rounds_of(int64_t tiles) { return static_cast<double>((tiles + kCU
 // 8192 x 20480 x 5120 bf16 1131 / 1112 / 1137, 8192 x 5120 x 20480 1200 / 1152 / 1251, 5120 x 20480 x 8192 FP32 1243 / 1201 / 1127, 5120 x 5120 x 4096 FP32 188 / 217 / 154,
 // 4096 x 15360 x 2048 bf16 192 / 178 / 207.  Over the 130 products the tile with the smallest estimate takes 0.1 % more than the best one.
 // A larger tile has no round split, and tiles without a split sum in the same order.
-// (320 x 320 with a scale per row: the output stage has too few registers for the scales.)
+// (320 x 320 with a scale per row, or with an epilogue: the output stage has too few registers.)
 // Where the contraction is short the result is most of the work, which the estimate knows least about: there a larger tile has to promise more, most of all where the
 // result is accumulated (read too).  Measured, time in the tile of 256 rows over that in the larger one, geometric mean and least, by what the estimate promises: accumulated,
 // K < 1024, 256 x 320 under 0.9 1.06, 0.98, from 0.9 on 0.98, 0.88; 320 x 320 under 0.8 1.04, 0.95, from 0.8 on 0.96, 0.84; plain results, K < 400, from 0.95 on
@@ -576,7 +591,7 @@ struct Tile {
   int mb, nb;
   double gain;   // time in it over that in the tile of 256 rows
 };
-static Tile pick_tile(int64_t M, int64_t N, int64_t K, const Width& w, const TailPlan& tail, bool row_scales, bool accumulate) {
+static Tile pick_tile(int64_t M, int64_t N, int64_t K, const Width& w, const TailPlan& tail, bool no_320_rows, bool accumulate) {
   Tile best{8, w.nb, 1.0};
   double base = 0.0;   // (the tile of 256 rows comes first)
   for (const TileTime& t : kTileTimes) {
@@ -585,7 +600,7 @@ static Tile pick_tile(int64_t M, int64_t N, int64_t K, const Width& w, const Tai
     if (t.nb <= 8) {
       if (t.nb != w.nb) continue;
       if (w.nb == 8 && tail.tail) rounds = static_cast<double>((tiles - tail.tail) / kCUs) + 1.0 / tail.splits + 0.3;   // (the partial tiles)
-    } else if (row_scales && t.mb == 10) {
+    } else if (no_320_rows && t.mb == 10) {
       continue;
     }
     const double us = tile_us(t, tiles, rounds, K);
@@ -610,26 +625,26 @@ struct TileChoice {
   TailPlan tail;
   double rounds_us;
 };
-static TileChoice choose_tile(int64_t M, int64_t N, int64_t K, bool row_scales, bool accumulate, const TailPlan& tail) {
+static TileChoice choose_tile(int64_t M, int64_t N, int64_t K, bool no_320_rows, bool accumulate, const TailPlan& tail) {
   Width w = pick_width(M, N, tail, false);
-  Tile t = pick_tile(M, N, K, w, tail, row_scales, false);
+  Tile t = pick_tile(M, N, K, w, tail, no_320_rows, false);
   const double us = w.rounds * (9.2 + static_cast<double>(K) * (w.tiles >= kCUs ? 0.0186 : 0.0159)) * (K > 1536 && K <= 4096 ? t.gain : 1.0);
   if (accumulate && K < 1024) {
     w = pick_width(M, N, tail, true);
-    t = pick_tile(M, N, K, w, tail, row_scales, true);
+    t = pick_tile(M, N, K, w, tail, no_320_rows, true);
   }
   return TileChoice{t.mb, t.nb, t.nb == 8 ? tail : TailPlan{0, 1}, us};
 }
 // The split is chosen if the workspace has the room for its partial tiles; otherwise the last round is an ordinary one.
-static TileChoice choose_tile(int64_t M, int64_t N, int64_t K, bool row_scales, bool accumulate, size_t room_for_partials) {
-  const TileChoice c = choose_tile(M, N, K, row_scales, accumulate, plan_tail(M, N, K));
-  return partial_bytes(c.tail) <= room_for_partials ? c : choose_tile(M, N, K, row_scales, accumulate, TailPlan{0, 1});
+static TileChoice choose_tile(int64_t M, int64_t N, int64_t K, bool no_320_rows, bool accumulate, size_t room_for_partials) {
+  const TileChoice c = choose_tile(M, N, K, no_320_rows, accumulate, plan_tail(M, N, K));
+  return partial_bytes(c.tail) <= room_for_partials ? c : choose_tile(M, N, K, no_320_rows, accumulate, TailPlan{0, 1});
 }
 
 // Enough for every way in which the operands may come; a call may use less (plan_two_pass).
 size_t gemm_workspace_bytes(int64_t M, int64_t N, int64_t K) {
   size_t partials = 0;
-  for (const bool row_scales : {false, true}) partials = std::max(partials, partial_bytes(choose_tile(M, N, K, row_scales, false, SIZE_MAX).tail));
+  for (const bool no_320_rows : {false, true}) partials = std::max(partials, partial_bytes(choose_tile(M, N, K, no_320_rows, false, SIZE_MAX).tail));
   return operand_bytes(M, N, K) + partials;
 }
 
@@ -648,7 +663,7 @@ TwoPassPlan plan_two_pass(const GemmArgs& g) {
   const int64_t rows = (g.a.fp16 ? 0 : M) + (g.b.fp16 ? 0 : N);
   const size_t operands = operand_bytes(rows, 0, g.K);
   if (operands > g.workspace_bytes) return plan;
-  const TileChoice c = choose_tile(M, N, g.K, g.a.ts_per_row != 0 || g.b.ts_per_row != 0, g.accumulate, g.workspace_bytes - operands);
+  const TileChoice c = choose_tile(M, N, g.K, g.a.ts_per_row != 0 || g.b.ts_per_row != 0 || g.epilogue, g.accumulate, g.workspace_bytes - operands);
   plan.us = 7.4 + static_cast<double>(rows) * static_cast<double>(g.K) * 2.5625 / 5.0e6 + c.rounds_us;
   plan.mb = c.mb;
   plan.nb = c.nb;
@@ -662,15 +677,15 @@ TwoPassPlan plan_two_pass(const GemmArgs& g) {
   return plan;
 }
 
-#define NVFP4_LAUNCH_F16(BF16, ROWSCALES, SPLIT, MB, NB)                                                              \
+#define NVFP4_LAUNCH_F16(BF16, ROWSCALES, SPLIT, MB, NB, KIND, ...)                                                   \
   do {                                                                                                            \
     static PerDeviceOnce once;                                                                                    \
     constexpr int lds_bytes = kStages * stage_bytes(MB, NB);                                                      \
-    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&gemm_f16_kernel<BF16, ROWSCALES, SPLIT, MB, NB>), lds_bytes, once); \
+    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&gemm_f16_kernel<BF16, ROWSCALES, SPLIT, MB, NB, KIND>), lds_bytes, once); \
     if (e != hipSuccess) return e;                                                                                \
-    hipLaunchKernelGGL((gemm_f16_kernel<BF16, ROWSCALES, SPLIT, MB, NB>), dim3(wgs), dim3(kThreads), lds_bytes, s, a16, b16, \
+    hipLaunchKernelGGL((gemm_f16_kernel<BF16, ROWSCALES, SPLIT, MB, NB, KIND>), dim3(wgs), dim3(kThreads), lds_bytes, s, a16, b16, \
                        g.a.outer, g.b.outer, g.K, g.a.ts, g.b.ts, g.d, g.ldd, g.accumulate, tiles_m, tiles_n,     \
-                       tile_begin, tile_count, k_splits, partials, g.a.ts_per_row != 0, g.b.ts_per_row != 0);      \
+                       tile_begin, tile_count, k_splits, partials, g.a.ts_per_row != 0, g.b.ts_per_row != 0, EpilogueArg<KIND>{__VA_ARGS__}); \
   } while (0)
 
 // Tiles [tile_begin, tile_begin + tile_count); k_splits > 1: each shared by that many workgroups, summed by a second launch.
@@ -681,27 +696,42 @@ static hipError_t launch_f16(bool bf16_out, const _Float16* a16, const _Float16*
   unsigned wgs = static_cast<unsigned>(tile_count) * static_cast<unsigned>(k_splits);
   if (k_splits == 1 && g.K / TK >= 2 && wgs > static_cast<unsigned>(kCUs)) wgs = kCUs;
   const bool row_scales = g.a.ts_per_row != 0 || g.b.ts_per_row != 0;
+  const EpilogueKind kind = epilogue_kind(g.epilogue);
   if (k_splits > 1) {
-    NVFP4_LAUNCH_F16(false, false, true, 8, 8);
+    NVFP4_LAUNCH_F16(false, false, true, 8, 8, kNoEpilogue);
     const dim3 grid(static_cast<unsigned>(tile_count) * 32);   // tile, 128 x 128 block, 16 rows
-#define NVFP4_LAUNCH_SUM(BF16, ROWSCALES)                                                                              \
-  hipLaunchKernelGGL((splitk_sum_kernel<BF16, ROWSCALES>), grid, dim3(64), 0, s, partials, k_splits, g.a.outer, g.b.outer, \
+#define NVFP4_LAUNCH_SUM(BF16, ROWSCALES, KIND, ...)                                                                   \
+  hipLaunchKernelGGL((splitk_sum_kernel<BF16, ROWSCALES, KIND>), grid, dim3(64), 0, s, partials, k_splits, g.a.outer, g.b.outer, \
                      g.a.ts, g.b.ts, g.d, g.ldd, g.accumulate, tiles_m, tiles_n, tile_begin, g.a.ts_per_row != 0,      \
-                     g.b.ts_per_row != 0)
-    if (bf16_out) {
-      if (row_scales) NVFP4_LAUNCH_SUM(true, true); else NVFP4_LAUNCH_SUM(true, false);
+                     g.b.ts_per_row != 0, EpilogueArg<KIND>{__VA_ARGS__})
+    if (kind == kForward) {
+      NVFP4_LAUNCH_SUM(false, false, kForward, *g.epilogue);
+    } else if (kind == kResidual) {
+      NVFP4_LAUNCH_SUM(false, false, kResidual, *g.epilogue);
+    } else if (kind == kGrad) {
+      NVFP4_LAUNCH_SUM(false, false, kGrad, *g.epilogue);
+    } else if (bf16_out) {
+      if (row_scales) NVFP4_LAUNCH_SUM(true, true, kNoEpilogue); else NVFP4_LAUNCH_SUM(true, false, kNoEpilogue);
     } else {
-      if (row_scales) NVFP4_LAUNCH_SUM(false, true); else NVFP4_LAUNCH_SUM(false, false);
+      if (row_scales) NVFP4_LAUNCH_SUM(false, true, kNoEpilogue); else NVFP4_LAUNCH_SUM(false, false, kNoEpilogue);
     }
 #undef NVFP4_LAUNCH_SUM
+  } else if (kind != kNoEpilogue) {
+    if constexpr (kMB == 8) {
+      if (kind == kForward) NVFP4_LAUNCH_F16(false, false, false, kMB, kNB, kForward, *g.epilogue);
+      else if (kind == kResidual) NVFP4_LAUNCH_F16(false, false, false, kMB, kNB, kResidual, *g.epilogue);
+      else NVFP4_LAUNCH_F16(false, false, false, kMB, kNB, kGrad, *g.epilogue);
+    } else {
+      return hipErrorInvalidValue;   // (pick_tile offers none)
+    }
   } else if (row_scales) {
     if constexpr (kMB == 8) {
-      if (bf16_out) NVFP4_LAUNCH_F16(true, true, false, kMB, kNB); else NVFP4_LAUNCH_F16(false, true, false, kMB, kNB);
+      if (bf16_out) NVFP4_LAUNCH_F16(true, true, false, kMB, kNB, kNoEpilogue); else NVFP4_LAUNCH_F16(false, true, false, kMB, kNB, kNoEpilogue);
     } else {
       return hipErrorInvalidValue;   // (pick_tile offers none)
     }
   } else {
-    if (bf16_out) NVFP4_LAUNCH_F16(true, false, false, kMB, kNB); else NVFP4_LAUNCH_F16(false, false, false, kMB, kNB);
+    if (bf16_out) NVFP4_LAUNCH_F16(true, false, false, kMB, kNB, kNoEpilogue); else NVFP4_LAUNCH_F16(false, false, false, kMB, kNB, kNoEpilogue);
   }
   return hipGetLastError();
 }

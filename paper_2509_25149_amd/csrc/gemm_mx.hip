@@ -143,9 +143,10 @@ __device__ __forceinline__ void mfma(float4v& acc, const int4v& b, const int4v& 
 
 // For K not a multiple of 512, and scales that are not 16-byte aligned.  Bound by the number of line requests (see gemm_mx_kernel_k512): 4096 x 5120 with K = 4224, 4352, 4480 takes 94, 93, 100 us
 // (bf16; FP32 102, 102, 108), where the other kernel takes 47 and 48 (49, 53) with K = 4096 and 4608; with K = 128 and 640 19 and 28 (27, 35).
-template <bool kBf16Out>
+// kKind: the kind of epilogue; with one the output type is decided at run time (kBf16Out is false).
+template <bool kBf16Out, int kKind>
 __global__ __launch_bounds__(kThreads) void gemm_mx_kernel_any_k(Operand A, Operand B, int64_t K, void* __restrict__ Dv,
-                                                                 int64_t ldd, bool accumulate, int tiles_m, int tiles_n) {
+                                                                 int64_t ldd, bool accumulate, int tiles_m, int tiles_n, EpilogueArg<kKind> epilogue) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
 
   // Workgroup -> tile: consecutive ids go to different XCDs (round robin over 8, one L2 each);
@@ -261,8 +262,11 @@ __global__ __launch_bounds__(kThreads) void gemm_mx_kernel_any_k(Operand A, Oper
   const TensorScales out_scale{A.ts, B.ts, false, false};    // both are 1 for MXFP4 (no tensor-level scale)
   const int Mt = static_cast<int>(A.outer - m0 < TM ? A.outer - m0 : TM);
   const int Nt = static_cast<int>(B.outer - n0 < TN ? B.outer - n0 : TN);
-  store_wave_block<kBf16Out>(acc, out_scale, Dv, ldd, accumulate, m0 + wm * 128, n0 + wn * 128, Mt - wm * 128, Nt - wn * 128,
-                             lane);
+  if constexpr (kKind != kNoEpilogue)
+    store_wave_block_epilogue<kKind, 8, 8>(acc, out_scale, epilogue, Dv, ldd, m0 + wm * 128, n0 + wn * 128, Mt - wm * 128, Nt - wn * 128, lane);
+  else
+    store_wave_block<kBf16Out>(acc, out_scale, Dv, ldd, accumulate, m0 + wm * 128, n0 + wn * 128, Mt - wm * 128, Nt - wn * 128,
+                               lane);
 }
 
 // ---------------------------------------------------------------- K a multiple of 512
@@ -375,9 +379,9 @@ struct Schedule {
 // neither drains nor refills at a tile boundary.  K is a multiple of 512, so every tile is an even number of stages
 // and a whole number of scale chunks: the stage buffers simply keep turning.  The output stage's stores are not waited for.
 // kNB: 16-column blocks per wavefront (2 x 2 wavefronts of 8 16-row blocks).
-template <bool kBf16Out, int kNB>
+template <bool kBf16Out, int kNB, int kKind>
 __global__ __launch_bounds__(kThreads) void gemm_mx_kernel_k512(Operand A, Operand B, int64_t K, void* __restrict__ Dv,
-                                                                int64_t ldd, bool accumulate, int tiles_m, int tiles_n) {
+                                                                int64_t ldd, bool accumulate, int tiles_m, int tiles_n, EpilogueArg<kKind> epilogue) {
   using S = Schedule<kNB>;
   constexpr int kMB = S::kMB, kTM = TM, kTN = 32 * kNB, kStageBytes = wide_stage_bytes(kNB), kOperandBytes = kTM * kWideRowBytes;
   constexpr int kR = S::kR, kHalf = S::kHalf;
@@ -563,7 +567,7 @@ __global__ __launch_bounds__(kThreads) void gemm_mx_kernel_k512(Operand A, Opera
       // The lower half's A fragments are back; in a stage's second step the next stage has landed (its loads and scales: all but those of this step).
       if constexpr (kSecond) {
         if (kS == 1 && stores_behind && st == 0)
-          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(S::kEarlyLoads + kTileStoresMx<kBf16Out, kNB> > 63 ? 63 : S::kEarlyLoads + kTileStoresMx<kBf16Out, kNB>) : "memory");
+          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(S::kEarlyLoads + kTileStoresMx<kBf16Out || kKind != kNoEpilogue, kNB> > 63 ? 63 : S::kEarlyLoads + kTileStoresMx<kBf16Out || kKind != kNoEpilogue, kNB>) : "memory");
         else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(S::kEarlyLoads) : "memory");
         __builtin_amdgcn_s_barrier();
       } else {
@@ -627,7 +631,11 @@ __global__ __launch_bounds__(kThreads) void gemm_mx_kernel_k512(Operand A, Opera
     const int64_t m0 = static_cast<int64_t>(tm) * kTM, n0 = static_cast<int64_t>(tn) * kTN;
     const int Mt = static_cast<int>(A.outer - m0 < kTM ? A.outer - m0 : kTM);
     const int Nt = static_cast<int>(B.outer - n0 < kTN ? B.outer - n0 : kTN);
-    store_wave_block<kBf16Out, kNB>(acc, out_scale, Dv, ldd, accumulate, m0 + wm * (16 * kMB), n0 + wn * (16 * kNB), Mt - wm * (16 * kMB),
+    if constexpr (kKind != kNoEpilogue)
+      store_wave_block_epilogue<kKind, kMB, kNB>(acc, out_scale, epilogue, Dv, ldd, m0 + wm * (16 * kMB), n0 + wn * (16 * kNB), Mt - wm * (16 * kMB),
+                                                 Nt - wn * (16 * kNB), lane);
+    else
+      store_wave_block<kBf16Out, kNB>(acc, out_scale, Dv, ldd, accumulate, m0 + wm * (16 * kMB), n0 + wn * (16 * kNB), Mt - wm * (16 * kMB),
                                                      Nt - wn * (16 * kNB), lane);
     if (!has_next) break;
     stores_behind = Mt == kTM && Nt == kTN;   // every lane stored every block: the count is known
@@ -641,12 +649,12 @@ __global__ __launch_bounds__(kThreads) void gemm_mx_kernel_k512(Operand A, Opera
 
 }  // namespace
 
-template <class Kernel>
-static hipError_t launch_mx(Kernel kernel, PerDeviceOnce& once, int lds_bytes, const GemmArgs& g, dim3 grid, int tiles_m, int tiles_n,
-                            hipStream_t s) {
+template <class Kernel, int kKind>
+static hipError_t launch_mx(Kernel kernel, PerDeviceOnce& once, int lds_bytes, const GemmArgs& g, const EpilogueArg<kKind>& epilogue, dim3 grid, int tiles_m,
+                            int tiles_n, hipStream_t s) {
   const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), lds_bytes, once);   // more dynamic LDS than the default limit
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds_bytes, s, g.a, g.b, g.K, g.d, g.ldd, g.accumulate, tiles_m, tiles_n);
+  hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds_bytes, s, g.a, g.b, g.K, g.d, g.ldd, g.accumulate, tiles_m, tiles_n, epilogue);
   return hipGetLastError();
 }
 
@@ -673,15 +681,30 @@ static int pick_mx_width(int64_t M, int64_t N) {
   return best;
 }
 
-template <int kNB>
-static hipError_t launch_k512(const GemmArgs& g, int tiles_m, hipStream_t s) {
-  static PerDeviceOnce once_bf16, once_f32;
+template <bool kBf16Out, int kNB, int kKind>
+static hipError_t launch_k512_as(const GemmArgs& g, const EpilogueArg<kKind>& epilogue, int tiles_m, hipStream_t s) {
+  static PerDeviceOnce once;
   const int tiles_n = static_cast<int>((g.b.outer + 32 * kNB - 1) / (32 * kNB));
   const int64_t tiles = static_cast<int64_t>(tiles_m) * tiles_n;
   const dim3 grid(static_cast<unsigned>(tiles < 256 ? tiles : 256));   // one workgroup per CU, each running its tiles as one stream
-  constexpr int lds = wide_lds_bytes(kNB);
-  if (g.out_bf16) return launch_mx(gemm_mx_kernel_k512<true, kNB>, once_bf16, lds, g, grid, tiles_m, tiles_n, s);
-  return launch_mx(gemm_mx_kernel_k512<false, kNB>, once_f32, lds, g, grid, tiles_m, tiles_n, s);
+  return launch_mx(gemm_mx_kernel_k512<kBf16Out, kNB, kKind>, once, wide_lds_bytes(kNB), g, epilogue, grid, tiles_m, tiles_n, s);
+}
+template <int kNB>
+static hipError_t launch_k512(const GemmArgs& g, int tiles_m, hipStream_t s) {
+  switch (epilogue_kind(g.epilogue)) {
+    case kForward: return launch_k512_as<false, kNB, kForward>(g, *g.epilogue, tiles_m, s);
+    case kResidual: return launch_k512_as<false, kNB, kResidual>(g, *g.epilogue, tiles_m, s);
+    case kGrad: return launch_k512_as<false, kNB, kGrad>(g, *g.epilogue, tiles_m, s);
+    default: break;
+  }
+  return g.out_bf16 ? launch_k512_as<true, kNB, kNoEpilogue>(g, {}, tiles_m, s) : launch_k512_as<false, kNB, kNoEpilogue>(g, {}, tiles_m, s);
+}
+
+template <bool kBf16Out, int kKind>
+static hipError_t launch_any_k(const GemmArgs& g, const EpilogueArg<kKind>& epilogue, int tiles_m, int tiles_n, hipStream_t s) {
+  static PerDeviceOnce once;
+  const dim3 grid(static_cast<unsigned>(tiles_m) * static_cast<unsigned>(tiles_n));
+  return launch_mx(gemm_mx_kernel_any_k<kBf16Out, kKind>, once, kLdsBytes, g, epilogue, grid, tiles_m, tiles_n, s);
 }
 
 hipError_t launch_gemm_mx(const GemmArgs& g, hipStream_t s) {
@@ -698,10 +721,13 @@ hipError_t launch_gemm_mx(const GemmArgs& g, hipStream_t s) {
       default: return launch_k512<8>(g, tiles_m, s);
     }
   }
-  const dim3 grid(static_cast<unsigned>(tiles_m) * static_cast<unsigned>(tiles_n));
-  static PerDeviceOnce set[2];
-  if (g.out_bf16) return launch_mx(gemm_mx_kernel_any_k<true>, set[0], kLdsBytes, g, grid, tiles_m, tiles_n, s);
-  return launch_mx(gemm_mx_kernel_any_k<false>, set[1], kLdsBytes, g, grid, tiles_m, tiles_n, s);
+  switch (epilogue_kind(g.epilogue)) {
+    case kForward: return launch_any_k<false, kForward>(g, *g.epilogue, tiles_m, tiles_n, s);
+    case kResidual: return launch_any_k<false, kResidual>(g, *g.epilogue, tiles_m, tiles_n, s);
+    case kGrad: return launch_any_k<false, kGrad>(g, *g.epilogue, tiles_m, tiles_n, s);
+    default: break;
+  }
+  return g.out_bf16 ? launch_any_k<true, kNoEpilogue>(g, {}, tiles_m, tiles_n, s) : launch_any_k<false, kNoEpilogue>(g, {}, tiles_m, tiles_n, s);
 }
 
 }  // namespace nvfp4

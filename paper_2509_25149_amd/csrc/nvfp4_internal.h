@@ -74,6 +74,17 @@ struct Operand {
   int ts_per_row = 0;   // 0: ts = {s_dec, amax}; 1: ts = s_dec of every row, then the amax of every row (App. B.1, last sentence)
   const void* fp16 = nullptr;   // the copy already decoded to FP16 [outer, K] (nvfp4_predecode), or null
 };
+// What nvfp4_gemm_epilogue does to the scaled sums before they are stored (gemm_epilogue.h); null pointers where there is nothing to do.
+struct GemmEpilogue {
+  const float* bias;           // [N]
+  const void* residual;        // [M, N], leading dimension ldr
+  int64_t ldr;
+  uint8_t *keep_codes, *keep_scales;             // 8 bits of sum + bias
+  const uint8_t *grad_codes, *grad_scales;       // 8 bits whose act' the sums are multiplied by
+  int64_t cols;                // N
+  int act;
+  bool residual_bf16, out_bf16;
+};
 struct GemmArgs {
   Operand a, b;  // D[m, n] = sum_k A[m, k] B[n, k]
   int64_t K;
@@ -84,6 +95,7 @@ struct GemmArgs {
   bool mx = false;   // operands are MXFP4 (UE8M0 scale per 32) instead of NVFP4
   void* workspace;        // optional: room for both operands decoded to FP16
   size_t workspace_bytes;
+  const GemmEpilogue* epilogue = nullptr;   // (not with accumulate)
 };
 hipError_t launch_gemm(const GemmArgs& g, hipStream_t s);
 // Two products, each as by launch_gemm and in this order; in one launch where both are small (see gemm_direct_pair_kernel), that is faster and neither's result lies over what the other

@@ -50,8 +50,9 @@ def slope(z, name):
         return np.ones_like(z)
     p = logistic_argument(z, name)
     dp = np.ones_like(z) if name == "silu" else 2 * np.sqrt(2 / np.pi) * (1 + 3 * 0.044715 * z * z)
-    s = 1 / (1 + np.exp(-p))
-    return s + z * s * (1 / (1 + np.exp(p))) * dp
+    with np.errstate(over="ignore"):
+        s = 1 / (1 + np.exp(-p))
+        return s + z * s * (1 / (1 + np.exp(p))) * dp
 
 
 def act_tolerance(z, name):
@@ -67,7 +68,8 @@ def slope_tolerance(z, name):
         return 2.0 ** -23 * np.abs(slope(z, name))
     p = logistic_argument(z, name)
     dp = np.ones_like(z) if name == "silu" else 2 * np.sqrt(2 / np.pi) * (1 + 3 * 0.044715 * z * z)
-    s, t = 1 / (1 + np.exp(-p)), 1 / ((1 + np.exp(-p)) * (1 + np.exp(p)))
+    with np.errstate(over="ignore"):
+        s, t = 1 / (1 + np.exp(-p)), 1 / ((1 + np.exp(-p)) * (1 + np.exp(p)))
     return 2.0 ** -22 * (4 + 2 * np.abs(p)) * (s + np.abs(z) * t * dp) + 1e-37
 
 

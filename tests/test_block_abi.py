@@ -82,3 +82,27 @@ def test_the_binding_refuses():
                  lambda: nv.nvfp4_rmsnorm_backward(x, x, torch.zeros(4)), lambda: nv.Checkpoint8(x.byte(), x.byte())):
         with pytest.raises(ValueError):
             call()
+
+
+def test_gemm_epilogue_refuses(lib):
+    def desc(rows, cols):
+        d = nv.QTensorStruct()
+        d.rows, d.cols, d.layout_mask, d.block_dim = rows, cols, 1, 1
+        d.row_codes = d.row_scales = d.row_tensor_scale = P
+        return d
+
+    def call(m=32, n=48, k=64, kb=64, epilogue=True, d=P, dt=1, ldd=48, **e):
+        a, b, s = desc(m, k), desc(n, kb), nv.EpilogueStruct(**e)
+        return lib.nvfp4_gemm_epilogue(ctypes.byref(a), ctypes.byref(b), 1, ctypes.byref(s) if epilogue else None, d, dt, ldd, None, 0, None)
+
+    def c(rows=32, cols=48, codes=P, scales=P):
+        return ctypes.pointer(nv.CheckpointStruct(rows, cols, codes, scales))
+    assert ctypes.sizeof(nv.EpilogueStruct) == 48
+    assert call(epilogue=False) == -1 and call(d=None) == -1 and call(dt=2) == -1 and call(dt=3) == -1 and call(activation=4) == -1 and call(activation=-1) == -1
+    assert call(kb=80) == -4 and call(ldd=40) == -2 and call(ldd=52) == -2 and call(d=P + 8) == -1       # as nvfp4_gemm
+    assert call(bias=P + 4) == -1
+    assert call(residual=P, ldr=40) == -2 and call(residual=P, ldr=50) == -2 and call(residual=P + 8, ldr=48) == -1 and call(residual=P, ldr=48, residual_dtype=2) == -1
+    assert call(keep=c(cols=64)) == -4 and call(keep=c(rows=16)) == -4 and call(keep=c(codes=None)) == -1 and call(keep=c(codes=P + 4)) == -1
+    assert call(grad_of=c(rows=48)) == -4 and call(grad_of=c(scales=None)) == -1
+    for other in (dict(bias=P), dict(residual=P, ldr=48), dict(keep=c())):
+        assert call(grad_of=c(), **other) == -1                                                            # one form or the other
