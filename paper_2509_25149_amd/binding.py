@@ -7,6 +7,7 @@ There is no CPU fallback: if the library is missing, loading raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import NamedTuple, Optional
@@ -374,6 +375,8 @@ def nvfp4_dequantize(q: QTensor, which_copy: int, undo_rht: bool = False, out_dt
 
 
 # ---------------------------------------------------------------- around the linear layers
+# (Small calls take as long as the host needs for them, of which allocating an output is 1.3 us, 1.7 to 2.3 where torch.empty is given the sizes as a
+# tuple or torch.Size, and every look at a tensor 0.1: each tensor is looked at once.)
 
 _DTYPES = {torch.float32: OUT_F32, torch.bfloat16: OUT_BF16}
 _TORCH = {OUT_F32: torch.float32, OUT_BF16: torch.bfloat16}
@@ -387,10 +390,13 @@ class Checkpoint8:
         if codes.dim() != 2 or codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or not codes.is_cuda or not scales.is_cuda or \
                 not codes.is_contiguous() or not scales.is_contiguous() or scales.shape != (codes.shape[0], codes.shape[1] // 16):
             raise ValueError("codes and scales must be contiguous uint8 CUDA tensors [rows, cols] and [rows, cols // 16]")
-        self.codes, self.scales = codes, scales
-        self.rows, self.cols = codes.shape
-        self.desc = CheckpointStruct(self.rows, self.cols, codes.data_ptr(), scales.data_ptr())
+        self._set(codes, scales, *codes.shape)
+
+    def _set(self, codes, scales, rows, cols):
+        self.codes, self.scales, self.rows, self.cols = codes, scales, rows, cols
+        self.desc = CheckpointStruct(rows, cols, codes.data_ptr(), scales.data_ptr())
         self.ref = ctypes.byref(self.desc)
+        return self
 
 
 class NormResult(NamedTuple):
@@ -400,31 +406,36 @@ class NormResult(NamedTuple):
     checkpoint: Optional[Checkpoint8]
 
 
+def checkpoint_sizes(rows: int, cols: int):
+    c, s = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(load_library().nvfp4_checkpoint_sizes(rows, cols, ctypes.addressof(c), ctypes.addressof(s)))
+    return c.value, s.value
+
+
 def alloc_checkpoint(rows: int, cols: int, device="cuda") -> Checkpoint8:
-    _check(load_library().nvfp4_checkpoint_sizes(rows, cols, None, None))
-    return Checkpoint8(torch.empty((rows, cols), dtype=torch.uint8, device=device), torch.empty((rows, cols // 16), dtype=torch.uint8, device=device))
+    if rows < 0 or cols <= 0 or cols % 16:
+        checkpoint_sizes(rows, cols)                  # says what is wrong
+    return Checkpoint8.__new__(Checkpoint8)._set(torch.empty(rows, cols, dtype=torch.uint8, device=device),
+                                                 torch.empty(rows, cols // 16, dtype=torch.uint8, device=device), rows, cols)
 
 
-def _matrix(t: torch.Tensor, what: str, shape=None) -> int:
-    """Element type of a 2-D FP32 or bf16 CUDA tensor whose rows are contiguous."""
-    dt = _DTYPES.get(t.dtype)
-    if dt is None or not t.is_cuda or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] != 1) or (shape is not None and t.shape != shape):
+def _matrix(t: torch.Tensor, what: str, shape=None):
+    """Element type, address and leading dimension of a 2-D FP32 or bf16 CUDA tensor whose rows are contiguous."""
+    dt, size, strides = _DTYPES.get(t.dtype), t.shape, t.stride()
+    if dt is None or len(size) != 2 or (strides[1] != 1 and size[1] != 1) or not t.is_cuda or (shape is not None and size != shape):
         raise ValueError(f"{what} must be a 2-D float32 or bf16 CUDA tensor with unit inner stride" + (f" of shape {tuple(shape)}" if shape is not None else ""))
-    return dt
-
-
-def _ld(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])     # (torch leaves the stride of a single row open)
+    return dt, t.data_ptr(), strides[0] if size[0] > 1 else max(strides[0], size[1])     # (torch leaves the stride of a single row open)
 
 
 def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
+    if t.dtype != torch.float32 or t.shape != (n,) or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous float32 CUDA tensor of {n} elements")
     return t.data_ptr()
 
 
+@functools.lru_cache(maxsize=1024)
 def rowsum_workspace_bytes(rows: int, cols: int) -> int:
     w = ctypes.c_size_t()
     _check(load_library().nvfp4_rowsum_workspace_bytes(rows, cols, ctypes.addressof(w)))
@@ -433,29 +444,35 @@ def rowsum_workspace_bytes(rows: int, cols: int) -> int:
 
 def _rowsum_workspace(workspace: Optional[torch.Tensor], rows: int, cols: int, device):
     if workspace is None:
-        workspace = _workspace(device, rowsum_workspace_bytes(rows, cols))
+        need = rowsum_workspace_bytes(rows, cols)
+        if need == 0:
+            return None, 0
+        workspace = _workspace(device, need)
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def nvfp4_checkpoint_save(x: torch.Tensor, out: Optional[Checkpoint8] = None) -> Checkpoint8:
     """Keep x (float32 or bf16, [rows, cols]) in 8 bits."""
-    dt = _matrix(x, "x")
+    dt, xp, ldx = _matrix(x, "x")
+    rows, cols = x.shape
     if out is None:
-        out = alloc_checkpoint(*x.shape, x.device)
-    elif (out.rows, out.cols) != tuple(x.shape):
+        out = alloc_checkpoint(rows, cols, x.device)
+    elif (out.rows, out.cols) != (rows, cols):
         raise ValueError("out must have the shape of x")
-    _check(load_library().nvfp4_checkpoint_save(x.data_ptr(), dt, _ld(x), out.ref, _stream()))
+    _check(load_library().nvfp4_checkpoint_save(xp, dt, ldx, out.ref, _stream()))
     return out
 
 
 def nvfp4_checkpoint_load(checkpoint: Checkpoint8, activation: int = ACT_NONE, col_scale: Optional[torch.Tensor] = None, out_dtype: int = OUT_BF16,
                           out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """act(values) * col_scale."""
-    shape = (checkpoint.rows, checkpoint.cols)
+    rows, cols = checkpoint.rows, checkpoint.cols
     if out is None:
-        out = torch.empty(shape, dtype=_TORCH[out_dtype], device=checkpoint.codes.device)
-    dt = _matrix(out, "out", shape)
-    _check(load_library().nvfp4_checkpoint_load(checkpoint.ref, activation, _vector(col_scale, shape[1], "col_scale"), out.data_ptr(), dt, _ld(out), _stream()))
+        out = torch.empty(rows, cols, dtype=_TORCH[out_dtype], device=checkpoint.codes.device)
+        dt, op, ld = out_dtype, out.data_ptr(), cols
+    else:
+        dt, op, ld = _matrix(out, "out", (rows, cols))
+    _check(load_library().nvfp4_checkpoint_load(checkpoint.ref, activation, _vector(col_scale, cols, "col_scale"), op, dt, ld, _stream()))
     return out
 
 
@@ -465,32 +482,40 @@ def nvfp4_rmsnorm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor] = None,
                           rstd: Optional[torch.Tensor] = None) -> NormResult:
     """y = norm(x + residual) * gamma.  h_dtype: type of x + residual (default: the residual's, which has to have it).  y_dtype None: no y.
     checkpoint: True or a Checkpoint8 to keep the normalised rows (or, NORM_KEEP_OUTPUT, y) in 8 bits."""
-    xt = _matrix(x, "x")
-    rows, cols = x.shape
+    xt, xp, ldx = _matrix(x, "x")
+    size, device = x.shape, x.device
+    rows, cols = size
     ht, rp, ldr, hp, ldh = xt, None, 0, None, 0
     if residual is not None:
-        ht = _matrix(residual, "residual", x.shape)
+        ht, rp, ldr = _matrix(residual, "residual", size)
         if h_dtype is not None and h_dtype != ht:
             raise ValueError("residual must be of type h_dtype")
         if h is None:
-            h = torch.empty((rows, cols), dtype=residual.dtype, device=x.device)
-        elif _matrix(h, "h", x.shape) != ht:
-            raise ValueError("h must be of the residual's type")
-        rp, ldr, hp, ldh = residual.data_ptr(), _ld(residual), h.data_ptr(), _ld(h)
+            h = torch.empty_like(residual)     # (rows are contiguous: so is what is like them)
+            hp, ldh = h.data_ptr(), cols
+        else:
+            t, hp, ldh = _matrix(h, "h", size)
+            if t != ht:
+                raise ValueError("h must be of the residual's type")
     elif h is not None:
         raise ValueError("h without a residual is x itself")
     yt, yp, ldy = OUT_BF16, None, 0
-    if y is not None or y_dtype is not None:
-        if y is None:
-            y = torch.empty((rows, cols), dtype=_TORCH[y_dtype], device=x.device)
-        yt, yp, ldy = _matrix(y, "y", x.shape), y.data_ptr(), _ld(y)
+    if y is not None:
+        yt, yp, ldy = _matrix(y, "y", size)
+    elif y_dtype is not None:
+        y = torch.empty_like(x) if y_dtype == xt else torch.empty_like(x, dtype=_TORCH[y_dtype])
+        yt, yp, ldy = y_dtype, y.data_ptr(), cols
     if rstd is None:
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-    keep = None
+        rstd = torch.empty(rows, dtype=torch.float32, device=device)
+        sp = rstd.data_ptr()
+    else:
+        sp = _vector(rstd, rows, "rstd")
+    keep = ref = None
     if checkpoint is not None and checkpoint is not False:
-        keep = checkpoint if isinstance(checkpoint, Checkpoint8) else alloc_checkpoint(rows, cols, x.device)
-    _check(load_library().nvfp4_rmsnorm_forward(x.data_ptr(), xt, _ld(x), rp, ldr, _vector(gamma, cols, "gamma"), eps, rows, cols, hp, ht, ldh, yp, yt, ldy,
-                                                _vector(rstd, rows, "rstd"), None if keep is None else keep.ref, keep_kind, _stream()))
+        keep = checkpoint if isinstance(checkpoint, Checkpoint8) else alloc_checkpoint(rows, cols, device)
+        ref = keep.ref
+    _check(load_library().nvfp4_rmsnorm_forward(xp, xt, ldx, rp, ldr, _vector(gamma, cols, "gamma"), eps, rows, cols, hp, ht, ldh, yp, yt, ldy, sp, ref,
+                                                keep_kind, _stream()))
     return NormResult(y, x if residual is None else h, rstd, keep)
 
 
@@ -499,31 +524,36 @@ def nvfp4_rmsnorm_backward(dy: torch.Tensor, saved, rstd: torch.Tensor, gamma: O
                            accumulate_dgamma: bool = False, workspace: Optional[torch.Tensor] = None):
     """saved: the norm's input h, or the Checkpoint8 of the normalised rows.  h, dres and dx are of one type (dx_dtype; default: h's, dres's or dy's).
     dgamma: float32 [cols], added into with accumulate_dgamma.  Returns (dx, dgamma)."""
-    dt = _matrix(dy, "dy")
-    rows, cols = dy.shape
+    dt, yp, ldy = _matrix(dy, "dy")
+    size, device = dy.shape, dy.device
+    rows, cols = size
     st = dx_dtype
     hp, ldh, sp, rp, ldr = None, 0, None, None, 0
     if isinstance(saved, Checkpoint8):
         sp = saved.ref
     else:
-        st = _one_type(st, _matrix(saved, "saved", dy.shape))
-        hp, ldh = saved.data_ptr(), _ld(saved)
+        t, hp, ldh = _matrix(saved, "saved", size)
+        st = _one_type(st, t)
     if dres is not None:
-        st = _one_type(st, _matrix(dres, "dres", dy.shape))
-        rp, ldr = dres.data_ptr(), _ld(dres)
+        t, rp, ldr = _matrix(dres, "dres", size)
+        st = _one_type(st, t)
     if dx is not None:
-        st = _one_type(st, _matrix(dx, "dx", dy.shape))
+        t, xp, ldx = _matrix(dx, "dx", size)
+        st = _one_type(st, t)
     else:
         st = dt if st is None else st
-        dx = torch.empty((rows, cols), dtype=_TORCH[st], device=dy.device)
+        dx = torch.empty_like(dy) if st == dt else torch.empty_like(dy, dtype=_TORCH[st])
+        xp, ldx = dx.data_ptr(), cols
     if dgamma is None:
         if accumulate_dgamma:
             raise ValueError("accumulate_dgamma needs dgamma")
-        dgamma = torch.empty(cols, dtype=torch.float32, device=dy.device)
-    ws, ws_bytes = _rowsum_workspace(workspace, rows, cols, dy.device)
-    _check(load_library().nvfp4_rmsnorm_backward(dy.data_ptr(), dt, _ld(dy), hp, ldh, sp, _vector(rstd, rows, "rstd"), _vector(gamma, cols, "gamma"), rp, ldr,
-                                                 rows, cols, dx.data_ptr(), st, _ld(dx), _vector(dgamma, cols, "dgamma"), int(accumulate_dgamma), ws, ws_bytes,
-                                                 _stream()))
+        dgamma = torch.empty(cols, dtype=torch.float32, device=device)
+        gp = dgamma.data_ptr()
+    else:
+        gp = _vector(dgamma, cols, "dgamma")
+    ws, ws_bytes = _rowsum_workspace(workspace, rows, cols, device)
+    _check(load_library().nvfp4_rmsnorm_backward(yp, dt, ldy, hp, ldh, sp, _vector(rstd, rows, "rstd"), _vector(gamma, cols, "gamma"), rp, ldr, rows, cols, xp, st,
+                                                 ldx, gp, int(accumulate_dgamma), ws, ws_bytes, _stream()))
     return dx, dgamma
 
 
@@ -538,25 +568,34 @@ def nvfp4_activation_backward(da: torch.Tensor, saved: Optional[Checkpoint8] = N
                               workspace: Optional[torch.Tensor] = None):
     """dz = da * act'(z) from z's checkpoint, dbias = the sum of dz over rows (float32 [cols], added into with accumulate_dbias).
     Returns (dz, dbias), None for what is not asked for."""
-    dt = _matrix(da, "da")
-    rows, cols = da.shape
+    dt, ap, lda = _matrix(da, "da")
+    size, device = da.shape, da.device
+    rows, cols = size
     zp, ldz = None, 0
-    if want_dz:
-        if dz is None:
-            dz = torch.empty((rows, cols), dtype=da.dtype, device=da.device)
-        elif _matrix(dz, "dz", da.shape) != dt:
+    if not want_dz:
+        dz = None
+    elif dz is None:
+        dz = torch.empty_like(da)
+        zp, ldz = dz.data_ptr(), cols
+    else:
+        t, zp, ldz = _matrix(dz, "dz", size)
+        if t != dt:
             raise ValueError("dz must be of the type of da")
-        zp, ldz = dz.data_ptr(), _ld(dz)
-    ws, ws_bytes = None, 0
-    if bias_grad:
+    ws, ws_bytes, bp = None, 0, None
+    if not bias_grad:
+        dbias = None
+    else:
         if dbias is None:
             if accumulate_dbias:
                 raise ValueError("accumulate_dbias needs dbias")
-            dbias = torch.empty(cols, dtype=torch.float32, device=da.device)
-        ws, ws_bytes = _rowsum_workspace(workspace, rows, cols, da.device)
-    _check(load_library().nvfp4_activation_backward(da.data_ptr(), dt, _ld(da), rows, cols, None if saved is None else saved.ref, activation, zp, ldz,
-                                                    _vector(dbias, cols, "dbias") if bias_grad else None, int(accumulate_dbias), ws, ws_bytes, _stream()))
-    return dz if want_dz else None, dbias if bias_grad else None
+            dbias = torch.empty(cols, dtype=torch.float32, device=device)
+            bp = dbias.data_ptr()
+        else:
+            bp = _vector(dbias, cols, "dbias")
+        ws, ws_bytes = _rowsum_workspace(workspace, rows, cols, device)
+    _check(load_library().nvfp4_activation_backward(ap, dt, lda, rows, cols, None if saved is None else saved.ref, activation, zp, ldz, bp, int(accumulate_dbias), ws,
+                                                    ws_bytes, _stream()))
+    return dz, dbias
 
 
 def nvfp4_gemm_epilogue(a: QTensor, b: QTensor, op: int, bias: Optional[torch.Tensor] = None, activation: int = ACT_NONE,
@@ -566,24 +605,19 @@ def nvfp4_gemm_epilogue(a: QTensor, b: QTensor, op: int, bias: Optional[torch.Te
     as for nvfp4_gemm."""
     m = a.cols if op == OP_WGRAD else a.rows
     n = b.rows if op == OP_DGRAD else b.cols
-    e = EpilogueStruct(activation=activation)
-    if bias is not None:
-        e.bias = _vector(bias, n, "bias")
+    e = EpilogueStruct(None if bias is None else _vector(bias, n, "bias"), None, 0, None if keep is None else ctypes.pointer(keep.desc),
+                       None if grad_of is None else ctypes.pointer(grad_of.desc), OUT_F32, activation)
     if residual is not None:
-        e.residual_dtype = _matrix(residual, "residual", (m, n))
-        e.residual, e.ldr = residual.data_ptr(), _ld(residual)
-    if keep is not None:
-        e.keep = ctypes.pointer(keep.desc)
-    if grad_of is not None:
-        e.grad_of = ctypes.pointer(grad_of.desc)
+        e.residual_dtype, e.residual, e.ldr = _matrix(residual, "residual", (m, n))
     if out is None:
-        dev = (a.row_codes if a.row_codes is not None else a.col_codes).device
-        out = torch.empty((m, n), dtype=_TORCH[out_dtype], device=dev)
-    elif _matrix(out, "out", (m, n)) != out_dtype:
-        raise ValueError("out must be of type out_dtype")
+        out = torch.empty(m, n, dtype=_TORCH[out_dtype], device=(a.row_codes if a.row_codes is not None else a.col_codes).device)
+        op_, ldd = out.data_ptr(), n
+    else:
+        t, op_, ldd = _matrix(out, "out", (m, n))
+        if t != out_dtype:
+            raise ValueError("out must be of type out_dtype")
     ws_ptr, ws_bytes = (workspace.data_ptr(), workspace.numel()) if workspace is not None else (None, 0)
-    _check(load_library().nvfp4_gemm_epilogue(ctypes.byref(a.desc), ctypes.byref(b.desc), op, ctypes.byref(e), out.data_ptr(), out_dtype, _ld(out), ws_ptr, ws_bytes,
-                                              _stream()))
+    _check(load_library().nvfp4_gemm_epilogue(ctypes.byref(a.desc), ctypes.byref(b.desc), op, ctypes.byref(e), op_, out_dtype, ldd, ws_ptr, ws_bytes, _stream()))
     return out
 
 

@@ -2,7 +2,8 @@
 //   forward   h = x + r;  rstd = 1 / sqrt(mean(h^2) + eps);  xhat = h rstd;  y = xhat gamma;  optionally 8 bits of xhat or y
 //   backward  g = dy gamma;  dx = rstd (g - xhat mean(g xhat)) + dres;  dgamma = sum over rows of dy xhat
 // Sums, statistics and all arithmetic in FP32; every output is rounded once, from the FP32 value (the norm sees x + r before it is rounded for h).
-// One pass: a row stays in registers between its sum and its output, eight columns to a lane and chunk.
+// One pass: a row stays in registers between its sum and its output, eight columns to a lane and chunk.  Memory bounds both.  8192 x 5120, bf16 with residual
+// and 8-bit output: 70 us for 380 MB (5.4 TB/s; a large copy runs at 5.1).
 #include "nvfp4_internal.h"
 #include "checkpoint8.h"
 
@@ -99,14 +100,26 @@ __global__ __launch_bounds__(kWaveRow ? 256 : 1024) void rmsnorm_forward_kernel(
 }
 
 // What a lane holds of a row of the backward pass, as loaded: dy, xhat (h, or its 8 bits), dres.
-template <bool kDyBf16, bool kSBf16, bool kSaved8>
+template <bool kDyBf16, bool kSBf16, bool kSaved8, bool kDres>
 struct BackwardEight {
   Eight<kDyBf16> dy;
   Eight<kSBf16> h, dres;
   uint2 codes;
   uint32_t byte;
-  // g = dy gamma and xhat
-  __device__ __forceinline__ void get(const float* gamma, int col, float rstd, float (&g)[8], float (&xhat)[8]) const {
+  __device__ __forceinline__ void load(const RmsNormBackward& a, int64_t row, int col, bool with_dres) {
+    dy.load(static_cast<const char*>(a.dy) + row * a.lddy * (kDyBf16 ? 2 : 4), col);
+    if (kSaved8) {
+      codes = *reinterpret_cast<const uint2*>(a.codes + row * a.cols + col);
+      byte = a.scales[row * (a.cols / 16) + col / 16];
+    } else {
+      h.load(static_cast<const char*>(a.h) + row * a.ldh * (kSBf16 ? 2 : 4), col);
+    }
+    if (with_dres) load_dres(a, row, col);
+  }
+  __device__ __forceinline__ void load_dres(const RmsNormBackward& a, int64_t row, int col) {
+    if (kDres) dres.load(static_cast<const char*>(a.dres) + row * a.lddr * (kSBf16 ? 2 : 4), col);
+  }
+  __device__ __forceinline__ void get_xhat(float rstd, float (&xhat)[8]) const {
     if (kSaved8) {
       checkpoint_values4(codes.x, byte, xhat);
       checkpoint_values4(codes.y, byte, xhat + 4);
@@ -115,132 +128,149 @@ struct BackwardEight {
 #pragma unroll
       for (int i = 0; i < 8; ++i) xhat[i] *= rstd;
     }
-    dy.get(g);
-    if (gamma) {
-      const float4v *gp = reinterpret_cast<const float4v*>(gamma + col), g0 = gp[0], g1 = gp[1];
+  }
+  // dx = rstd (g - xhat c) + dres
+  __device__ __forceinline__ void get_dx(const float (&g)[8], const float (&xhat)[8], float rstd, float c, float (&d)[8]) const {
+    if (kDres) dres.get(d);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) g[i] *= g0[i], g[4 + i] *= g1[i];
-    }
+    for (int i = 0; i < 8; ++i) d[i] = rstd * (g[i] - xhat[i] * c) + (kDres ? d[i] : 0.0f);
+  }
+  __device__ __forceinline__ void forget() {
+    dy.forget();
+    if (kSaved8) asm volatile("" : "+v"(codes.x), "+v"(codes.y));
+    else h.forget();
   }
 };
 
+__device__ __forceinline__ void load_gamma(const float* gamma, int col, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = 1.0f;
+  if (gamma) {
+    Eight<false> e;
+    e.load(gamma, col);
+    e.get(v);
+  }
+}
+
 // Workgroup w takes rows w, w + parts, ... and leaves its sum of dy xhat in row w of the partial sums (kWaveRow: a wavefront per row, four of them
-// in a workgroup add theirs through LDS).
-template <bool kDyBf16, bool kSBf16, bool kSaved8, int kChunks, bool kWaveRow>
-__global__ __launch_bounds__(kWaveRow ? 256 : 1024) void rmsnorm_backward_kernel(RmsNormBackward a, float* __restrict__ partials, bool add) {
-  // Four chunks: there are no registers for everything; the sums are kept in LDS (each lane its own) and dres is loaded where it is added.
-  constexpr bool kLate = kChunks > 2;
+// in a workgroup add theirs through LDS).  The next row's loads are issued before the row in hand is worked on (kAhead): a workgroup waits for memory once
+// a row otherwise, and few are resident.  For that nothing else may be loaded in the loop -- memory answers in order -- so gamma stays in registers, and
+// columns and rows past the end are replaced by the last instead of being skipped.  8192 x 5120, bf16, from 8 bits, with dres: 60 us = 4.9 TB/s with the second launch's
+// 4 us; 80 with twice as many workgroups that load a row, work on it and store it in turn.
+// Four chunks (more than 16384 columns), and workgroups of more than 512 threads, have no registers for that; with four the sums are kept in LDS too (each
+// lane its own) and dres is loaded where it is added.
+template <bool kDyBf16, bool kSBf16, bool kSaved8, bool kDres, int kChunks, int kMaxThreads, bool kWaveRow>
+__global__ __launch_bounds__(kMaxThreads) void rmsnorm_backward_kernel(RmsNormBackward a, float* __restrict__ partials, bool add) {
+  constexpr bool kAhead = kMaxThreads <= 512, kLate = kChunks > 2;
   extern __shared__ __attribute__((aligned(16))) float lds[];   // a wavefront's sums in two halves, used in turn; kWaveRow: four rows of partial sums
   const int threads = kWaveRow ? 64 : blockDim.x, t = kWaveRow ? threadIdx.x & 63 : threadIdx.x;
   const int wave = threadIdx.x >> 6;
   const int cols = static_cast<int>(a.cols);
   const int64_t first = kWaveRow ? static_cast<int64_t>(blockIdx.x) * 4 + wave : blockIdx.x, step = kWaveRow ? static_cast<int64_t>(gridDim.x) * 4 : gridDim.x;
   const float inv = 1.0f / static_cast<float>(cols);
-
-  float dgamma[kLate ? 1 : kChunks][8] = {};
-  float* const kept = lds + 32;
-  if (kLate) {
+  int col[kChunks];   // of the lane's eight columns, or the row's last eight
+  bool in[kChunks];
 #pragma unroll
-    for (int ch = 0; ch < kChunks; ++ch) {
-      const int col = (ch * threads + t) * 8;
-      if (col < cols) store8(kept, col, false, dgamma[0]);
-    }
+  for (int ch = 0; ch < kChunks; ++ch) {
+    col[ch] = (ch * threads + t) * 8;
+    in[ch] = col[ch] < cols;
+    col[ch] = min(col[ch], cols - 8);
   }
 
+  float dgamma[kLate ? 1 : kChunks][8] = {}, gamma[kAhead ? kChunks : 1][8];
+  float* const kept = lds + 32;
+#pragma unroll
+  for (int ch = 0; ch < kChunks; ++ch) {
+    if (kAhead) load_gamma(a.gamma, col[ch], gamma[kAhead ? ch : 0]);
+    if (kLate && in[ch]) store8(kept, col[ch], false, dgamma[0]);
+  }
+
+  using Loaded = BackwardEight<kDyBf16, kSBf16, kSaved8, kDres>;
+  Loaded row_in[kChunks], next_in[kAhead ? kChunks : 1];
+  float rstd = 0.0f, next_rstd = 0.0f;
+  if (kAhead && first < a.rows) {
+#pragma unroll
+    for (int ch = 0; ch < kChunks; ++ch) row_in[ch].load(a, first, col[ch], true);
+    rstd = a.rstd[first];
+  }
   int turn = 0;
   for (int64_t row = first; row < a.rows; row += step, turn ^= 16) {
-    const void* dy = static_cast<const char*>(a.dy) + row * a.lddy * (kDyBf16 ? 2 : 4);
-    const void* h = static_cast<const char*>(a.h) + row * a.ldh * (kSBf16 ? 2 : 4);
-    const void* dres = static_cast<const char*>(a.dres) + row * a.lddr * (kSBf16 ? 2 : 4);
-    BackwardEight<kDyBf16, kSBf16, kSaved8> in[kChunks];
+    const int64_t from = kAhead ? min(row + step, a.rows - 1) : row;
 #pragma unroll
-    for (int ch = 0; ch < kChunks; ++ch) {
-      const int col = (ch * threads + t) * 8;
-      if (col < cols) {
-        in[ch].dy.load(dy, col);
-        if (kSaved8) {
-          in[ch].codes = *reinterpret_cast<const uint2*>(a.codes + row * a.cols + col);
-          in[ch].byte = a.scales[row * (a.cols / 16) + col / 16];
-        } else {
-          in[ch].h.load(h, col);
-        }
-        if (a.dres && !kLate) in[ch].dres.load(dres, col);
-      }
-    }
-    const float rstd = a.rstd[row];
+    for (int ch = 0; ch < kChunks; ++ch) (kAhead ? next_in[kAhead ? ch : 0] : row_in[ch]).load(a, from, col[ch], !kLate);
+    (kAhead ? next_rstd : rstd) = a.rstd[from];
     float sum = 0.0f;
 #pragma unroll
     for (int ch = 0; ch < kChunks; ++ch) {
-      const int col = (ch * threads + t) * 8;
-      if (col < cols) {
-        float g[8], xhat[8], d[8];
-        in[ch].get(a.gamma, col, rstd, g, xhat);
-        in[ch].dy.get(d);
+      if (in[ch]) {
+        float g[8], xhat[8];
+        row_in[ch].get_xhat(rstd, xhat);
+        row_in[ch].dy.get(g);
         float(&into)[8] = dgamma[kLate ? 0 : ch];
+        float(&gm)[8] = gamma[kAhead ? ch : 0];
+        if (!kAhead) load_gamma(a.gamma, col[ch], gm);
         Eight<false> k;
         if (kLate) {
-          k.load(kept, col);
+          k.load(kept, col[ch]);
           k.get(into);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          into[i] = __builtin_fmaf(d[i], xhat[i], into[i]);
-          sum = __builtin_fmaf(g[i], xhat[i], sum);
+          into[i] = __builtin_fmaf(g[i], xhat[i], into[i]);
+          sum = __builtin_fmaf(g[i] * gm[i], xhat[i], sum);
         }
-        if (kLate) store8(kept, col, false, into);
+        if (kLate) store8(kept, col[ch], false, into);
       }
     }
     const float c = row_sum<kWaveRow>(sum, lds + turn) * inv;
 #pragma unroll
     for (int ch = 0; ch < kChunks; ++ch) {
-      const int col = (ch * threads + t) * 8;
-      if (col < cols && a.dx) {
-        float g[8], xhat[8], d[8] = {};
-        if (kLate) {
-          in[ch].dy.forget();
-          if (kSaved8) asm volatile("" : "+v"(in[ch].codes.x), "+v"(in[ch].codes.y));
-          else in[ch].h.forget();
-        }
-        in[ch].get(a.gamma, col, rstd, g, xhat);
-        if (a.dres) {
-          if (kLate) in[ch].dres.load(dres, col);
-          in[ch].dres.get(d);
-        }
+      if (in[ch] && a.dx) {
+        float g[8], xhat[8], d[8];
+        if (kLate) row_in[ch].forget();
+        row_in[ch].get_xhat(rstd, xhat);
+        row_in[ch].dy.get(g);
+        float(&gm)[8] = gamma[kAhead ? ch : 0];
+        if (!kAhead) load_gamma(a.gamma, col[ch], gm);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] += rstd * (g[i] - xhat[i] * c);
-        store8(static_cast<char*>(a.dx) + row * a.lddx * (kSBf16 ? 2 : 4), col, kSBf16, d);
+        for (int i = 0; i < 8; ++i) g[i] *= gm[i];
+        if (kLate) row_in[ch].load_dres(a, row, col[ch]);
+        row_in[ch].get_dx(g, xhat, rstd, c, d);
+        store8(static_cast<char*>(a.dx) + row * a.lddx * (kSBf16 ? 2 : 4), col[ch], kSBf16, d);
       }
+    }
+    if (kAhead) {
+#pragma unroll
+      for (int ch = 0; ch < kChunks; ++ch) row_in[ch] = next_in[kAhead ? ch : 0];
+      rstd = next_rstd;
     }
   }
   if (!partials) return;
   float* to = partials + static_cast<int64_t>(blockIdx.x) * a.cols;
   if (kWaveRow) {
 #pragma unroll
-    for (int ch = 0; ch < kChunks; ++ch) {
-      const int col = (ch * threads + t) * 8;
-      if (col < cols) store8(lds + wave * cols, col, false, dgamma[kLate ? 0 : ch]);
-    }
+    for (int ch = 0; ch < kChunks; ++ch)
+      if (in[ch]) store8(lds + wave * cols, col[ch], false, dgamma[kLate ? 0 : ch]);
     __syncthreads();
-    for (int col = threadIdx.x; col < cols; col += 256) {
-      const float s = (lds[col] + lds[cols + col]) + (lds[2 * cols + col] + lds[3 * cols + col]);
-      to[col] = add ? to[col] + s : s;
+    for (int c = threadIdx.x; c < cols; c += 256) {
+      const float s = (lds[c] + lds[cols + c]) + (lds[2 * cols + c] + lds[3 * cols + c]);
+      to[c] = add ? to[c] + s : s;
     }
   } else {
 #pragma unroll
     for (int ch = 0; ch < kChunks; ++ch) {
-      const int col = (ch * threads + t) * 8;
-      if (col < cols) {
+      if (in[ch]) {
         float(&sums)[8] = dgamma[kLate ? 0 : ch];
         if (kLate) {
           Eight<false> k;
-          k.load(kept, col);
+          k.load(kept, col[ch]);
           k.get(sums);
         }
         if (add) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) sums[i] += to[col + i];
+          for (int i = 0; i < 8; ++i) sums[i] += to[col[ch] + i];
         }
-        store8(to, col, false, sums);
+        store8(to, col[ch], false, sums);
       }
     }
   }
@@ -278,34 +308,47 @@ hipError_t forward_of(const RmsNormForward& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-constexpr int kMostParts = 512;
+constexpr int kMostCols = 32768;
+// Workgroups of the backward pass: one to a CU where a row has 4096 columns or more, otherwise as many as have that many columns on their way together.  More
+// of them write more partial sums (5120 columns: 5 MB from 256, 10 from 512) and get fewer rows each to overlap.  us with 2048 / 4096 / 8192 / 16384 columns:
+// 8192 x 5120 60 / 60 / 63 / 69, x 2560 44 / 35 / 34 / 40, x 2048 37 / 28 / 30 / 36, x 1024 16 / 16 / 17 / 19, 1040 x 2064 13.1 / 12.9 / 15.9 / 17.
+constexpr int64_t kColsOnTheWay = 4096, kCUs = 256;
 int backward_parts(int64_t rows, int64_t cols) {
-  const int64_t groups = row_shape(cols).wave ? (rows + 3) / 4 : rows;
-  return static_cast<int>(groups < kMostParts ? groups : kMostParts);
+  const int64_t each = row_shape(cols).wave ? 4 : 1, groups = (rows + each - 1) / each;
+  const int64_t most = kCUs * ((kColsOnTheWay + cols * each - 1) / (cols * each));
+  return static_cast<int>(groups < most ? groups : most);
 }
 
-template <bool kDyBf16, bool kSBf16, bool kSaved8>
+template <bool kDyBf16, bool kSBf16, bool kSaved8, bool kDres>
 hipError_t backward_of(const RmsNormBackward& a, int parts, float* partials, bool add, hipStream_t s) {
   const RowShape p = row_shape(a.cols);
   const unsigned lds = p.wave ? static_cast<unsigned>(a.cols) * 16 : 128 + (p.chunks == 4 ? static_cast<unsigned>(a.cols) * 4 : 0);
-  if (p.chunks == 4) {
-    static PerDeviceOnce once;
-    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&rmsnorm_backward_kernel<kDyBf16, kSBf16, kSaved8, 4, false>), 128 + 32768 * 4, once);
-    if (e != hipSuccess) return e;
-  }
-#define NVFP4_NORM(CH, WAVE) \
-  hipLaunchKernelGGL((rmsnorm_backward_kernel<kDyBf16, kSBf16, kSaved8, CH, WAVE>), dim3(parts), dim3(WAVE ? 256 : p.threads), lds, s, a, partials, add)
+#define NVFP4_NORM(CH, MOST, WAVE) \
+  hipLaunchKernelGGL((rmsnorm_backward_kernel<kDyBf16, kSBf16, kSaved8, kDres, CH, MOST, WAVE>), dim3(parts), dim3(WAVE ? 256 : p.threads), lds, s, a, partials, add)
   if (p.wave) {
-    if (p.chunks == 1) NVFP4_NORM(1, true); else NVFP4_NORM(2, true);
+    if (p.chunks == 1) NVFP4_NORM(1, 256, true); else NVFP4_NORM(2, 256, true);
   } else if (p.chunks == 1) {
-    NVFP4_NORM(1, false);
+    NVFP4_NORM(1, 256, false);
   } else if (p.chunks == 2) {
-    NVFP4_NORM(2, false);
+    if (p.threads <= 512) NVFP4_NORM(2, 512, false); else NVFP4_NORM(2, 1024, false);
   } else {
-    NVFP4_NORM(4, false);
+    static PerDeviceOnce once;
+    const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void*>(&rmsnorm_backward_kernel<kDyBf16, kSBf16, kSaved8, kDres, 4, 1024, false>), 128 + kMostCols * 4, once);
+    if (e != hipSuccess) return e;
+    NVFP4_NORM(4, 1024, false);
   }
 #undef NVFP4_NORM
   return hipGetLastError();
+}
+
+template <bool... kFlags>
+hipError_t backward_with(const RmsNormBackward& a, int parts, float* partials, bool add, hipStream_t s) {
+  if constexpr (sizeof...(kFlags) == 4) {
+    return backward_of<kFlags...>(a, parts, partials, add, s);
+  } else {
+    const bool flags[] = {a.dy_bf16, a.s_bf16, a.codes != nullptr, a.dres != nullptr};
+    return flags[sizeof...(kFlags)] ? backward_with<kFlags..., true>(a, parts, partials, add, s) : backward_with<kFlags..., false>(a, parts, partials, add, s);
+  }
 }
 
 }  // namespace
@@ -327,18 +370,7 @@ hipError_t launch_rmsnorm_backward(const RmsNormBackward& a, hipStream_t s) {
   float* partials = a.dgamma ? (parts > 1 ? a.partials : a.dgamma) : nullptr;
   if (parts > 0) {
     const bool add = parts == 1 && a.accumulate;
-    const int kind = (a.dy_bf16 ? 4 : 0) | (a.s_bf16 ? 2 : 0) | (a.codes ? 1 : 0);
-    hipError_t e;
-    switch (kind) {
-      case 0: e = backward_of<false, false, false>(a, parts, partials, add, s); break;
-      case 1: e = backward_of<false, false, true>(a, parts, partials, add, s); break;
-      case 2: e = backward_of<false, true, false>(a, parts, partials, add, s); break;
-      case 3: e = backward_of<false, true, true>(a, parts, partials, add, s); break;
-      case 4: e = backward_of<true, false, false>(a, parts, partials, add, s); break;
-      case 5: e = backward_of<true, false, true>(a, parts, partials, add, s); break;
-      case 6: e = backward_of<true, true, false>(a, parts, partials, add, s); break;
-      default: e = backward_of<true, true, true>(a, parts, partials, add, s); break;
-    }
+    const hipError_t e = backward_with<>(a, parts, partials, add, s);
     if (e != hipSuccess) return e;
   }
   if (!a.dgamma || parts == 1) return hipSuccess;
