@@ -174,18 +174,19 @@ __device__ __forceinline__ void store_wave_block(float4v (&acc)[8][kNB], const T
 
 
 // ---------------------------------------------------------------- what nvfp4_gemm_epilogue does to the scaled sums
-//   z = sum + bias;  8 bits of z are kept;  D = act(z) + residual             (kForward; kResidual: with a residual)
+//   z = sum + bias;  8 bits of z are kept;  D = act(z) + residual             (kForward; kResidualF32, kResidualBf16: with a residual)
 //   D = sum * act'(z), z from its 8 bits                                       (kGrad)
-// All of it in FP32 in registers, D rounded once.  The kinds are instances of their own because two of them load as much as they store; bias, activation,
-// what is kept and the types are decided at run time, alike for the whole launch.
-enum EpilogueKind { kNoEpilogue = 0, kForward = 1, kResidual = 2, kGrad = 3 };
+// All of it in FP32 in registers, D rounded once.  The kinds are instances of their own because all but the first load as much as they store, and the
+// compiler waits for the right loads only where it knows how many follow them; bias, activation, what is kept and D's type are decided at run time, alike
+// for the whole launch.
+enum EpilogueKind { kNoEpilogue = 0, kForward = 1, kResidualF32 = 2, kResidualBf16 = 3, kGrad = 4 };
 template <int kKind>
 struct EpilogueArg : GemmEpilogue {
   __host__ __device__ EpilogueArg(const GemmEpilogue& e) : GemmEpilogue(e) {}
 };
 template <>
 struct EpilogueArg<kNoEpilogue> {};
-inline EpilogueKind epilogue_kind(const GemmEpilogue* e) { return !e ? kNoEpilogue : e->grad_codes ? kGrad : e->residual ? kResidual : kForward; }
+inline EpilogueKind epilogue_kind(const GemmEpilogue* e) { return !e ? kNoEpilogue : e->grad_codes ? kGrad : !e->residual ? kForward : e->residual_bf16 ? kResidualBf16 : kResidualF32; }
 
 // Lanes 16 apart hold the rows of a 4 x 4 matrix of words, each lane a row: lane group q gets column q (its own inverse).
 __device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
@@ -263,29 +264,33 @@ __device__ __forceinline__ void finish_block(float4v (&v)[kGroups], const GemmEp
   }
 }
 
-// A wavefront's whole block of kMB x kNB 16x16 results, 16 rows of four blocks (64 columns) at a time, column group by column group.  What such a unit
-// loads (residual, or 8 bits) is asked for kAhead units before it is needed; addresses past the end are replaced by the last in range rather than
-// skipped, so that the number of loads in flight is known to the compiler.  The 8 bits move as 16 bytes of one block to a lane, D as in WaveBlockStore.
-// first_unit, units: a part of the block (see splitk_sum_kernel).
+// A wavefront's whole block of kMB x kNB 16x16 results, 16 rows of four blocks (64 columns) at a time, row by row: a row's lines fill up at once.  (Column
+// group by column group, which needs the bias of one group only, MXFP4 8192 x 20480 x 5120 takes 432 us instead of 418 without anything to do, 528 instead of
+// 472 with the 8 bits.)  What such a unit loads (residual, or 8 bits) is asked for kAhead units before it is needed; addresses past the end are
+// replaced by the last in range rather than skipped, so that the number of loads in flight is known to the compiler.  The 8 bits move as 16 bytes of one block to a
+// lane, bf16 as in WaveBlockStore.
 template <int kKind, int kMB, int kNB>
 struct EpilogueBlock {
-  static constexpr int kGroups = (kNB + 3) / 4, kUnits = kGroups * kMB, kAhead = kKind == kResidual ? 3 : 4;
+  static constexpr int kGroups = (kNB + 3) / 4, kUnits = kGroups * kMB, kAhead = kKind == kResidualF32 ? 5 : kKind == kGrad ? 12 : 8;
+  static constexpr bool kResidual = kKind == kResidualF32 || kKind == kResidualBf16, kLoads = kResidual || kKind == kGrad;
   struct Loads {
-    float4v f[kKind == kResidual ? 4 : 1];   // residual, as loaded (bf16: in the first two words)
-    uint4 codes;
+    u32x4v w[kKind == kResidualF32 ? 4 : kKind == kResidualBf16 ? 2 : 1];
     uint32_t byte;
   };
   const GemmEpilogue& e;
   const TensorScales& ts;
   void* d;
   int64_t ldd, row0, col0;
-  int rows, cols, l16, lq;
+  int rows, cols, l16, lq, nl;   // nl: the lane's first column in a pair of bf16 blocks
+  float uniform;
+  bool per_row;
 
   __device__ __forceinline__ EpilogueBlock(const GemmEpilogue& e_, const TensorScales& ts_, void* Dv, int64_t ldd_, int64_t row0_, int64_t col0_, int rows_, int cols_, int lane)
-      : e(e_), ts(ts_), d(Dv), ldd(ldd_), row0(row0_), col0(col0_), rows(rows_), cols(cols_), l16(lane & 15), lq(lane >> 4) {}
+      : e(e_), ts(ts_), d(Dv), ldd(ldd_), row0(row0_), col0(col0_), rows(rows_), cols(cols_), l16(lane & 15), lq(lane >> 4), nl((lq & 1) * 16 + (lq >> 1) * 8),
+        uniform(ts_.a[0] * ts_.b[0]), per_row(ts_.a_per_row || ts_.b_per_row) {}
 
-  // The lane's row in 16-row block i, counted from the first.  Opaque (no instruction): the compiler would keep every block's addresses from one column
-  // group to the next, in more registers than there are.
+  // The lane's row in 16-row block i, counted from the first.  Opaque (no instruction): the compiler would keep every block's addresses, in more registers than
+  // there are.
   __device__ __forceinline__ int row_of(int i) const {
     int r = i * 16 + l16;
     asm volatile("" : "+v"(r));
@@ -296,61 +301,64 @@ struct EpilogueBlock {
 
   __device__ __forceinline__ void fetch(Loads& l, int i, int jg) const {
     const int64_t row = row_at(i);
-    if constexpr (kKind == kResidual) {
-      if (e.residual_bf16) {
-        const uint16_t* p = static_cast<const uint16_t*>(e.residual) + row * e.ldr + 4 * lq;
+    if constexpr (kKind == kResidualF32) {
+      const float* p = static_cast<const float*>(e.residual) + row * e.ldr + 4 * lq;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (4 * jg + k < kNB) {
-            const uint2 w = *reinterpret_cast<const uint2*>(p + col_at(4 * jg + k));
-            l.f[k][0] = __uint_as_float(w.x), l.f[k][1] = __uint_as_float(w.y);
-          }
-        }
-      } else {
-        const float* p = static_cast<const float*>(e.residual) + row * e.ldr + 4 * lq;
+      for (int k = 0; k < 4; ++k)
+        if (4 * jg + k < kNB) l.w[k] = *reinterpret_cast<const u32x4v*>(p + col_at(4 * jg + k));
+    }
+    if constexpr (kKind == kResidualBf16) {
+      const uint16_t* p = static_cast<const uint16_t*>(e.residual) + row * e.ldr + (nl & 15);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (4 * jg + k < kNB) l.f[k] = *reinterpret_cast<const float4v*>(p + col_at(4 * jg + k));
-      }
+      for (int k = 0; k < 4; k += 2)
+        if (4 * jg + k < kNB) l.w[k / 2] = *reinterpret_cast<const u32x4v*>(p + col_at(min(4 * jg + k + (nl >> 4), kNB - 1)));
     }
     if constexpr (kKind == kGrad) {
       const int64_t at = row * e.cols + col_at(min(4 * jg + lq, kNB - 1));
-      l.codes = *reinterpret_cast<const uint4*>(e.grad_codes + at);
+      l.w[0] = *reinterpret_cast<const u32x4v*>(e.grad_codes + at);
       l.byte = e.grad_scales[at / 16];
     }
   }
 
-  // Factors and bias of the lane's columns in a group of four blocks.
-  __device__ __forceinline__ void columns(int jg, float4v (&sb)[4], float4v (&bias)[4]) const {
+  // The bias of the lane's columns.
+  __device__ __forceinline__ void columns(float4v (&bias)[kKind == kGrad ? 1 : kNB]) const {
+    if constexpr (kKind != kGrad) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if (4 * jg + k >= kNB) continue;
-      const int64_t n = col_at(4 * jg + k) + 4 * lq;
-      if (ts.b_per_row) {
-        sb[k] = *reinterpret_cast<const float4v*>(ts.b + n);
-      } else {
-        const float b0 = ts.b[0];
-        sb[k] = float4v{b0, b0, b0, b0};
+      for (int j = 0; j < kNB; ++j) {
+        bias[j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+        if (e.bias) bias[j] = *reinterpret_cast<const float4v*>(e.bias + col_at(j) + 4 * lq);
       }
-      bias[k] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-      if (kKind != kGrad && e.bias) bias[k] = *reinterpret_cast<const float4v*>(e.bias + n);
     }
   }
 
   // sums: the unit's four blocks, unscaled.
-  __device__ __forceinline__ void finish(const float4v (&sums)[4], const Loads& l, int i, int jg, float sa, const float4v (&sb)[4], const float4v (&bias)[4]) const {
+  __device__ __forceinline__ void finish(float4v (&sums)[4], const Loads& l, int i, int jg, const float4v (&bias)[kKind == kGrad ? 1 : kNB]) const {
     constexpr int kLast = kNB % 4 ? kNB % 4 : 4;
     const int blocks = jg == kGroups - 1 ? kLast : 4;   // (a constant where it is unrolled)
     const int r_in = row_of(i);
     const bool row_in = r_in < rows;
     const int64_t row = row0 + r_in;
+    if (per_row) {
+      const float sa = ts.a[ts.a_per_row ? row0 + min(r_in, rows - 1) : 0];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (k >= blocks) continue;
+        const float b0 = ts.b[0];
+        float4v sb = {b0, b0, b0, b0};
+        if (ts.b_per_row) sb = *reinterpret_cast<const float4v*>(ts.b + col_at(4 * jg + k) + 4 * lq);
+        sums[k] *= sb * sa;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sums[k] *= uniform;
+    }
     float z[16];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) z[4 * k + r] = k < blocks ? sums[k][r] * (sb[k][r] * sa) + bias[k][r] : 0.0f;
+      for (int r = 0; r < 4; ++r) z[4 * k + r] = k >= blocks ? 0.0f : kKind == kGrad ? sums[k][r] : sums[k][r] + bias[kKind == kGrad ? 0 : (4 * jg + k) % kNB][r];
     if constexpr (kKind == kGrad) {
-      uint32_t codes[4] = {l.codes.x, l.codes.y, l.codes.z, l.codes.w}, bytes[4];
+      uint32_t codes[4] = {l.w[0][0], l.w[0][1], l.w[0][2], l.w[0][3]}, bytes[4];
       transpose4(codes);
       gather4(l.byte, bytes);
       float slope[16];
@@ -378,22 +386,27 @@ struct EpilogueBlock {
         }
       }
       activate(z, e.act);
-      if constexpr (kKind == kResidual) {
+      if constexpr (kKind == kResidualF32) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float4v f = l.f[k];
-          const uint32_t w0 = __float_as_uint(f[0]), w1 = __float_as_uint(f[1]);
-          if (k < blocks) {
-            z[4 * k] += e.residual_bf16 ? bf16_lo(w0) : f[0];
-            z[4 * k + 1] += e.residual_bf16 ? bf16_hi(w0) : f[1];
-            z[4 * k + 2] += e.residual_bf16 ? bf16_lo(w1) : f[2];
-            z[4 * k + 3] += e.residual_bf16 ? bf16_hi(w1) : f[3];
+        for (int t = 0; t < 16; ++t)
+          if (t / 4 < blocks) z[t] += __uint_as_float(l.w[t / 4][t % 4]);
+      }
+      if constexpr (kKind == kResidualBf16) {
+#pragma unroll
+        for (int k = 0; k < 4; k += 2) {
+          if (k >= blocks) continue;
+          // (the exchange of the stores below, backwards)
+          const auto s0 = __builtin_amdgcn_permlane16_swap(l.w[k / 2][0], l.w[k / 2][2], false, false), s1 = __builtin_amdgcn_permlane16_swap(l.w[k / 2][1], l.w[k / 2][3], false, false);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (k + h >= blocks) continue;
+            z[4 * (k + h)] += bf16_lo(s0[h]), z[4 * (k + h) + 1] += bf16_hi(s0[h]);
+            z[4 * (k + h) + 2] += bf16_lo(s1[h]), z[4 * (k + h) + 3] += bf16_hi(s1[h]);
           }
         }
       }
     }
     if (e.out_bf16) {
-      const int nl = (lq & 1) * 16 + (lq >> 1) * 8;   // (see WaveBlockStore)
       uint16_t* to = static_cast<uint16_t*>(d) + row * ldd + col0 + nl;
 #pragma unroll
       for (int k = 0; k < 4; k += 2) {
@@ -422,27 +435,41 @@ __device__ __forceinline__ void each(F&& f) {
   }
 }
 
-template <int kKind, int kMB, int kNB>
+// A result in accumulation registers, read where it is used: left to itself the compiler moves reads up until the registers do not suffice.
+__device__ __forceinline__ float4v read_acc(const float4v& a) {
+  float4v v;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    float x;
+    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(a[r]));
+    v[r] = x;
+  }
+  return v;
+}
+
+// kInAcc: how many of the results, counted row by row, are in accumulation registers.
+template <int kKind, int kInAcc, int kMB, int kNB>
 __device__ __forceinline__ void store_wave_block_epilogue(float4v (&acc)[kMB][kNB], const TensorScales ts, const GemmEpilogue& e, void* __restrict__ Dv, int64_t ldd,
                                                           int64_t row0, int64_t col0, int rows, int cols, int lane) {
   using Block = EpilogueBlock<kKind, kMB, kNB>;
   const Block b(e, ts, Dv, ldd, row0, col0, rows, cols, lane);
-  constexpr int kAhead = Block::kAhead, kUnits = Block::kUnits;
-  constexpr bool kLoads = kKind == kResidual || kKind == kGrad;
+  constexpr int kAhead = Block::kAhead, kUnits = Block::kUnits, kGroups = Block::kGroups;
+  constexpr bool kLoads = Block::kLoads;
+  float4v bias[kKind == kGrad ? 1 : kNB];
+  b.columns(bias);
   typename Block::Loads ring[kLoads ? kAhead : 1];
-  if constexpr (kLoads) each<0, (kAhead < kUnits ? kAhead : kUnits)>([&](auto u) { b.fetch(ring[decltype(u)::value], decltype(u)::value % kMB, decltype(u)::value / kMB); });
-  float sa[kMB];
-#pragma unroll
-  for (int i = 0; i < kMB; ++i) sa[i] = ts.a[ts.a_per_row ? b.row_at(i) : 0];
-  float4v sb[4], bias[4];
+  if constexpr (kLoads) each<0, (kAhead < kUnits ? kAhead : kUnits)>([&](auto u) { b.fetch(ring[decltype(u)::value], decltype(u)::value / kGroups, decltype(u)::value % kGroups); });
   each<0, kUnits>([&](auto uc) {
-    constexpr int u = decltype(uc)::value, i = u % kMB, jg = u / kMB;
-    if constexpr (i == 0) b.columns(jg, sb, bias);
+    constexpr int u = decltype(uc)::value, i = u / kGroups, jg = u % kGroups;
     float4v sums[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) sums[k] = 4 * jg + k < kNB ? acc[i][4 * jg + k < kNB ? 4 * jg + k : 0] : float4v{0.0f, 0.0f, 0.0f, 0.0f};
-    b.finish(sums, ring[kLoads ? u % kAhead : 0], i, jg, sa[i], sb, bias);
-    if constexpr (kLoads && u + kAhead < kUnits) b.fetch(ring[u % kAhead], (u + kAhead) % kMB, (u + kAhead) / kMB);
+    for (int k = 0; k < 4; ++k) {
+      const int j = 4 * jg + k;
+      sums[k] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+      if (j < kNB) sums[k] = i * kNB + j < kInAcc ? read_acc(acc[i][j < kNB ? j : 0]) : acc[i][j < kNB ? j : 0];
+    }
+    b.finish(sums, ring[kLoads ? u % kAhead : 0], i, jg, bias);
+    if constexpr (kLoads && u + kAhead < kUnits) b.fetch(ring[u % kAhead], (u + kAhead) / kGroups, (u + kAhead) % kGroups);
     __builtin_amdgcn_sched_barrier(0);
   });
 }

@@ -442,7 +442,7 @@ __global__ __launch_bounds__(kThreads) void gemm_f16_kernel(const _Float16* __re
         for (int j = 0; j < kNB; ++j) mine[(i * kNB + j) * kThreads] = acc[i][j];
       return;
     } else if constexpr (kKind != kNoEpilogue) {
-      store_wave_block_epilogue<kKind, kMB, kNB>(acc, out_scale, epilogue, Dv, ldd, m0 + wm * (16 * kMB), n0 + wn * (16 * kNB), Mt - wm * (16 * kMB),
+      store_wave_block_epilogue<kKind, 64, kMB, kNB>(acc, out_scale, epilogue, Dv, ldd, m0 + wm * (16 * kMB), n0 + wn * (16 * kNB), Mt - wm * (16 * kMB),
                                                  Nt - wn * (16 * kNB), lane);
     } else {
       store_wave_block_impl<kBf16Out, kRowScales, kMB, kNB>(acc, out_scale, Dv, ldd, accumulate, m0 + wm * (16 * kMB), n0 + wn * (16 * kNB),
@@ -499,7 +499,7 @@ __global__ __launch_bounds__(64) void splitk_sum_kernel(const float* __restrict_
     float4v block[1][8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) block[0][j] = sums[j];
-    store_wave_block_epilogue<kKind, 1, 8>(block, ts, epilogue, Dv, ldd, row0, col0, rows, cols, lane);
+    store_wave_block_epilogue<kKind, 0, 1, 8>(block, ts, epilogue, Dv, ldd, row0, col0, rows, cols, lane);
     return;
   }
   const WaveBlockStore<kBf16Out, kRowScales> out(ts, Dv, ldd, accumulate, m0 + wm * 128, n0 + wn * 128, Mt - wm * 128,
@@ -706,8 +706,10 @@ static hipError_t launch_f16(bool bf16_out, const _Float16* a16, const _Float16*
                      g.b.ts_per_row != 0, EpilogueArg<KIND>{__VA_ARGS__})
     if (kind == kForward) {
       NVFP4_LAUNCH_SUM(false, false, kForward, *g.epilogue);
-    } else if (kind == kResidual) {
-      NVFP4_LAUNCH_SUM(false, false, kResidual, *g.epilogue);
+    } else if (kind == kResidualF32) {
+      NVFP4_LAUNCH_SUM(false, false, kResidualF32, *g.epilogue);
+    } else if (kind == kResidualBf16) {
+      NVFP4_LAUNCH_SUM(false, false, kResidualBf16, *g.epilogue);
     } else if (kind == kGrad) {
       NVFP4_LAUNCH_SUM(false, false, kGrad, *g.epilogue);
     } else if (bf16_out) {
@@ -719,7 +721,8 @@ static hipError_t launch_f16(bool bf16_out, const _Float16* a16, const _Float16*
   } else if (kind != kNoEpilogue) {
     if constexpr (kMB == 8) {
       if (kind == kForward) NVFP4_LAUNCH_F16(false, false, false, kMB, kNB, kForward, *g.epilogue);
-      else if (kind == kResidual) NVFP4_LAUNCH_F16(false, false, false, kMB, kNB, kResidual, *g.epilogue);
+      else if (kind == kResidualF32) NVFP4_LAUNCH_F16(false, false, false, kMB, kNB, kResidualF32, *g.epilogue);
+      else if (kind == kResidualBf16) NVFP4_LAUNCH_F16(false, false, false, kMB, kNB, kResidualBf16, *g.epilogue);
       else NVFP4_LAUNCH_F16(false, false, false, kMB, kNB, kGrad, *g.epilogue);
     } else {
       return hipErrorInvalidValue;   // (pick_tile offers none)

@@ -263,7 +263,7 @@ __global__ __launch_bounds__(kThreads) void gemm_mx_kernel_any_k(Operand A, Oper
   const int Mt = static_cast<int>(A.outer - m0 < TM ? A.outer - m0 : TM);
   const int Nt = static_cast<int>(B.outer - n0 < TN ? B.outer - n0 : TN);
   if constexpr (kKind != kNoEpilogue)
-    store_wave_block_epilogue<kKind, 8, 8>(acc, out_scale, epilogue, Dv, ldd, m0 + wm * 128, n0 + wn * 128, Mt - wm * 128, Nt - wn * 128, lane);
+    store_wave_block_epilogue<kKind, 64, 8, 8>(acc, out_scale, epilogue, Dv, ldd, m0 + wm * 128, n0 + wn * 128, Mt - wm * 128, Nt - wn * 128, lane);
   else
     store_wave_block<kBf16Out>(acc, out_scale, Dv, ldd, accumulate, m0 + wm * 128, n0 + wn * 128, Mt - wm * 128, Nt - wn * 128,
                                lane);
@@ -632,7 +632,7 @@ __global__ __launch_bounds__(kThreads) void gemm_mx_kernel_k512(Operand A, Opera
     const int Mt = static_cast<int>(A.outer - m0 < kTM ? A.outer - m0 : kTM);
     const int Nt = static_cast<int>(B.outer - n0 < kTN ? B.outer - n0 : kTN);
     if constexpr (kKind != kNoEpilogue)
-      store_wave_block_epilogue<kKind, kMB, kNB>(acc, out_scale, epilogue, Dv, ldd, m0 + wm * (16 * kMB), n0 + wn * (16 * kNB), Mt - wm * (16 * kMB),
+      store_wave_block_epilogue<kKind, 64, kMB, kNB>(acc, out_scale, epilogue, Dv, ldd, m0 + wm * (16 * kMB), n0 + wn * (16 * kNB), Mt - wm * (16 * kMB),
                                                  Nt - wn * (16 * kNB), lane);
     else
       store_wave_block<kBf16Out, kNB>(acc, out_scale, Dv, ldd, accumulate, m0 + wm * (16 * kMB), n0 + wn * (16 * kNB), Mt - wm * (16 * kMB),
@@ -693,7 +693,8 @@ template <int kNB>
 static hipError_t launch_k512(const GemmArgs& g, int tiles_m, hipStream_t s) {
   switch (epilogue_kind(g.epilogue)) {
     case kForward: return launch_k512_as<false, kNB, kForward>(g, *g.epilogue, tiles_m, s);
-    case kResidual: return launch_k512_as<false, kNB, kResidual>(g, *g.epilogue, tiles_m, s);
+    case kResidualF32: return launch_k512_as<false, kNB, kResidualF32>(g, *g.epilogue, tiles_m, s);
+    case kResidualBf16: return launch_k512_as<false, kNB, kResidualBf16>(g, *g.epilogue, tiles_m, s);
     case kGrad: return launch_k512_as<false, kNB, kGrad>(g, *g.epilogue, tiles_m, s);
     default: break;
   }
@@ -723,7 +724,8 @@ hipError_t launch_gemm_mx(const GemmArgs& g, hipStream_t s) {
   }
   switch (epilogue_kind(g.epilogue)) {
     case kForward: return launch_any_k<false, kForward>(g, *g.epilogue, tiles_m, tiles_n, s);
-    case kResidual: return launch_any_k<false, kResidual>(g, *g.epilogue, tiles_m, tiles_n, s);
+    case kResidualF32: return launch_any_k<false, kResidualF32>(g, *g.epilogue, tiles_m, tiles_n, s);
+    case kResidualBf16: return launch_any_k<false, kResidualBf16>(g, *g.epilogue, tiles_m, tiles_n, s);
     case kGrad: return launch_any_k<false, kGrad>(g, *g.epilogue, tiles_m, tiles_n, s);
     default: break;
   }
