@@ -88,15 +88,21 @@ __device__ __forceinline__ void checkpoint_values4(uint32_t codes, uint32_t byte
 // Numbers of include/nvfp4.h's NVFP4_ACT_*.
 enum { kActNone = 0, kActRelu2 = 1, kActGelu = 2, kActSilu = 3 };
 
-// s(p) and s (1 - s) from q = exp(-|p|): 1 / (1 + q), or q / (1 + q) below zero, and q / (1 + q)^2.  q is a square because the exponential instruction has no
-// subnormal results and a product has: nothing is flushed to zero before it is below the smallest number.
+// The argument p = z (c1 + c3 z^2) times log2(e) / 2: with w = 2^-|that|, q = w^2 = exp(-|p|), and s = 1 / (1 + q), or q / (1 + q) below zero.  (A square, because the
+// exponential instruction has no subnormal results and a product has: nothing is flushed to zero before it is below the smallest number.)
 struct Logistic {
-  float s, t;
+  float p, q, r;   // r = 1 / (1 + q)
+  __device__ __forceinline__ Logistic(float z, float c1, float c3) {
+    p = z * __builtin_fmaf(c3 * z, z, c1);
+    const float w = __builtin_amdgcn_exp2f(-__builtin_fabsf(p));
+    q = w * w;
+    r = __builtin_amdgcn_rcpf(1.0f + q);
+  }
+  __device__ __forceinline__ float s() const { return p < 0.0f ? q * r : r; }
 };
-__device__ __forceinline__ Logistic logistic(float p) {
-  const float w = __builtin_amdgcn_exp2f(__builtin_fabsf(p) * -0.72134752044448170f), q = w * w, r = __builtin_amdgcn_rcpf(1.0f + q), qr = q * r;
-  return {p < 0.0f ? qr : r, qr * r};
-}
+constexpr float kHalfLog2E = 0.72134752044448170f;
+__device__ __forceinline__ float logistic_c1(int act) { return act == kActSilu ? kHalfLog2E : 1.5957691216057308f * kHalfLog2E; }
+__device__ __forceinline__ float logistic_c3(int act) { return act == kActSilu ? 0.0f : 0.07135481282988394f * kHalfLog2E; }
 
 template <int kN>
 __device__ __forceinline__ void activate(float (&v)[kN], int act) {
@@ -107,9 +113,9 @@ __device__ __forceinline__ void activate(float (&v)[kN], int act) {
       v[i] = r * r;
     }
   } else if (act != kActNone) {
-    const float c1 = act == kActSilu ? 1.0f : 1.5957691216057308f, c3 = act == kActSilu ? 0.0f : 0.07135481282988394f;
+    const float c1 = logistic_c1(act), c3 = logistic_c3(act);
 #pragma unroll
-    for (int i = 0; i < kN; ++i) v[i] *= logistic(v[i] * __builtin_fmaf(c3 * v[i], v[i], c1)).s;
+    for (int i = 0; i < kN; ++i) v[i] *= Logistic(v[i], c1, c3).s();
   }
 }
 
@@ -123,12 +129,13 @@ __device__ __forceinline__ void activation_slope(float (&v)[kN], int act) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) v[i] = 1.0f;
   } else {
-    const float c1 = act == kActSilu ? 1.0f : 1.5957691216057308f, c3 = act == kActSilu ? 0.0f : 0.07135481282988394f;
+    const float c1 = logistic_c1(act), c3 = logistic_c3(act), d1 = c1 / kHalfLog2E, d3 = 3.0f * c3 / kHalfLog2E;
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const float z = v[i];
-      const Logistic l = logistic(z * __builtin_fmaf(c3 * z, z, c1));
-      v[i] = l.s + (l.t > 0.0f ? z * l.t * __builtin_fmaf(3.0f * c3 * z, z, c1) : 0.0f);   // (far out t is 0 and the polynomial infinite)
+      const Logistic l(z, c1, c3);
+      const float qr = l.q * l.r, t = qr * l.r;   // s (1 - s)
+      v[i] = (l.p < 0.0f ? qr : l.r) + (t > 0.0f ? z * t * __builtin_fmaf(d3 * z, z, d1) : 0.0f);   // (far out t is 0 and the polynomial infinite)
     }
   }
 }

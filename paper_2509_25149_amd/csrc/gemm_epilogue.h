@@ -278,45 +278,49 @@ struct EpilogueBlock {
     uint32_t byte;
   };
   const GemmEpilogue& e;
-  const TensorScales& ts;
-  void* d;
+  const float *ts_a, *ts_b;
   int64_t ldd, row0, col0;
   int rows, cols, l16, lq, nl;   // nl: the lane's first column in a pair of bf16 blocks
-  float uniform;
-  bool per_row;
+  bool a_per_row, b_per_row;
+  // The lane's place in the block's first 16 rows; 16-row block i is i * 16 leading dimensions on, the same for all lanes.
+  char* d;
+  const char* residual;
+  uint8_t *codes, *scales;       // of block lq
 
-  __device__ __forceinline__ EpilogueBlock(const GemmEpilogue& e_, const TensorScales& ts_, void* Dv, int64_t ldd_, int64_t row0_, int64_t col0_, int rows_, int cols_, int lane)
-      : e(e_), ts(ts_), d(Dv), ldd(ldd_), row0(row0_), col0(col0_), rows(rows_), cols(cols_), l16(lane & 15), lq(lane >> 4), nl((lq & 1) * 16 + (lq >> 1) * 8),
-        uniform(ts_.a[0] * ts_.b[0]), per_row(ts_.a_per_row || ts_.b_per_row) {}
-
-  // The lane's row in 16-row block i, counted from the first.  Opaque (no instruction): the compiler would keep every block's addresses, in more registers than
-  // there are.
-  __device__ __forceinline__ int row_of(int i) const {
-    int r = i * 16 + l16;
-    asm volatile("" : "+v"(r));
-    return r;
+  __device__ __forceinline__ EpilogueBlock(const GemmEpilogue& e_, const TensorScales& ts, void* Dv, int64_t ldd_, int64_t row0_, int64_t col0_, int rows_, int cols_, int lane)
+      : e(e_), ts_a(ts.a), ts_b(ts.b), ldd(ldd_), row0(row0_), col0(col0_), rows(rows_), cols(cols_), l16(lane & 15), lq(lane >> 4), nl((lq & 1) * 16 + (lq >> 1) * 8),
+        a_per_row(ts.a_per_row), b_per_row(ts.b_per_row) {
+    const int64_t row = row0 + l16;
+    d = static_cast<char*>(Dv) + (e.out_bf16 ? (row * ldd + col0 + nl) * 2 : (row * ldd + col0 + 4 * lq) * 4);
+    if constexpr (kKind == kResidualF32) residual = static_cast<const char*>(e.residual) + (row * e.ldr + col0 + 4 * lq) * 4;
+    if constexpr (kKind == kResidualBf16) residual = static_cast<const char*>(e.residual) + (row * e.ldr + col0 + (nl & 15)) * 2;
+    const int64_t at = row * e.cols + col0;
+    codes = (kKind == kGrad ? const_cast<uint8_t*>(e.grad_codes) : e.keep_codes) + at;
+    scales = (kKind == kGrad ? const_cast<uint8_t*>(e.grad_scales) : e.keep_scales) + at / 16;
   }
-  __device__ __forceinline__ int64_t row_at(int i) const { return row0 + min(row_of(i), rows - 1); }
-  __device__ __forceinline__ int64_t col_at(int j) const { return col0 + min(16 * j, cols - 16); }   // first column of block j
+
+  // 16-row block i and column block j, or the last that exist (rows and columns come in multiples of 16; a block past the end may start behind them all).
+  __device__ __forceinline__ int row_block(int i) const { return min(i, (rows >> 4) - 1); }
+  __device__ __forceinline__ int col_block(int j) const { return min(j, (cols >> 4) - 1); }
 
   __device__ __forceinline__ void fetch(Loads& l, int i, int jg) const {
-    const int64_t row = row_at(i);
+    const int64_t down = static_cast<int64_t>(row_block(i)) * 16;
     if constexpr (kKind == kResidualF32) {
-      const float* p = static_cast<const float*>(e.residual) + row * e.ldr + 4 * lq;
+      const char* p = residual + down * e.ldr * 4;
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (4 * jg + k < kNB) l.w[k] = *reinterpret_cast<const u32x4v*>(p + col_at(4 * jg + k));
+        if (4 * jg + k < kNB) l.w[k] = *reinterpret_cast<const u32x4v*>(p + col_block(4 * jg + k) * 64);
     }
     if constexpr (kKind == kResidualBf16) {
-      const uint16_t* p = static_cast<const uint16_t*>(e.residual) + row * e.ldr + (nl & 15);
+      const char* p = residual + down * e.ldr * 2;
 #pragma unroll
       for (int k = 0; k < 4; k += 2)
-        if (4 * jg + k < kNB) l.w[k / 2] = *reinterpret_cast<const u32x4v*>(p + col_at(min(4 * jg + k + (nl >> 4), kNB - 1)));
+        if (4 * jg + k < kNB) l.w[k / 2] = *reinterpret_cast<const u32x4v*>(p + col_block(min(4 * jg + k + (nl >> 4), kNB - 1)) * 32);
     }
     if constexpr (kKind == kGrad) {
-      const int64_t at = row * e.cols + col_at(min(4 * jg + lq, kNB - 1));
-      l.w[0] = *reinterpret_cast<const u32x4v*>(e.grad_codes + at);
-      l.byte = e.grad_scales[at / 16];
+      const int j = col_block(min(4 * jg + lq, kNB - 1));
+      l.w[0] = *reinterpret_cast<const u32x4v*>(codes + down * e.cols + j * 16);
+      l.byte = scales[down * (e.cols >> 4) + j];
     }
   }
 
@@ -326,102 +330,99 @@ struct EpilogueBlock {
 #pragma unroll
       for (int j = 0; j < kNB; ++j) {
         bias[j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-        if (e.bias) bias[j] = *reinterpret_cast<const float4v*>(e.bias + col_at(j) + 4 * lq);
+        if (e.bias) bias[j] = *reinterpret_cast<const float4v*>(e.bias + col0 + col_block(j) * 16 + 4 * lq);
       }
     }
   }
 
-  // sums: the unit's four blocks, unscaled.
-  __device__ __forceinline__ void finish(float4v (&sums)[4], const Loads& l, int i, int jg, const float4v (&bias)[kKind == kGrad ? 1 : kNB]) const {
-    constexpr int kLast = kNB % 4 ? kNB % 4 : 4;
-    const int blocks = jg == kGroups - 1 ? kLast : 4;   // (a constant where it is unrolled)
-    const int r_in = row_of(i);
-    const bool row_in = r_in < rows;
-    const int64_t row = row0 + r_in;
-    if (per_row) {
-      const float sa = ts.a[ts.a_per_row ? row0 + min(r_in, rows - 1) : 0];
+  // sums: the unit's blocks, unscaled: four of them, or what is left at the end of a row.  uniform: the operands' factor where neither has one per row.
+  template <int kBlocks>
+  __device__ __forceinline__ void finish(float4v (&sums)[kBlocks], const Loads& l, int i, int jg, float uniform, const float4v (&bias)[kKind == kGrad ? 1 : kNB]) const {
+    const bool row_in = i * 16 < rows;
+    const int64_t down = static_cast<int64_t>(i) * 16;
+    if (a_per_row || b_per_row) {
+      const float sa = ts_a[a_per_row ? row0 + row_block(i) * 16 + l16 : 0];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (k >= blocks) continue;
-        const float b0 = ts.b[0];
+      for (int k = 0; k < kBlocks; ++k) {
+        const float b0 = ts_b[0];
         float4v sb = {b0, b0, b0, b0};
-        if (ts.b_per_row) sb = *reinterpret_cast<const float4v*>(ts.b + col_at(4 * jg + k) + 4 * lq);
+        if (b_per_row) sb = *reinterpret_cast<const float4v*>(ts_b + col0 + col_block(4 * jg + k) * 16 + 4 * lq);
         sums[k] *= sb * sa;
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) sums[k] *= uniform;
+      for (int k = 0; k < kBlocks; ++k) sums[k] *= uniform;
     }
-    float z[16];
+    float z[4 * kBlocks];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) z[4 * k + r] = k >= blocks ? 0.0f : kKind == kGrad ? sums[k][r] : sums[k][r] + bias[kKind == kGrad ? 0 : (4 * jg + k) % kNB][r];
+    for (int t = 0; t < 4 * kBlocks; ++t) z[t] = sums[t / 4][t % 4] + (kKind == kGrad ? 0.0f : bias[kKind == kGrad ? 0 : 4 * jg + t / 4][t % 4]);
     if constexpr (kKind == kGrad) {
-      uint32_t codes[4] = {l.w[0][0], l.w[0][1], l.w[0][2], l.w[0][3]}, bytes[4];
-      transpose4(codes);
+      uint32_t codes4[4] = {l.w[0][0], l.w[0][1], l.w[0][2], l.w[0][3]}, bytes[4];
+      transpose4(codes4);
       gather4(l.byte, bytes);
-      float slope[16];
+      float slope[4 * kBlocks];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) checkpoint_values4(codes[k], bytes[k], slope + 4 * k);
+      for (int k = 0; k < kBlocks; ++k) checkpoint_values4(codes4[k], bytes[k], slope + 4 * k);
       activation_slope(slope, e.act);
 #pragma unroll
-      for (int t = 0; t < 16; ++t) z[t] *= slope[t];
+      for (int t = 0; t < 4 * kBlocks; ++t) z[t] *= slope[t];
     } else {
       if (e.keep_codes) {
         uint32_t m[4], w[4], bytes[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) m[k] = max(max(magnitude(z[4 * k]), magnitude(z[4 * k + 1])), max(magnitude(z[4 * k + 2]), magnitude(z[4 * k + 3])));
+        for (int k = 0; k < 4; ++k) {
+          const int t = k < kBlocks ? 4 * k : 0;
+          m[k] = k < kBlocks ? max(max(magnitude(z[t]), magnitude(z[t + 1])), max(magnitude(z[t + 2]), magnitude(z[t + 3]))) : 0u;
+        }
         transpose4(m);
         const uint32_t byte = checkpoint_scale(max(max(m[0], m[1]), max(m[2], m[3])));   // of block 4 jg + lq
         gather4(byte, bytes);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = checkpoint_codes4(z[4 * k], z[4 * k + 1], z[4 * k + 2], z[4 * k + 3], bytes[k]);
+        for (int k = 0; k < 4; ++k) {
+          const int t = k < kBlocks ? 4 * k : 0;
+          w[k] = k < kBlocks ? checkpoint_codes4(z[t], z[t + 1], z[t + 2], z[t + 3], bytes[k]) : 0u;
+        }
         transpose4(w);
         const int c = 16 * (4 * jg + lq);
-        if (row_in && lq < blocks && c < cols) {
-          const int64_t at = row * e.cols + col0 + c;
-          *reinterpret_cast<u32x4v*>(e.keep_codes + at) = u32x4v{w[0], w[1], w[2], w[3]};
-          e.keep_scales[at / 16] = static_cast<uint8_t>(byte);
+        if (row_in && lq < kBlocks && c < cols) {
+          *reinterpret_cast<u32x4v*>(codes + down * e.cols + c) = u32x4v{w[0], w[1], w[2], w[3]};
+          scales[down * (e.cols >> 4) + (c >> 4)] = static_cast<uint8_t>(byte);
         }
       }
       activate(z, e.act);
       if constexpr (kKind == kResidualF32) {
 #pragma unroll
-        for (int t = 0; t < 16; ++t)
-          if (t / 4 < blocks) z[t] += __uint_as_float(l.w[t / 4][t % 4]);
+        for (int t = 0; t < 4 * kBlocks; ++t) z[t] += __uint_as_float(l.w[t / 4][t % 4]);
       }
       if constexpr (kKind == kResidualBf16) {
 #pragma unroll
-        for (int k = 0; k < 4; k += 2) {
-          if (k >= blocks) continue;
+        for (int k = 0; k < kBlocks; ++k) {
           // (the exchange of the stores below, backwards)
-          const auto s0 = __builtin_amdgcn_permlane16_swap(l.w[k / 2][0], l.w[k / 2][2], false, false), s1 = __builtin_amdgcn_permlane16_swap(l.w[k / 2][1], l.w[k / 2][3], false, false);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (k + h >= blocks) continue;
-            z[4 * (k + h)] += bf16_lo(s0[h]), z[4 * (k + h) + 1] += bf16_hi(s0[h]);
-            z[4 * (k + h) + 2] += bf16_lo(s1[h]), z[4 * (k + h) + 3] += bf16_hi(s1[h]);
-          }
+          const u32x4v p = l.w[k / 2];
+          const auto s0 = __builtin_amdgcn_permlane16_swap(p[0], p[2], false, false), s1 = __builtin_amdgcn_permlane16_swap(p[1], p[3], false, false);
+          z[4 * k] += bf16_lo(s0[k % 2]), z[4 * k + 1] += bf16_hi(s0[k % 2]);
+          z[4 * k + 2] += bf16_lo(s1[k % 2]), z[4 * k + 3] += bf16_hi(s1[k % 2]);
         }
       }
     }
     if (e.out_bf16) {
-      uint16_t* to = static_cast<uint16_t*>(d) + row * ldd + col0 + nl;
+      uint16_t* to = reinterpret_cast<uint16_t*>(d) + down * ldd;
 #pragma unroll
-      for (int k = 0; k < 4; k += 2) {
-        if (k >= blocks) continue;
-        const auto s0 = __builtin_amdgcn_permlane16_swap(f32x2_to_bf16(z[4 * k], z[4 * k + 1]), f32x2_to_bf16(z[4 * k + 4], z[4 * k + 5]), false, false);
-        const auto s1 = __builtin_amdgcn_permlane16_swap(f32x2_to_bf16(z[4 * k + 2], z[4 * k + 3]), f32x2_to_bf16(z[4 * k + 6], z[4 * k + 7]), false, false);
+      for (int k = 0; k < kBlocks; k += 2) {
+        constexpr int kEnd = 4 * kBlocks;
+        const uint32_t a0 = f32x2_to_bf16(z[4 * k], z[4 * k + 1]), a1 = f32x2_to_bf16(z[4 * k + 2], z[4 * k + 3]);
+        const uint32_t b0 = 4 * k + 4 < kEnd ? f32x2_to_bf16(z[(4 * k + 4) % kEnd], z[(4 * k + 5) % kEnd]) : 0u;
+        const uint32_t b1 = 4 * k + 4 < kEnd ? f32x2_to_bf16(z[(4 * k + 6) % kEnd], z[(4 * k + 7) % kEnd]) : 0u;
+        const auto s0 = __builtin_amdgcn_permlane16_swap(a0, b0, false, false), s1 = __builtin_amdgcn_permlane16_swap(a1, b1, false, false);
         const int c = 16 * (4 * jg + k);
-        if (row_in && c + nl < cols && (k + 1 < blocks || nl < 16)) *reinterpret_cast<u32x4v*>(to + c) = u32x4v{s0[0], s1[0], s0[1], s1[1]};
+        if (row_in && c + nl < cols && (k + 1 < kBlocks || nl < 16)) *reinterpret_cast<u32x4v*>(to + c) = u32x4v{s0[0], s1[0], s0[1], s1[1]};
       }
     } else {
-      float* to = static_cast<float*>(d) + row * ldd + col0 + 4 * lq;
+      float* to = reinterpret_cast<float*>(d) + down * ldd;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < kBlocks; ++k) {
         const int c = 16 * (4 * jg + k);
-        if (k < blocks && row_in && c < cols) *reinterpret_cast<float4v*>(to + c) = float4v{z[4 * k], z[4 * k + 1], z[4 * k + 2], z[4 * k + 3]};
+        if (row_in && c < cols) *reinterpret_cast<float4v*>(to + c) = float4v{z[4 * k], z[4 * k + 1], z[4 * k + 2], z[4 * k + 3]};
       }
     }
   }
@@ -449,26 +450,23 @@ __device__ __forceinline__ float4v read_acc(const float4v& a) {
 
 // kInAcc: how many of the results, counted row by row, are in accumulation registers.
 template <int kKind, int kInAcc, int kMB, int kNB>
-__device__ __forceinline__ void store_wave_block_epilogue(float4v (&acc)[kMB][kNB], const TensorScales ts, const GemmEpilogue& e, void* __restrict__ Dv, int64_t ldd,
+__device__ __forceinline__ void store_wave_block_epilogue(float4v (&acc)[kMB][kNB], const TensorScales& ts, const GemmEpilogue& e, void* __restrict__ Dv, int64_t ldd,
                                                           int64_t row0, int64_t col0, int rows, int cols, int lane) {
   using Block = EpilogueBlock<kKind, kMB, kNB>;
   const Block b(e, ts, Dv, ldd, row0, col0, rows, cols, lane);
   constexpr int kAhead = Block::kAhead, kUnits = Block::kUnits, kGroups = Block::kGroups;
   constexpr bool kLoads = Block::kLoads;
+  const float uniform = ts.a[0] * ts.b[0];
   float4v bias[kKind == kGrad ? 1 : kNB];
   b.columns(bias);
   typename Block::Loads ring[kLoads ? kAhead : 1];
   if constexpr (kLoads) each<0, (kAhead < kUnits ? kAhead : kUnits)>([&](auto u) { b.fetch(ring[decltype(u)::value], decltype(u)::value / kGroups, decltype(u)::value % kGroups); });
   each<0, kUnits>([&](auto uc) {
-    constexpr int u = decltype(uc)::value, i = u / kGroups, jg = u % kGroups;
-    float4v sums[4];
+    constexpr int u = decltype(uc)::value, i = u / kGroups, jg = u % kGroups, kBlocks = 4 * jg + 4 <= kNB ? 4 : kNB - 4 * jg;
+    float4v sums[kBlocks];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int j = 4 * jg + k;
-      sums[k] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-      if (j < kNB) sums[k] = i * kNB + j < kInAcc ? read_acc(acc[i][j < kNB ? j : 0]) : acc[i][j < kNB ? j : 0];
-    }
-    b.finish(sums, ring[kLoads ? u % kAhead : 0], i, jg, bias);
+    for (int k = 0; k < kBlocks; ++k) sums[k] = i * kNB + 4 * jg + k < kInAcc ? read_acc(acc[i][4 * jg + k]) : acc[i][4 * jg + k];
+    b.template finish<kBlocks>(sums, ring[kLoads ? u % kAhead : 0], i, jg, uniform, bias);
     if constexpr (kLoads && u + kAhead < kUnits) b.fetch(ring[u % kAhead], (u + kAhead) / kGroups, (u + kAhead) % kGroups);
     __builtin_amdgcn_sched_barrier(0);
   });
