@@ -493,8 +493,8 @@ namespace {
 
 bool element_type(int t) { return t == NVFP4_OUT_F32 || t == NVFP4_OUT_BF16; }
 bool activation(int a) { return a >= NVFP4_ACT_NONE && a <= NVFP4_ACT_SILU; }
-// (the kernels number the rows' workgroups with 31 bits)
-bool good_shape(int64_t rows, int64_t cols) { return rows >= 0 && rows <= 0x7fffffff && cols > 0 && cols <= 0x7fffffff && cols % 16 == 0; }
+// (the kernels number the rows' workgroups with 31 bits, and the columns' threads, four to a column, with 32)
+bool good_shape(int64_t rows, int64_t cols) { return rows >= 0 && rows <= 0x7fffffff && cols > 0 && cols < 0x40000000 && cols % 16 == 0; }
 bool good_ld(int64_t ld, int64_t cols) { return ld >= cols && ld % 8 == 0; }
 constexpr int64_t kMostNormCols = 32768;
 

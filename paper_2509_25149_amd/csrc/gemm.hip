@@ -112,11 +112,16 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(Operand A, Operand B
   for (int i = 0; i < 2; ++i) {
     const int m = wm * 64 + i * 32 + l32;
     if constexpr (kKind != kNoEpilogue) {
+      const int first = (lane >> 5) * 4;
+      EpilogueOfBlock<2, true> loads[4];
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        if (wn * 64 + b * 16 < N) loads[b].fetch(epilogue, m0 + m, n0 + wn * 64 + b * 16, first, m < M);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
 #pragma unroll
         for (int q = 0; q < 4; q += 2) {   // a 16-column block
-          const int n = wn * 64 + j * 32 + q * 8, first = (lane >> 5) * 4;
+          const int n = wn * 64 + j * 32 + q * 8;
           if (n >= N) continue;            // (alike in all lanes)
           float4v v[2];
 #pragma unroll
@@ -125,7 +130,7 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(Operand A, Operand B
 #pragma unroll
             for (int t = 0; t < 4; ++t) v[g][t] = acc[i][j][(q + g) * 4 + t] * sc[t];
           }
-          finish_block<2>(v, epilogue, Dv, ldd, m0 + m, n0 + n, first, m < M);
+          loads[j * 2 + q / 2].finish(v, epilogue, Dv, ldd, m0 + m, n0 + n, first, m < M);
         }
       }
       continue;
@@ -325,14 +330,20 @@ __global__ __launch_bounds__(kBigThreads) void gemm_kernel_256(Operand A, Operan
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int m = wm * 128 + i * 16 + l16;
+    EpilogueOfBlock<1, true> loads[kKind != kNoEpilogue ? 4 : 1];
+    if constexpr (kKind != kNoEpilogue) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (m < M && wn * 64 + j * 16 < N) loads[j].fetch(epilogue, m0 + m, n0 + wn * 64 + j * 16, lq * 4, true);
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int n = wn * 64 + j * 16 + lq * 4;
       if (m < M && n < N) {  // N is a multiple of 16, so the 4 columns are in or out together
         float4v v = acc[i][j] * scale4(ts, out_scale, vec, true, m0 + m, n0 + n);
         if constexpr (kKind != kNoEpilogue) {   // (rows and columns come in multiples of 16: all lanes are here)
-          float4v block[1] = {v};
-          finish_block<1>(block, epilogue, Dv, ldd, m0 + m, n0 + n - lq * 4, lq * 4, true);
+          const float4v block[1] = {v};
+          loads[kKind != kNoEpilogue ? j : 0].finish(block, epilogue, Dv, ldd, m0 + m, n0 + n - lq * 4, lq * 4, true);
         } else if (kBf16Out) {
           uint16_t* d = static_cast<uint16_t*>(Dv) + (m0 + m) * ldd + n0 + n;
           uint2 o;

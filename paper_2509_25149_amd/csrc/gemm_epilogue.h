@@ -210,59 +210,88 @@ __device__ __forceinline__ uint32_t max_over_groups(uint32_t v) {
   return max_over_halves(max(a[0], a[1]));
 }
 
-__device__ __forceinline__ float4v load4(const void* base, bool bf16, int64_t at) {
-  if (!bf16) return *reinterpret_cast<const float4v*>(static_cast<const float*>(base) + at);
-  const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + at);
-  return float4v{bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
-}
-
 // One 16-column block, for the kernels that store block by block: the lane holds kGroups groups of four columns of row m, n0 + first + 8 g .. + 3 (one
 // group for 16x16 results, first = 4 (lane >> 4); two for 32x32, first = 4 (lane >> 5)).  The lanes that share a row's block come together; `in`: the row
-// exists.  Stores D too.
-template <int kGroups>
-__device__ __forceinline__ void finish_block(float4v (&v)[kGroups], const GemmEpilogue& e, void* __restrict__ Dv, int64_t ldd, int64_t m, int64_t n0, int first, bool in) {
-  float z[kGroups * 4];
-#pragma unroll
-  for (int g = 0; g < kGroups; ++g) {
-    float4v b = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (e.bias) b = *reinterpret_cast<const float4v*>(e.bias + n0 + first + 8 * g);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) z[4 * g + r] = v[g][r] + b[r];
-  }
-  const int64_t at = m * e.cols + n0;
-  if (e.grad_codes) {
-    float slope[kGroups * 4];
-    const uint32_t byte = in ? e.grad_scales[at / 16] : 0u;
+// exists.  fetch() what is added or multiplied, of several blocks before the first is finished; finish() stores D too.  kLoads: whether there can be a residual
+// or a derivative.
+template <int kGroups, bool kLoads>
+struct EpilogueOfBlock {
+  float4v bias[kGroups];
+  u32x4v residual[kGroups];   // as loaded (bf16: in the first two words)
+  uint32_t codes[kGroups], byte;
+
+  __device__ __forceinline__ void fetch(const GemmEpilogue& e, int64_t m, int64_t n0, int first, bool in) {
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
-      const uint32_t codes = in ? *reinterpret_cast<const uint32_t*>(e.grad_codes + at + first + 8 * g) : 0u;
-      checkpoint_values4(codes, byte, slope + 4 * g);
+      bias[g] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+      codes[g] = 0u;
     }
-    activation_slope(slope, e.act);
+    byte = 0u;
+    if (e.bias) {
 #pragma unroll
-    for (int i = 0; i < kGroups * 4; ++i) z[i] *= slope[i];
-  } else {
-    if (e.keep_codes) {
-      const uint32_t byte = checkpoint_scale(kGroups == 1 ? max_over_groups(max_magnitude(z)) : max_over_halves(max_magnitude(z)));
-      if (in) {
+      for (int g = 0; g < kGroups; ++g) bias[g] = *reinterpret_cast<const float4v*>(e.bias + n0 + first + 8 * g);
+    }
+    if (kLoads && e.residual && in) {
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g)
-          *reinterpret_cast<uint32_t*>(e.keep_codes + at + first + 8 * g) = checkpoint_codes4(z[4 * g], z[4 * g + 1], z[4 * g + 2], z[4 * g + 3], byte);
-        if (first == 0) e.keep_scales[at / 16] = static_cast<uint8_t>(byte);
+      for (int g = 0; g < kGroups; ++g) {
+        const int64_t at = m * e.ldr + n0 + first + 8 * g;
+        if (e.residual_bf16) {
+          const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(e.residual) + at);
+          residual[g][0] = w.x, residual[g][1] = w.y;
+        } else {
+          residual[g] = *reinterpret_cast<const u32x4v*>(static_cast<const float*>(e.residual) + at);
+        }
       }
     }
-    activate(z, e.act);
-  }
-  if (!in) return;
+    if (kLoads && e.grad_codes && in) {
+      const int64_t at = m * e.cols + n0;
+      byte = e.grad_scales[at / 16];
 #pragma unroll
-  for (int g = 0; g < kGroups; ++g) {
-    const int64_t n = n0 + first + 8 * g;
-    float4v d = {z[4 * g], z[4 * g + 1], z[4 * g + 2], z[4 * g + 3]};
-    if (e.residual) d += load4(e.residual, e.residual_bf16, m * e.ldr + n);
-    if (e.out_bf16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(Dv) + m * ldd + n) = make_uint2(f32x2_to_bf16(d[0], d[1]), f32x2_to_bf16(d[2], d[3]));
-    else *reinterpret_cast<float4v*>(static_cast<float*>(Dv) + m * ldd + n) = d;
+      for (int g = 0; g < kGroups; ++g) codes[g] = *reinterpret_cast<const uint32_t*>(e.grad_codes + at + first + 8 * g);
+    }
   }
-}
+
+  __device__ __forceinline__ void finish(const float4v (&v)[kGroups], const GemmEpilogue& e, void* __restrict__ Dv, int64_t ldd, int64_t m, int64_t n0, int first, bool in) const {
+    float z[kGroups * 4];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) z[4 * g + r] = v[g][r] + bias[g][r];
+    if (kLoads && e.grad_codes) {
+      float slope[kGroups * 4];
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) checkpoint_values4(codes[g], byte, slope + 4 * g);
+      activation_slope(slope, e.act);
+#pragma unroll
+      for (int i = 0; i < kGroups * 4; ++i) z[i] *= slope[i];
+    } else {
+      if (e.keep_codes) {
+        const int64_t at = m * e.cols + n0;
+        const uint32_t b = checkpoint_scale(kGroups == 1 ? max_over_groups(max_magnitude(z)) : max_over_halves(max_magnitude(z)));
+        if (in) {
+#pragma unroll
+          for (int g = 0; g < kGroups; ++g)
+            *reinterpret_cast<uint32_t*>(e.keep_codes + at + first + 8 * g) = checkpoint_codes4(z[4 * g], z[4 * g + 1], z[4 * g + 2], z[4 * g + 3], b);
+          if (first == 0) e.keep_scales[at / 16] = static_cast<uint8_t>(b);
+        }
+      }
+      activate(z, e.act);
+    }
+    if (!in) return;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const int64_t n = n0 + first + 8 * g;
+      float4v d = {z[4 * g], z[4 * g + 1], z[4 * g + 2], z[4 * g + 3]};
+      if (kLoads && e.residual) {
+        const u32x4v w = residual[g];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) d[r] += !e.residual_bf16 ? __uint_as_float(w[r]) : r % 2 ? bf16_hi(w[r / 2]) : bf16_lo(w[r / 2]);
+      }
+      if (e.out_bf16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(Dv) + m * ldd + n) = make_uint2(f32x2_to_bf16(d[0], d[1]), f32x2_to_bf16(d[2], d[3]));
+      else *reinterpret_cast<float4v*>(static_cast<float*>(Dv) + m * ldd + n) = d;
+    }
+  }
+};
 
 // A wavefront's whole block of kMB x kNB 16x16 results, 16 rows of four blocks (64 columns) at a time, row by row: a row's lines fill up at once.  (Column
 // group by column group, which needs the bias of one group only, MXFP4 8192 x 20480 x 5120 takes 432 us instead of 418 without anything to do, 528 instead of

@@ -4,6 +4,9 @@
 // Sums, statistics and all arithmetic in FP32; every output is rounded once, from the FP32 value (the norm sees x + r before it is rounded for h).
 // One pass: a row stays in registers between its sum and its output, eight columns to a lane and chunk.  Memory bounds both.  8192 x 5120, bf16 with residual
 // and 8-bit output: 70 us for 380 MB (5.4 TB/s; a large copy runs at 5.1).
+#include <algorithm>
+#include <type_traits>
+
 #include "nvfp4_internal.h"
 #include "checkpoint8.h"
 
@@ -353,10 +356,31 @@ hipError_t backward_with(const RmsNormBackward& a, int parts, float* partials, b
 
 }  // namespace
 
-hipError_t launch_rmsnorm_forward(const RmsNormForward& a, hipStream_t s) {
-  if (a.rows == 0) return hipSuccess;
-  if (a.x_bf16) return a.h_bf16 ? forward_of<true, true>(a, s) : forward_of<true, false>(a, s);
-  return a.h_bf16 ? forward_of<false, true>(a, s) : forward_of<false, false>(a, s);
+// The same call from row r on, for at most `rows` of them.
+static RmsNormForward rows_from(RmsNormForward a, int64_t r, int64_t rows) {
+  auto on = [r](auto*& p, int64_t bytes) {
+    if (p) p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(reinterpret_cast<uintptr_t>(p) + r * bytes);
+  };
+  on(a.x, a.ldx * (a.x_bf16 ? 2 : 4));
+  on(a.residual, a.ldr * (a.h_bf16 ? 2 : 4));
+  on(a.h, a.ldh * (a.h_bf16 ? 2 : 4));
+  on(a.y, a.ldy * (a.y_bf16 ? 2 : 4));
+  on(a.rstd, 4);
+  on(a.codes, a.cols);
+  on(a.scales, a.cols / 16);
+  a.rows = std::min(a.rows - r, rows);
+  return a;
+}
+
+hipError_t launch_rmsnorm_forward(const RmsNormForward& all, hipStream_t s) {
+  const int64_t most = 0xfffffff0 / std::max(row_shape(all.cols).threads, 64) / 4 * 4;   // rows of a launch, which holds 2^32 threads
+  for (int64_t r = 0; r < all.rows; r += most) {
+    const RmsNormForward a = rows_from(all, r, most);
+    const hipError_t e = a.x_bf16 ? (a.h_bf16 ? forward_of<true, true>(a, s) : forward_of<true, false>(a, s))
+                                  : (a.h_bf16 ? forward_of<false, true>(a, s) : forward_of<false, false>(a, s));
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 size_t rmsnorm_partial_bytes(int64_t rows, int64_t cols) {

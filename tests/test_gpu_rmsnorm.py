@@ -160,3 +160,19 @@ def test_same_bits_every_time_and_on_another_stream():
     s.synchronize()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     assert torch.all(buf[need:] == 0xAB)
+
+
+def test_more_rows_than_a_launch_has_threads_for():
+    """67.2 million rows of 16 columns, a wavefront each: 2^32 threads are reached at 67.1 million."""
+    rows, cols = (1 << 26) + 100_000, 16
+    x = torch.ones(rows, cols, device="cuda", dtype=BF16)
+    v = activations(3, cols, 11, BF16)
+    x[-3:] = bm.tensor(v, BF16)
+    x[(1 << 26) - 4] = 0
+    out = nv.nvfp4_rmsnorm_forward(x, eps=EPS, checkpoint=True)
+    ref = bm.norm(v, None, None, EPS)[3]
+    bm.within(out.y[-3:], ref, 2 * FP32 * np.abs(ref) + bm.rounding(ref, BF16))
+    rest = out.y[:-3]
+    assert int((rest == 0).sum()) == cols and int((rest == 1).sum()) == rest.numel() - cols
+    assert int((out.checkpoint.codes[:-3] == 0).sum()) == cols
+    check_checkpoint(nv.Checkpoint8(out.checkpoint.codes[-3:], out.checkpoint.scales[-3:]), ref)
