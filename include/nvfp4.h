@@ -362,7 +362,8 @@ int nvfp4_checkpoint_load(const nvfp4_checkpoint* c, int activation, const float
  *   rstd      FP32 [rows], or NULL
  *   keep      8 bits of xhat (keep_kind NVFP4_NORM_KEEP_NORMALIZED: what nvfp4_rmsnorm_backward reads) or of y
  *             (NVFP4_NORM_KEEP_OUTPUT), or NULL
- * The norm is taken of the FP32 sum, before it is rounded for h.  Every tensor is read or written once.
+ * The norm is taken of the FP32 sum, before it is rounded for h.  Every tensor is read or written once.  (A row of zeros with eps = 0
+ * gives what the formula gives, NaN.)
  */
 enum { NVFP4_NORM_KEEP_NORMALIZED = 0, NVFP4_NORM_KEEP_OUTPUT = 1 };
 int nvfp4_rmsnorm_forward(const void* x, int x_dtype, int64_t ldx, const void* residual, int64_t ldr, const float* gamma, float eps, int64_t rows,

@@ -13,7 +13,9 @@ namespace nvfp4 {
 
 namespace {
 
-// A workgroup covers 512 columns (eight to a lane) of kRows rows, its wavefronts taking every fourth row.
+// A workgroup covers 512 columns (eight to a lane) of some rows, its wavefronts taking every fourth row.  (A line of 128 scales belongs to four such strips, and is
+// fetched by as many XCDs: 200 MiB instead of 170 for 8192 x 20480.  Four wavefronts side by side on 2048 columns read 170 and take longer: load 90 us instead of
+// 88, activation gradient 181 instead of 164.)
 constexpr int kStrip = 512;
 
 template <bool kBf16>

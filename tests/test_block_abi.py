@@ -1,5 +1,7 @@
 """CPU: the calls around the linear layers refuse bad arguments before anything is enqueued; the binding refuses what it can see."""
 import ctypes
+import os
+import subprocess
 
 import pytest
 import torch
@@ -16,6 +18,20 @@ def lib():
 
 def ckpt(rows=32, cols=64, codes=P, scales=P):
     return ctypes.byref(nv.CheckpointStruct(rows, cols, codes, scales))
+
+
+def test_struct_layouts_match_the_header(tmp_path):
+    structs = {"nvfp4_checkpoint": nv.CheckpointStruct, "nvfp4_epilogue": nv.EpilogueStruct}
+    lines = []
+    for name, mirror in structs.items():
+        lines.append(f'printf("%zu\\n", sizeof({name}));')
+        lines += [f'printf("%zu\\n", offsetof({name}, {f[0]}));' for f in mirror._fields_]
+    src, exe = tmp_path / "layout.c", tmp_path / "layout"
+    src.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "nvfp4.h"\nint main(void) {\n' + "\n".join(lines) + "\nreturn 0;\n}\n")
+    subprocess.run(["gcc", "-std=c99", "-I", os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include"), str(src), "-o", str(exe)], check=True)
+    got = [int(v) for v in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
+    want = [v for m in structs.values() for v in [ctypes.sizeof(m)] + [getattr(m, f[0]).offset for f in m._fields_]]
+    assert got == want
 
 
 def test_struct_layout():
