@@ -308,7 +308,7 @@ struct EpilogueBlock {
     uint32_t byte;
   };
   const GemmEpilogue& e;
-  const float *ts_a, *ts_b;
+  const float* ts_b;
   int64_t ldd, row0, col0;
   int rows, cols, l16, lq, nl;   // nl: the lane's first column in a pair of bf16 blocks
   bool a_per_row, b_per_row;
@@ -318,7 +318,7 @@ struct EpilogueBlock {
   uint8_t *codes, *scales;       // of block lq
 
   __device__ __forceinline__ EpilogueBlock(const GemmEpilogue& e_, const TensorScales& ts, void* Dv, int64_t ldd_, int64_t row0_, int64_t col0_, int rows_, int cols_, int lane)
-      : e(e_), ts_a(ts.a), ts_b(ts.b), ldd(ldd_), row0(row0_), col0(col0_), rows(rows_), cols(cols_), l16(lane & 15), lq(lane >> 4), nl((lq & 1) * 16 + (lq >> 1) * 8),
+      : e(e_), ts_b(ts.b), ldd(ldd_), row0(row0_), col0(col0_), rows(rows_), cols(cols_), l16(lane & 15), lq(lane >> 4), nl((lq & 1) * 16 + (lq >> 1) * 8),
         a_per_row(ts.a_per_row), b_per_row(ts.b_per_row) {
     const int64_t row = row0 + l16;
     d = static_cast<char*>(Dv) + (e.out_bf16 ? (row * ldd + col0 + nl) * 2 : (row * ldd + col0 + 4 * lq) * 4);
@@ -365,23 +365,27 @@ struct EpilogueBlock {
     }
   }
 
-  // sums: the unit's blocks, unscaled: four of them, or what is left at the end of a row.  uniform: the operands' factor where neither has one per row.
+  // The operands' factors: their product where neither has one per row; otherwise A's of each of the lane's rows, and B's first.  (B's are read where they are
+  // used, which waits for all that is in flight: 8192 x 20480 x 5120 with a residual 1228 us instead of 1136.)
+  struct Factors {
+    float uniform, a[kMB], b0;
+  };
+
+  // sums: the unit's blocks, unscaled: four of them, or what is left at the end of a row.
   template <int kBlocks>
-  __device__ __forceinline__ void finish(float4v (&sums)[kBlocks], const Loads& l, int i, int jg, float uniform, const float4v (&bias)[kKind == kGrad ? 1 : kNB]) const {
+  __device__ __forceinline__ void finish(float4v (&sums)[kBlocks], const Loads& l, int i, int jg, const Factors& f, const float4v (&bias)[kKind == kGrad ? 1 : kNB]) const {
     const bool row_in = i * 16 < rows;
     const int64_t down = static_cast<int64_t>(i) * 16;
     if (a_per_row || b_per_row) {
-      const float sa = ts_a[a_per_row ? row0 + row_block(i) * 16 + l16 : 0];
 #pragma unroll
       for (int k = 0; k < kBlocks; ++k) {
-        const float b0 = ts_b[0];
-        float4v sb = {b0, b0, b0, b0};
+        float4v sb = {f.b0, f.b0, f.b0, f.b0};
         if (b_per_row) sb = *reinterpret_cast<const float4v*>(ts_b + col0 + col_block(4 * jg + k) * 16 + 4 * lq);
-        sums[k] *= sb * sa;
+        sums[k] *= sb * f.a[i];
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < kBlocks; ++k) sums[k] *= uniform;
+      for (int k = 0; k < kBlocks; ++k) sums[k] *= f.uniform;
     }
     float z[4 * kBlocks];
 #pragma unroll
@@ -486,7 +490,10 @@ __device__ __forceinline__ void store_wave_block_epilogue(float4v (&acc)[kMB][kN
   const Block b(e, ts, Dv, ldd, row0, col0, rows, cols, lane);
   constexpr int kAhead = Block::kAhead, kUnits = Block::kUnits, kGroups = Block::kGroups;
   constexpr bool kLoads = Block::kLoads;
-  const float uniform = ts.a[0] * ts.b[0];
+  typename Block::Factors factors;
+  factors.uniform = ts.a[0] * ts.b[0], factors.b0 = ts.b[0];
+#pragma unroll
+  for (int i = 0; i < kMB; ++i) factors.a[i] = ts.a[b.a_per_row ? row0 + b.row_block(i) * 16 + b.l16 : 0];
   float4v bias[kKind == kGrad ? 1 : kNB];
   b.columns(bias);
   typename Block::Loads ring[kLoads ? kAhead : 1];
@@ -496,7 +503,7 @@ __device__ __forceinline__ void store_wave_block_epilogue(float4v (&acc)[kMB][kN
     float4v sums[kBlocks];
 #pragma unroll
     for (int k = 0; k < kBlocks; ++k) sums[k] = i * kNB + 4 * jg + k < kInAcc ? read_acc(acc[i][4 * jg + k]) : acc[i][4 * jg + k];
-    b.template finish<kBlocks>(sums, ring[kLoads ? u % kAhead : 0], i, jg, uniform, bias);
+    b.template finish<kBlocks>(sums, ring[kLoads ? u % kAhead : 0], i, jg, factors, bias);
     if constexpr (kLoads && u + kAhead < kUnits) b.fetch(ring[u % kAhead], (u + kAhead) / kGroups, (u + kAhead) % kGroups);
     __builtin_amdgcn_sched_barrier(0);
   });
