@@ -124,8 +124,11 @@ int strips_of(int64_t cols) { return static_cast<int>((cols + kStrip - 1) / kStr
 // Workgroups start in order, so the shorter they are the closer together the chip reads and writes; the sums' second launch has their number to
 // add up.  8192 x 20480, us with 1024 / 4096 / 8192 / 16384 / 32768 workgroups: save bf16 103 / 107 / 101 / 96 / 91, load bf16 107 / 105 / 99 / 93 / 88, activation gradient
 // without sums 169 / 167 / 156 / 150 / 146; with sums, 128 / 256 / 512 parts: 170 / 165 / 164, 8192 x 1296 20 / 15.5 / 16.2.
-constexpr int64_t kMostGroups = 32768, kMostParts = 256;
+// A few rows are one workgroup's to a strip, whose sums need no second launch (16 x 5120, us on the GPU / called from Python: 5.2 / 5.7, in two launches 5.3 / 8.6; 32 rows 8.0 /
+// 7.9 and 5.3 / 8.4).
+constexpr int64_t kMostGroups = 32768, kMostParts = 256, kFew = 16;
 int rows_of(int64_t rows, int64_t cols, bool sums) {
+  if (sums && rows <= kFew) return kFew;
   int64_t groups = std::max<int64_t>(kMostGroups / strips_of(cols), 1);
   if (sums) groups = std::min(groups, kMostParts);
   const int64_t each = (rows + groups - 1) / groups;

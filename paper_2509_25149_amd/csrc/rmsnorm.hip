@@ -315,9 +315,11 @@ constexpr int kMostCols = 32768;
 // Workgroups of the backward pass: one to a CU where a row has 4096 columns or more, otherwise as many as have that many columns on their way together.  More
 // of them write more partial sums (5120 columns: 5 MB from 256, 10 from 512) and get fewer rows each to overlap.  us with 2048 / 4096 / 8192 / 16384 columns:
 // 8192 x 5120 60 / 60 / 63 / 69, x 2560 44 / 35 / 34 / 40, x 2048 37 / 28 / 30 / 36, x 1024 16 / 16 / 17 / 19, 1040 x 2064 13.1 / 12.9 / 15.9 / 17.
-constexpr int64_t kColsOnTheWay = 4096, kCUs = 256;
+// A few rows take one workgroup and no second launch (5120 columns, us on the GPU / called from Python: a row 3.4 / 6.9, four 7.3 / 7.1 so and 5.7 / 8.9 in two launches).
+constexpr int64_t kColsOnTheWay = 4096, kCUs = 256, kFew = 3;
 int backward_parts(int64_t rows, int64_t cols) {
   const int64_t each = row_shape(cols).wave ? 4 : 1, groups = (rows + each - 1) / each;
+  if (groups <= kFew) return groups > 0 ? 1 : 0;
   const int64_t most = kCUs * ((kColsOnTheWay + cols * each - 1) / (cols * each));
   return static_cast<int>(groups < most ? groups : most);
 }
