@@ -90,15 +90,18 @@ enum { kActNone = 0, kActRelu2 = 1, kActGelu = 2, kActSilu = 3 };
 
 // The argument p = z (c1 + c3 z^2) times log2(e) / 2: with w = 2^-|that|, q = w^2 = exp(-|p|), and s = 1 / (1 + q), or q / (1 + q) below zero.  (A square, because the
 // exponential instruction has no subnormal results and a product has: nothing is flushed to zero before it is below the smallest number.)
+// kOfSum: z may be infinite, where SiLU's p, 0 * z * z * z, is NaN: the clamp takes w = 0 then (a modifier of the exponential, no instruction; w is in [0, 1] without it).  z's own
+// NaN reaches the result through z s.  Without it z comes from a checkpoint, which has no infinities, and its NaN stays in q and r.
+template <bool kOfSum>
 struct Logistic {
-  float p, q, r;   // r = 1 / (1 + q)
-  __device__ __forceinline__ Logistic(float z, float c1, float c3) {
-    p = z * __builtin_fmaf(c3 * z, z, c1);
-    const float w = __builtin_amdgcn_exp2f(-__builtin_fabsf(p));
-    q = w * w;
+  float z, q, r;   // r = 1 / (1 + q)
+  __device__ __forceinline__ Logistic(float z_, float c1, float c3) : z(z_) {
+    const float p = z * __builtin_fmaf(c3 * z, z, c1);
+    const float w = __builtin_amdgcn_exp2f(-__builtin_fabsf(p)), in = kOfSum ? __builtin_amdgcn_fmed3f(w, 0.0f, 1.0f) : w;
+    q = in * in;
     r = __builtin_amdgcn_rcpf(1.0f + q);
   }
-  __device__ __forceinline__ float s() const { return p < 0.0f ? q * r : r; }
+  __device__ __forceinline__ float s() const { return z < 0.0f ? q * r : r; }   // (p has z's sign)
 };
 constexpr float kHalfLog2E = 0.72134752044448170f;
 __device__ __forceinline__ float logistic_c1(int act) { return act == kActSilu ? kHalfLog2E : 1.5957691216057308f * kHalfLog2E; }
@@ -115,7 +118,7 @@ __device__ __forceinline__ void activate(float (&v)[kN], int act) {
   } else if (act != kActNone) {
     const float c1 = logistic_c1(act), c3 = logistic_c3(act);
 #pragma unroll
-    for (int i = 0; i < kN; ++i) v[i] *= Logistic(v[i], c1, c3).s();
+    for (int i = 0; i < kN; ++i) v[i] *= Logistic<true>(v[i], c1, c3).s();
   }
 }
 
@@ -133,9 +136,9 @@ __device__ __forceinline__ void activation_slope(float (&v)[kN], int act) {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const float z = v[i];
-      const Logistic l(z, c1, c3);
+      const Logistic<false> l(z, c1, c3);
       const float qr = l.q * l.r, t = qr * l.r;   // s (1 - s)
-      v[i] = (l.p < 0.0f ? qr : l.r) + (t > 0.0f ? z * t * __builtin_fmaf(d3 * z, z, d1) : 0.0f);   // (far out t is 0 and the polynomial infinite)
+      v[i] = (z < 0.0f ? qr : l.r) + (t > 0.0f ? z * t * __builtin_fmaf(d3 * z, z, d1) : 0.0f);   // (far out t is 0 and the polynomial infinite)
     }
   }
 }
