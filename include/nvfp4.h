@@ -315,8 +315,9 @@ int nvfp4_dequantize(const nvfp4_qtensor* q, int which_copy, int undo_rht, void*
  * it for the backward pass.  Rules that all of these calls share:
  *   - Element types are NVFP4_OUT_F32 and NVFP4_OUT_BF16.  All arithmetic, sums and statistics are FP32; an output is
  *     rounded once, to nearest even.
- *   - Rows may be any number, 0 included (nothing to do; sums over no rows are 0); columns are a positive multiple of
- *     16; leading dimensions are in elements, at least the columns and multiples of 8 -- else NVFP4_ERR_BAD_SHAPE.
+ *   - Rows may be any number, 0 included (nothing to do; sums over no rows are 0), but for nvfp4_gemm_epilogue (below);
+ *     columns are a positive multiple of 16; leading dimensions are in elements, at least the columns and multiples of 8
+ *     -- else NVFP4_ERR_BAD_SHAPE.
  *     Pointers are 16-byte aligned (rstd 4, checkpoint scales 1), else NVFP4_ERR_INVALID_ARG; those of a tensor
  *     without rows may be NULL.
  *   - An output may be the very tensor that an input of the same type and leading dimension is (x or residual and h or
@@ -405,6 +406,7 @@ int nvfp4_activation_backward(const void* da, int dtype, int64_t ldda, int64_t r
  *   residual  [M, N] of type residual_dtype, leading dimension ldr, or NULL
  *   keep      the checkpoint that z goes to, or NULL
  *   grad_of   the checkpoint of z for the second form; then bias, residual and keep are NULL
+ * M and N are positive multiples of 16, as nvfp4_quantize's tensors are, else NVFP4_ERR_BAD_SHAPE.
  * a, b, op, D, ldd, workspace as in nvfp4_gemm (either format, tensor-level scales of either granularity); out_dtype
  * NVFP4_OUT_F32 or NVFP4_OUT_BF16.  All of it happens to the FP32 result, D is rounded once.
  */

@@ -626,6 +626,7 @@ int nvfp4_activation_backward(const void* da, int dtype, int64_t ldda, int64_t r
 static int plan_epilogue(const nvfp4_epilogue* p, int out_dtype, GemmArgs* g, GemmEpilogue* e) {
   if (!p || !element_type(out_dtype) || !activation(p->activation)) return NVFP4_ERR_INVALID_ARG;
   const int64_t M = g->a.outer, N = g->b.outer;
+  if (M % 16 || N % 16) return NVFP4_ERR_BAD_SHAPE;   // the output stages take 16 x 16 blocks whole: the last that exist, a block's scale, the blocks' rows
   *e = GemmEpilogue{};
   if (p->grad_of) {
     if (p->bias || p->residual || p->keep) return NVFP4_ERR_INVALID_ARG;
