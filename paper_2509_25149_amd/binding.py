@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import threading
 from dataclasses import dataclass
 from typing import NamedTuple, Optional
 
@@ -201,14 +202,22 @@ def alloc_qtensor(rows: int, cols: int, layout_mask: int, device="cuda", block_d
     return q
 
 
-_workspaces = {}
+class _Workspaces(threading.local):
+    """Scratch memory of the calls that are given none, per device and stream: calls on a stream run one after the other.  Each host thread has its own, since two threads'
+    calls on one stream may enqueue their launches between each other's."""
+    def __init__(self):
+        self.of = {}
 
 
-def _workspace(device, nbytes: int) -> torch.Tensor:
-    key = (torch.device(device).index or 0, _stream())
-    if key not in _workspaces or _workspaces[key].numel() < nbytes:
-        _workspaces[key] = torch.empty(max(nbytes, 1 << 16), dtype=torch.uint8, device=device)
-    return _workspaces[key]
+_workspaces = _Workspaces()
+
+
+def _workspace(device: torch.device, nbytes: int) -> torch.Tensor:
+    of, key = _workspaces.of, (device.index, _stream())
+    w = of.get(key)
+    if w is None or w.numel() < nbytes:
+        w = of[key] = torch.empty(max(nbytes, 1 << 16), dtype=torch.uint8, device=device)
+    return w
 
 
 def nvfp4_quantize(x: torch.Tensor, layout_mask: int, block_dim: int = BLOCK_1x16, rounding: int = ROUND_RNE,
