@@ -204,7 +204,9 @@ def alloc_qtensor(rows: int, cols: int, layout_mask: int, device="cuda", block_d
 
 class _Workspaces(threading.local):
     """Scratch memory of the calls that are given none, per device and stream: calls on a stream run one after the other.  Each host thread has its own, since two threads'
-    calls on one stream may enqueue their launches between each other's."""
+    calls on one stream may enqueue their launches between each other's.  A call that is being captured into a graph gets memory of its own: the graph keeps the address, and
+    its replays run beside and after whatever else is enqueued.  (torch.cuda.graph keeps what is allocated during its capture for the graph; a graph captured in another way
+    needs a workspace of the caller's.)"""
     def __init__(self):
         self.of = {}
 
@@ -212,12 +214,31 @@ class _Workspaces(threading.local):
 _workspaces = _Workspaces()
 
 
-def _workspace(device: torch.device, nbytes: int) -> torch.Tensor:
-    of, key = _workspaces.of, (device.index, _stream())
-    w = of.get(key)
-    if w is None or w.numel() < nbytes:
-        w = of[key] = torch.empty(max(nbytes, 1 << 16), dtype=torch.uint8, device=device)
+def _workspace(device: torch.device, nbytes: int):
+    """Address, size, and the tensor: to be held until the call has enqueued its work."""
+    capturing = torch.cuda.is_current_stream_capturing()
+    if not capturing:
+        of, key = _workspaces.of, (device.index, _stream())
+        w = of.get(key)
+        if w is not None and w[1] >= nbytes:
+            return w
+        nbytes = max(nbytes, 1 << 16)
+    t = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    w = (t.data_ptr(), nbytes, t)
+    if not capturing:
+        of[key] = w
     return w
+
+
+@functools.lru_cache(maxsize=1024)
+def _quantize_workspace_bytes(rows: int, cols: int) -> int:
+    return quantized_sizes(rows, cols)[2]
+
+
+def _quantize_workspace(workspace: Optional[torch.Tensor], rows: int, cols: int, device):
+    if workspace is None:
+        return _workspace(device, _quantize_workspace_bytes(rows, cols))
+    return workspace.data_ptr(), workspace.numel(), workspace
 
 
 def nvfp4_quantize(x: torch.Tensor, layout_mask: int, block_dim: int = BLOCK_1x16, rounding: int = ROUND_RNE,
@@ -230,10 +251,10 @@ def nvfp4_quantize(x: torch.Tensor, layout_mask: int, block_dim: int = BLOCK_1x1
     rows, cols = x.shape
     if out is None:
         out = alloc_qtensor(rows, cols, layout_mask, x.device, block_dim)
-    ws = workspace if workspace is not None else _workspace(x.device, quantized_sizes(rows, cols)[2])
+    ws, ws_bytes, workspace = _quantize_workspace(workspace, rows, cols, x.device)
     _check(load_library().nvfp4_quantize(x.data_ptr(), rows, cols, x.stride(0), layout_mask, block_dim, rounding,
                                          int(rht_on_col), rht_seed, sr_seed, ctypes.byref(out.desc),
-                                         ws.data_ptr(), ws.numel(), _stream()))
+                                         ws, ws_bytes, _stream()))
     out.row_fp16 = out.col_fp16 = None          # the library cleared the descriptor's pointers: the codes changed
     return out
 
@@ -258,9 +279,9 @@ def nvfp4_amax(x: torch.Tensor, rht_on_col=False, rht_seed: int = 0, out: Option
     rows, cols = x.shape
     if out is None:
         out = torch.empty(2, dtype=torch.float32, device=x.device)
-    ws = workspace if workspace is not None else _workspace(x.device, quantized_sizes(rows, cols)[2])
+    ws, ws_bytes, workspace = _quantize_workspace(workspace, rows, cols, x.device)
     _check(load_library().nvfp4_amax(x.data_ptr(), rows, cols, x.stride(0), int(rht_on_col), rht_seed, out.data_ptr(),
-                                     ws.data_ptr(), ws.numel(), _stream()))
+                                     ws, ws_bytes, _stream()))
     return out
 
 
@@ -454,10 +475,8 @@ def rowsum_workspace_bytes(rows: int, cols: int) -> int:
 def _rowsum_workspace(workspace: Optional[torch.Tensor], rows: int, cols: int, device):
     if workspace is None:
         need = rowsum_workspace_bytes(rows, cols)
-        if need == 0:
-            return None, 0
-        workspace = _workspace(device, need)
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        return _workspace(device, need) if need else (None, 0, None)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
 def nvfp4_checkpoint_save(x: torch.Tensor, out: Optional[Checkpoint8] = None) -> Checkpoint8:
@@ -560,7 +579,7 @@ def nvfp4_rmsnorm_backward(dy: torch.Tensor, saved, rstd: torch.Tensor, gamma: O
         gp = dgamma.data_ptr()
     else:
         gp = _vector(dgamma, cols, "dgamma")
-    ws, ws_bytes = _rowsum_workspace(workspace, rows, cols, device)
+    ws, ws_bytes, workspace = _rowsum_workspace(workspace, rows, cols, device)
     _check(load_library().nvfp4_rmsnorm_backward(yp, dt, ldy, hp, ldh, sp, _vector(rstd, rows, "rstd"), _vector(gamma, cols, "gamma"), rp, ldr, rows, cols, xp, st,
                                                  ldx, gp, int(accumulate_dgamma), ws, ws_bytes, _stream()))
     return dx, dgamma
@@ -601,7 +620,7 @@ def nvfp4_activation_backward(da: torch.Tensor, saved: Optional[Checkpoint8] = N
             bp = dbias.data_ptr()
         else:
             bp = _vector(dbias, cols, "dbias")
-        ws, ws_bytes = _rowsum_workspace(workspace, rows, cols, device)
+        ws, ws_bytes, workspace = _rowsum_workspace(workspace, rows, cols, device)
     _check(load_library().nvfp4_activation_backward(ap, dt, lda, rows, cols, None if saved is None else saved.ref, activation, zp, ldz, bp, int(accumulate_dbias), ws,
                                                     ws_bytes, _stream()))
     return dz, dbias

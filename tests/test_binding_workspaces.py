@@ -75,3 +75,25 @@ def test_two_threads_on_one_stream_do_not_share_a_workspace(stand_in, first, sec
     CALLS[first](512)
     assert len(lib.given) == 2 and all(p and n for p, n in lib.given)
     assert disjoint(*lib.given)
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+def test_a_captured_call_has_a_workspace_of_its_own(stand_in, monkeypatch, name):
+    """A graph keeps the address.  So it must not be one that a later call is given, nor one that is freed when a later call needs more."""
+    alive, empty = [], torch.empty                      # (kept alive here: addresses that are freed could be given out again)
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: alive.append(empty(*a, **k)) or alive[-1])
+    lib, capturing = stand_in(), [False]
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    CALLS[name](512)
+    capturing[0] = True
+    CALLS[name](512)
+    CALLS[name](512)
+    capturing[0] = False
+    CALLS[name](512)
+    CALLS[name](2048)
+    before, captured, captured_too, after, larger = lib.given
+    assert before == after                              # (one buffer as long as it is large enough)
+    for graph in (captured, captured_too):
+        for other in (before, after, larger):
+            assert disjoint(graph, other)
+    assert disjoint(captured, captured_too)
