@@ -454,7 +454,7 @@ def _matrix(t: torch.Tensor, what: str, shape=None):
     dt, size, strides = _DTYPES.get(t.dtype), t.shape, t.stride()
     if dt is None or len(size) != 2 or (strides[1] != 1 and size[1] != 1) or not t.is_cuda or (shape is not None and size != shape):
         raise ValueError(f"{what} must be a 2-D float32 or bf16 CUDA tensor with unit inner stride" + (f" of shape {tuple(shape)}" if shape is not None else ""))
-    return dt, t.data_ptr(), strides[0] if size[0] > 1 else max(strides[0], size[1])     # (torch leaves the stride of a single row open)
+    return dt, t.data_ptr(), strides[0] if size[0] > 1 else size[1]     # (torch leaves the stride of a single row open: it may be anything)
 
 
 def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
