@@ -29,6 +29,14 @@ from paper_2509_25149_amd import binding as nv  # noqa: E402
 RC = nv.LAYOUT_ROW | nv.LAYOUT_COL
 
 
+def keep_col_copy(q: nv.QTensor) -> nv.QTensor:
+    """Give a quantized tensor's row copy back: its memory, and its place in the descriptor, so that a call that asks for it is refused."""
+    q.row_codes = q.row_scales = q.row_ts = None
+    q.desc.row_codes = q.desc.row_scales = q.desc.row_tensor_scale = None
+    q.desc.layout_mask &= ~nv.LAYOUT_ROW
+    return q
+
+
 class MlpBlock:
     """Parameters in FP32 or bf16, gradients in FP32; sizes multiples of 16."""
 
@@ -66,9 +74,7 @@ class MlpBlock:
         a = nv.nvfp4_gemm_epilogue(qn, self.q1, nv.OP_FPROP, bias=self.b1, activation=nv.ACT_RELU2, keep=z, workspace=ws)
         qa = nv.nvfp4_quantize(a, RC, rht_on_col=True, rht_seed=self.rht_seed)
         y = nv.nvfp4_gemm_epilogue(qa, self.q2, nv.OP_FPROP, bias=self.b2, residual=norm.h, workspace=ws)
-        for q in (qn, qa):          # the row copies have done their work
-            q.row_codes = q.row_scales = None
-        return y, (norm.checkpoint, norm.rstd, qn, z, qa)
+        return y, (norm.checkpoint, norm.rstd, keep_col_copy(qn), z, keep_col_copy(qa))      # (the row copies have done their work)
 
     def backward(self, dy: torch.Tensor, saved, sr_seed: int = 0):
         """Adds to the gradients; returns the gradient of x and of r, which are one."""
