@@ -325,7 +325,11 @@ int nvfp4_dequantize(const nvfp4_qtensor* q, int which_copy, int undo_rht, void*
  *   - Sums over rows are added in a fixed order: the same inputs give the same bits.
  */
 enum { NVFP4_ACT_NONE = 0, NVFP4_ACT_RELU2 = 1, NVFP4_ACT_GELU = 2, NVFP4_ACT_SILU = 3 };
-/* RELU2: max(z, 0)^2.  SILU: z / (1 + exp(-z)).  GELU: z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))). */
+/* RELU2: max(z, 0)^2.  SILU: z / (1 + exp(-z)).  GELU: z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))).
+ * Infinities give what the formulas give: +inf at +inf; at -inf 0 for RELU2, NaN for SILU and GELU.
+ * SILU and GELU are z / (1 + exp(-p)), p = z or 2 sqrt(2 / pi) (z + 0.044715 z^3), evaluated in FP32: off by at most
+ * 2^-22 (4 + |p|) of themselves -- 1e-6 at 0, 2e-5 far below 0, where they are exp(p) z -- and their derivatives by
+ * 2^-22 (4 + 2 |p|) of the terms they are the sum of. */
 
 /*
  * An activation kept in 8 bits: every 16 consecutive columns of a row have one scale 2^e, e the smallest integer with
@@ -364,7 +368,7 @@ int nvfp4_checkpoint_load(const nvfp4_checkpoint* c, int activation, const float
  *   keep      8 bits of xhat (keep_kind NVFP4_NORM_KEEP_NORMALIZED: what nvfp4_rmsnorm_backward reads) or of y
  *             (NVFP4_NORM_KEEP_OUTPUT), or NULL
  * The norm is taken of the FP32 sum, before it is rounded for h.  Every tensor is read or written once.  (A row of zeros with eps = 0
- * gives what the formula gives, NaN.)
+ * gives what the formula gives, NaN.  The sum of squares is FP32: magnitudes above 1.8e19 overflow it, and that row's rstd and y are 0.)
  */
 enum { NVFP4_NORM_KEEP_NORMALIZED = 0, NVFP4_NORM_KEEP_OUTPUT = 1 };
 int nvfp4_rmsnorm_forward(const void* x, int x_dtype, int64_t ldx, const void* residual, int64_t ldr, const float* gamma, float eps, int64_t rows,

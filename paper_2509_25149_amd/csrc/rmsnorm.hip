@@ -158,7 +158,7 @@ __device__ __forceinline__ void load_gamma(const float* gamma, int col, float (&
 // Workgroup w takes rows w, w + parts, ... and leaves its sum of dy xhat in row w of the partial sums (kWaveRow: a wavefront per row, four of them
 // in a workgroup add theirs through LDS).  The next row's loads are issued before the row in hand is worked on (kAhead): a workgroup waits for memory once
 // a row otherwise, and few are resident.  For that nothing else may be loaded in the loop -- memory answers in order -- so gamma stays in registers, and
-// columns and rows past the end are replaced by the last instead of being skipped.  8192 x 5120, bf16, from 8 bits, with dres: 60 us = 4.9 TB/s with the second launch's
+// columns and rows past the end are replaced by the last instead of being skipped.  8192 x 5120, bf16, from 8 bits, with dres: 57 us = 5.2 TB/s with the second launch's
 // 4 us; 80 with twice as many workgroups that load a row, work on it and store it in turn.
 // Four chunks (more than 16384 columns), and workgroups of more than 512 threads, have no registers for that; with four the sums are kept in LDS too (each
 // lane its own) and dres is loaded where it is added.
@@ -314,7 +314,8 @@ hipError_t forward_of(const RmsNormForward& a, hipStream_t s) {
 constexpr int kMostCols = 32768;
 // Workgroups of the backward pass: one to a CU where a row has 4096 columns or more, otherwise as many as have that many columns on their way together.  More
 // of them write more partial sums (5120 columns: 5 MB from 256, 10 from 512) and get fewer rows each to overlap.  us with 2048 / 4096 / 8192 / 16384 columns:
-// 8192 x 5120 60 / 60 / 63 / 69, x 2560 44 / 35 / 34 / 40, x 2048 37 / 28 / 30 / 36, x 1024 16 / 16 / 17 / 19, 1040 x 2064 13.1 / 12.9 / 15.9 / 17.
+// 8192 x 5120 60 / 60 / 63 / 69, x 2560 44 / 35 / 34 / 40, x 2048 37 / 28 / 30 / 36, x 1024 16 / 16 / 17 / 19, 1040 x 2064 13.1 / 12.9 / 15.9 / 17 (there 496 of the 512
+// workgroups have two rows and 16 three).
 // A few rows take one workgroup and no second launch (5120 columns, us on the GPU / called from Python: a row 3.4 / 6.9, four 7.3 / 7.1 so and 5.7 / 8.9 in two launches).
 constexpr int64_t kColsOnTheWay = 4096, kCUs = 256, kFew = 3;
 int backward_parts(int64_t rows, int64_t cols) {

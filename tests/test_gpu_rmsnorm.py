@@ -10,8 +10,8 @@ pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
 OUT = {F32: nv.OUT_F32, BF16: nv.OUT_BF16}
 EPS = 1e-5
-# columns at and beside the limits of a wavefront (512, 1024), a workgroup with one, two and four chunks (2048, 16384, 32768); rows of one wavefront, of one
-# workgroup, more than the backward pass has workgroups (512)
+# columns at and beside the limits of a wavefront (512, 1024), a workgroup with one, two and four chunks (2048, 16384, 32768); a few rows, which the
+# backward pass gives to one workgroup, and as many as there are workgroups or (1025 x 2064) more
 SHAPES = [(1, 16), (1, 5120), (5, 496), (3, 512), (9, 528), (6, 1024), (7, 1040), (2, 2048), (3, 2064), (5, 5120), (2, 16384), (3, 16400), (2, 32768),
           (1030, 256), (2100, 48), (517, 1040), (1025, 2064)]
 FP32 = 64 * 2.0 ** -24     # relative error of a row's sum of squares (a tree of depth 64 at most) and of the operations behind it

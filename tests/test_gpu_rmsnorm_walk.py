@@ -42,3 +42,12 @@ def test_backward_over_several_rows(rows, cols, parts, each, dt, st, saved8, gam
     dx2, grown = nv.nvfp4_rmsnorm_backward(dy, saved, fwd.rstd, gt, dres=dres, dx=over, dx_dtype=OUT[st], dgamma=old, accumulate_dgamma=True)
     assert torch.equal(dx2, dx) and (over is None or dx2 is over)
     bm.within(grown, ref_gamma + before, tol + 2.0 ** -23 * (np.abs(before) + np.abs(ref_gamma)))
+
+
+def test_rows_whose_squares_overflow():
+    """FP32's largest number is 3.4e38: from 1.8e19 on a square is infinite, and what it is the norm of comes out as 0; the rows beside it are as ever."""
+    x = torch.ones(3, 2064, device="cuda")
+    x[1, 7] = 1.9e19
+    out = nv.nvfp4_rmsnorm_forward(x, y_dtype=nv.OUT_F32, checkpoint=True)
+    assert float(out.rstd[1]) == 0 and bool((out.y[1] == 0).all()) and bool((out.checkpoint.scales[1] == 0).all())
+    assert torch.allclose(out.y[[0, 2]], x[[0, 2]], atol=1e-5)
