@@ -429,6 +429,107 @@ int nvfp4_gemm_epilogue(const nvfp4_qtensor* a, const nvfp4_qtensor* b, int op, 
 /* Bytes of the workspace that either backward call needs for its sums over rows (host pointer out); may be 0. */
 int nvfp4_rowsum_workspace_bytes(int64_t rows, int64_t cols, size_t* workspace_bytes);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * The ends of a training step: tokens to rows at its front, log probabilities and the logits' gradient at its back, and the norm over all gradients before
+ * the optimizer.  These stay in high precision (Sec. 4.1 keeps embeddings, the output head and the main gradients so).  The rules of the section above hold
+ * here too, with these differences:
+ *   - Token numbers are NVFP4_INDEX_I32 or NVFP4_INDEX_I64 values on the device, aligned to their size.  A number outside the vocabulary is no error: such a
+ *     token has no row and is not counted (padding).
+ *   - A vocabulary may have any size; leading dimensions of logits stay multiples of 8, and nothing is read or written behind a row's last column.
+ *   - The gradient of the logits may be written over the logits, if it has their type and leading dimension; no other overlaps.
+ */
+enum { NVFP4_INDEX_I32 = 0, NVFP4_INDEX_I64 = 1 };
+
+/*
+ * out[t] = scale * table[ids[t]]; zeros for an id outside [0, vocab).
+ *   ids    [tokens], at most 2^30 - 1;  table  [vocab, cols] of type table_dtype, cols <= 32768;  out  [tokens, cols] of type out_dtype;  scale finite
+ */
+int nvfp4_embedding_forward(const void* ids, int index_type, int64_t tokens, const void* table, int table_dtype, int64_t vocab, int64_t cols, int64_t ldt,
+                            float scale, void* out, int out_dtype, int64_t ldo, nvfp4_stream_t stream);
+
+/*
+ * Its gradient: dtable[v] = scale * (sum of dout[t] over the tokens with ids[t] = v), stored (rows without a token as zeros), or added into with accumulate (those rows are
+ * not touched, and a row's sum is added in one addition).  Sums are FP32 in a fixed order.
+ *   dout       [tokens, cols] of type dtype
+ *   dtable     FP32 [vocab, cols]
+ *   workspace  device, 16-byte aligned, nvfp4_embedding_workspace_bytes
+ */
+int nvfp4_embedding_workspace_bytes(int64_t tokens, int64_t vocab, int64_t cols, size_t* workspace_bytes);
+int nvfp4_embedding_backward(const void* dout, int dtype, int64_t ldd, const void* ids, int index_type, int64_t tokens, int64_t vocab, int64_t cols, float scale,
+                             float* dtable, int64_t ldt, int accumulate, void* workspace, size_t workspace_bytes, nvfp4_stream_t stream);
+
+/*
+ * Log probabilities, with p = softmax(scale * logits) over each row:
+ *   logits       [rows, cols] of type dtype;  scale  > 0 and finite: the reciprocal of a temperature
+ *   targets      token numbers [rows], or NULL
+ *   logprob      FP32 [rows]: ln p[target], 0 where the target is outside [0, cols); or NULL
+ *   stats        FP32 [rows, 2]: the row's largest logit m, and ln sum exp(scale (logit - m)), for nvfp4_logprob_backward; or NULL.  They are kept apart because their
+ *                sum loses the second where the first is large.
+ *   lse          FP32 [rows]: scale m + the logarithm; or NULL
+ *   entropy      FP32 [rows]: -sum p ln p; or NULL
+ *   top          0 to 32, at most cols: the `top` largest logits of each row in descending order, of equal ones those with the lowest columns:
+ *                columns to top_index int32 [rows, top], log probabilities to top_logprob FP32 [rows, top]
+ *   workspace    device, 16-byte aligned, nvfp4_logprob_workspace_bytes; may be 0
+ * Logits of -infinity have probability 0.  A row that holds nothing else has no distribution: its log probabilities and lse are -infinity, its entropy is 0, and its gradient
+ * is zero.  The type's lowest value is a number like any other: a row of nothing else is uniform.  A row with a NaN or +infinity gives NaN
+ * in all of these but the columns (among which a NaN comes last).
+ */
+int nvfp4_logprob_workspace_bytes(int64_t rows, int64_t cols, int top, size_t* workspace_bytes);
+int nvfp4_logprob_forward(const void* logits, int dtype, int64_t ld, int64_t rows, int64_t cols, float scale, const void* targets, int index_type, float* logprob,
+                          float* stats, float* lse, float* entropy, int top, int32_t* top_index, float* top_logprob, void* workspace, size_t workspace_bytes,
+                          nvfp4_stream_t stream);
+
+/*
+ * Gradient of the logits from those of logprob, lse and entropy (FP32 [rows]; each may be NULL):
+ *   dlogits[j] = scale (g_logprob [j = target] + p[j] (g_lse - g_logprob - g_entropy (ln p[j] + entropy)))
+ * A target outside [0, cols) takes no g_logprob.  stats, entropy (only with g_entropy) as the forward pass gave them; dlogits of type d_dtype.
+ */
+int nvfp4_logprob_backward(const void* logits, int dtype, int64_t ld, int64_t rows, int64_t cols, float scale, const void* targets, int index_type,
+                           const float* stats, const float* g_logprob, const float* g_lse, const float* g_entropy, const float* entropy, void* dlogits,
+                           int d_dtype, int64_t ldd, nvfp4_stream_t stream);
+
+/*
+ * Both for a loss whose gradient by the log probabilities is known beforehand (a mean over tokens): the same results as nvfp4_logprob_forward and
+ * nvfp4_logprob_backward with g_logprob, with the logits read from memory once where they allow it.  stats must not be NULL; workspace: nvfp4_logprob_workspace_bytes with top = 0.
+ */
+int nvfp4_logprob_with_gradient(const void* logits, int dtype, int64_t ld, int64_t rows, int64_t cols, float scale, const void* targets, int index_type,
+                                const float* g_logprob, float* logprob, float* stats, float* lse, void* dlogits, int d_dtype, int64_t ldd, void* workspace,
+                                size_t workspace_bytes, nvfp4_stream_t stream);
+
+/*
+ * The gradients of a model, for their common norm and for clipping.
+ *   data       [rows, cols] of type dtype, leading dimension ld (any, at least cols), aligned to its element; the fastest are contiguous or have rows that start at multiples of 16 bytes
+ *   out        where the clipped gradient goes, of type out_dtype, leading dimension ld_out; NULL: to data.  Results do not overlap each other or another tensor's data;
+ *              equal places are refused
+ * Any rows and cols, 0 included; a vector is one row.  At most 2^20 tensors and 2^40 elements.
+ */
+typedef struct nvfp4_grad {
+  const void* data;
+  void* out;
+  int64_t rows, cols, ld, ld_out;
+  int32_t dtype, out_dtype;
+} nvfp4_grad;
+
+/*
+ * The list is laid out once and serves every step that uses the same buffers: nvfp4_grad_list_build fills table_host (host memory, 8-byte aligned, nvfp4_grad_list_sizes bytes), the caller copies it
+ * to device memory (16-byte aligned) and sets `table` to that.  Caller-owned, like everything here.
+ */
+typedef struct nvfp4_grad_list {
+  int64_t tensors, units;
+  const void* table;
+} nvfp4_grad_list;
+int nvfp4_grad_list_sizes(const nvfp4_grad* tensors, int64_t n, size_t* table_bytes, size_t* workspace_bytes);
+int nvfp4_grad_list_build(const nvfp4_grad* tensors, int64_t n, void* table_host, size_t table_bytes, nvfp4_grad_list* list);
+
+/*
+ * nvfp4_grad_sumsq: *sumsq = the sum of all squares, binary64, in a fixed order; device memory, as is the workspace (16-byte aligned, nvfp4_grad_list_sizes bytes).
+ * nvfp4_grad_clip:  norm = sqrt(*sumsq);  out = data * (norm > max_norm ? max_norm / norm : 1).  norm: device FP32, or NULL; max_norm >= 0, infinity for the norm alone.
+ * Two calls, so that the sums of several lists or of other GPUs' shards can be added in between.  A norm that is not finite leaves the values as they are; a gradient in its place that needs no
+ * clipping is not read.
+ */
+int nvfp4_grad_sumsq(const nvfp4_grad_list* list, double* sumsq, void* workspace, size_t workspace_bytes, nvfp4_stream_t stream);
+int nvfp4_grad_clip(const nvfp4_grad_list* list, const double* sumsq, float max_norm, float* norm, nvfp4_stream_t stream);
+
 /* 16-bit sign diagonal for a seed: bit i set means s_i = -1 (App. C). */
 uint32_t nvfp4_rht_sign_mask(uint64_t rht_seed);
 

@@ -28,13 +28,16 @@ OUT_F32, OUT_BF16, OUT_F32_ACCUMULATE = 0, 1, 2
 COPY_ROW, COPY_COL = 0, 1
 ACT_NONE, ACT_RELU2, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 NORM_KEEP_NORMALIZED, NORM_KEEP_OUTPUT = 0, 1
+INDEX_I32, INDEX_I64 = 0, 1
 
 EXPORTS = ["nvfp4_quantized_sizes", "nvfp4_quantize", "nvfp4_gemm", "nvfp4_gemm_workspace_bytes", "nvfp4_dequantize",
            "nvfp4_rht_sign_mask", "nvfp4_selftest_conversions", "nvfp4_status_string", "nvfp4_version",
            "nvfp4_linear_workspace_bytes", "nvfp4_linear_forward", "nvfp4_linear_backward",
            "nvfp4_amax", "nvfp4_quantize_with_amax", "nvfp4_quantize_static", "nvfp4_predecode",
            "nvfp4_checkpoint_sizes", "nvfp4_checkpoint_save", "nvfp4_checkpoint_load", "nvfp4_rmsnorm_forward", "nvfp4_rmsnorm_backward",
-           "nvfp4_activation_backward", "nvfp4_rowsum_workspace_bytes", "nvfp4_gemm_epilogue"]
+           "nvfp4_activation_backward", "nvfp4_rowsum_workspace_bytes", "nvfp4_gemm_epilogue",
+           "nvfp4_embedding_forward", "nvfp4_embedding_workspace_bytes", "nvfp4_embedding_backward", "nvfp4_logprob_workspace_bytes", "nvfp4_logprob_forward",
+           "nvfp4_logprob_backward", "nvfp4_logprob_with_gradient", "nvfp4_grad_list_sizes", "nvfp4_grad_list_build", "nvfp4_grad_sumsq", "nvfp4_grad_clip"]
 STATIC_SCRATCH_BYTES = 1 << 20
 
 
@@ -60,6 +63,17 @@ class EpilogueStruct(ctypes.Structure):
     """Mirror of ``nvfp4_epilogue``."""
     _fields_ = [("bias", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64), ("keep", ctypes.POINTER(CheckpointStruct)),
                 ("grad_of", ctypes.POINTER(CheckpointStruct)), ("residual_dtype", ctypes.c_int32), ("activation", ctypes.c_int32)]
+
+
+class GradStruct(ctypes.Structure):
+    """Mirror of ``nvfp4_grad``."""
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64),
+                ("ld_out", ctypes.c_int64), ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32)]
+
+
+class GradListStruct(ctypes.Structure):
+    """Mirror of ``nvfp4_grad_list``."""
+    _fields_ = [("tensors", ctypes.c_int64), ("units", ctypes.c_int64), ("table", ctypes.c_void_p)]
 
 
 _lib = None
@@ -123,6 +137,17 @@ def load_library() -> ctypes.CDLL:
         L.nvfp4_gemm_epilogue.argtypes = [qp, qp, ci, ctypes.POINTER(EpilogueStruct), vp, ci, i64, vp, ctypes.c_size_t, vp]
         L.nvfp4_rowsum_workspace_bytes.restype = ci
         L.nvfp4_rowsum_workspace_bytes.argtypes = [i64, i64, vp]
+        sz, gp, lp = ctypes.c_size_t, ctypes.POINTER(GradStruct), ctypes.POINTER(GradListStruct)
+        logits = [vp, ci, i64, i64, i64, cf, vp, ci]
+        for name, args in (("embedding_forward", [vp, ci, i64, vp, ci, i64, i64, i64, cf, vp, ci, i64, vp]), ("embedding_workspace_bytes", [i64, i64, i64, vp]),
+                           ("embedding_backward", [vp, ci, i64, vp, ci, i64, i64, i64, cf, vp, i64, ci, vp, sz, vp]),
+                           ("logprob_workspace_bytes", [i64, i64, ci, vp]), ("logprob_forward", logits + [vp, vp, vp, vp, ci, vp, vp, vp, sz, vp]),
+                           ("logprob_backward", logits + [vp, vp, vp, vp, vp, vp, ci, i64, vp]),
+                           ("logprob_with_gradient", logits + [vp, vp, vp, vp, vp, ci, i64, vp, sz, vp]),
+                           ("grad_list_sizes", [gp, i64, vp, vp]), ("grad_list_build", [gp, i64, vp, sz, lp]), ("grad_sumsq", [lp, vp, vp, sz, vp]),
+                           ("grad_clip", [lp, vp, cf, vp, vp])):
+            f = getattr(L, "nvfp4_" + name)
+            f.restype, f.argtypes = ci, args
         L.nvfp4_status_string.restype = ctypes.c_char_p
         L.nvfp4_status_string.argtypes = [ci]
         L.nvfp4_version.restype = ci
@@ -647,6 +672,227 @@ def nvfp4_gemm_epilogue(a: QTensor, b: QTensor, op: int, bias: Optional[torch.Te
     ws_ptr, ws_bytes = (workspace.data_ptr(), workspace.numel()) if workspace is not None else (None, 0)
     _check(load_library().nvfp4_gemm_epilogue(ctypes.byref(a.desc), ctypes.byref(b.desc), op, ctypes.byref(e), op_, out_dtype, ldd, ws_ptr, ws_bytes, _stream()))
     return out
+
+
+# ---------------------------------------------------------------- the ends of a training step
+
+_INDEX = {torch.int32: INDEX_I32, torch.int64: INDEX_I64}
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _here(*tensors) -> None:
+    """Kernels go to the current device's stream: tensors of another device are refused."""
+    device = _current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"a tensor on {t.device}, with device {device} current")
+
+
+def _indices(t: torch.Tensor, n: Optional[int], what: str):
+    kind, size = _INDEX.get(t.dtype), t.shape
+    if kind is None or len(size) != 1 or (n is not None and size[0] != n) or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 or int64 CUDA tensor" + (f" of {n} elements" if n is not None else " of one dimension"))
+    return kind, t.data_ptr()
+
+
+def nvfp4_embedding_forward(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0, out_dtype: Optional[int] = None,
+                            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """scale * table[ids], zeros for an id outside the table.  ids: int32 or int64 [tokens].  out_dtype: default the table's."""
+    _here(ids, table, out)
+    kind, ip = _indices(ids, None, "ids")
+    dt, tp, ldt = _matrix(table, "table")
+    tokens, (vocab, cols) = ids.shape[0], table.shape
+    if out is None:
+        ot = dt if out_dtype is None else out_dtype
+        out = torch.empty(tokens, cols, dtype=_TORCH[ot], device=table.device)
+        op, ldo = out.data_ptr(), cols
+    else:
+        ot, op, ldo = _matrix(out, "out", (tokens, cols))
+        if out_dtype is not None and ot != out_dtype:
+            raise ValueError("out must be of type out_dtype")
+    _check(load_library().nvfp4_embedding_forward(ip, kind, tokens, tp, dt, vocab, cols, ldt, scale, op, ot, ldo, _stream()))
+    return out
+
+
+@functools.lru_cache(maxsize=1024)
+def embedding_workspace_bytes(tokens: int, vocab: int, cols: int) -> int:
+    w = ctypes.c_size_t()
+    _check(load_library().nvfp4_embedding_workspace_bytes(tokens, vocab, cols, ctypes.addressof(w)))
+    return w.value
+
+
+def _scratch(workspace: Optional[torch.Tensor], need: int, device):
+    """Address and size of scratch memory, and what keeps it alive."""
+    if workspace is None:
+        return _workspace(device, need) if need else (None, 0, None)
+    _here(workspace)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def nvfp4_embedding_backward(dout: torch.Tensor, ids: torch.Tensor, vocab: Optional[int] = None, scale: float = 1.0, dtable: Optional[torch.Tensor] = None,
+                             accumulate: bool = False, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The table's gradient, float32 [vocab, cols]: scale * the sum of dout over each row's tokens; added into dtable with accumulate."""
+    _here(dout, ids, dtable)
+    dt, dp, ldd = _matrix(dout, "dout")
+    tokens, cols = dout.shape
+    kind, ip = _indices(ids, tokens, "ids")
+    if dtable is None:
+        if accumulate or vocab is None:
+            raise ValueError("accumulate needs dtable" if accumulate else "either vocab or dtable is needed")
+        dtable = torch.empty(vocab, cols, dtype=torch.float32, device=dout.device)
+        gp, ldt = dtable.data_ptr(), cols
+    else:
+        vocab = dtable.shape[0] if vocab is None else vocab
+        gt, gp, ldt = _matrix(dtable, "dtable", (vocab, cols))
+        if gt != OUT_F32:
+            raise ValueError("dtable must be float32")
+    ws, ws_bytes, workspace = _scratch(workspace, embedding_workspace_bytes(tokens, vocab, cols), dout.device)
+    _check(load_library().nvfp4_embedding_backward(dp, dt, ldd, ip, kind, tokens, vocab, cols, scale, gp, ldt, int(accumulate), ws, ws_bytes, _stream()))
+    return dtable
+
+
+class LogProbs(NamedTuple):
+    logprob: Optional[torch.Tensor]       # of the targets, float32 [rows]
+    lse: torch.Tensor                     # float32 [rows]
+    stats: torch.Tensor                   # float32 [rows, 2], for nvfp4_logprob_backward
+    entropy: Optional[torch.Tensor] = None
+    top_index: Optional[torch.Tensor] = None      # int32 [rows, top]
+    top_logprob: Optional[torch.Tensor] = None    # float32 [rows, top]
+    dlogits: Optional[torch.Tensor] = None
+
+
+@functools.lru_cache(maxsize=1024)
+def logprob_workspace_bytes(rows: int, cols: int, top: int = 0) -> int:
+    w = ctypes.c_size_t()
+    _check(load_library().nvfp4_logprob_workspace_bytes(rows, cols, top, ctypes.addressof(w)))
+    return w.value
+
+
+def nvfp4_logprob_forward(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, scale: float = 1.0, entropy: bool = False, top: int = 0,
+                          workspace: Optional[torch.Tensor] = None) -> LogProbs:
+    """ln softmax(scale * logits) at the targets (0 where a target is outside the row), with what else is asked for: see LogProbs."""
+    _here(logits, targets)
+    dt, zp, ld = _matrix(logits, "logits")
+    (rows, cols), device = logits.shape, logits.device
+    if ld % 8 and rows == 1:
+        ld = -(-cols // 8) * 8      # (a row alone may be of any length)
+    kind, tp = (INDEX_I64, None) if targets is None else _indices(targets, rows, "targets")
+    ws, ws_bytes, workspace = _scratch(workspace, logprob_workspace_bytes(rows, cols, top), device)
+    f32 = lambda *size: torch.empty(*size, dtype=torch.float32, device=device)
+    r = LogProbs(None if targets is None else f32(rows), f32(rows), f32(rows, 2), f32(rows) if entropy else None,
+                 torch.empty(rows, top, dtype=torch.int32, device=device) if top else None, f32(rows, top) if top else None)
+    _check(load_library().nvfp4_logprob_forward(zp, dt, ld, rows, cols, scale, tp, kind, *[None if t is None else t.data_ptr() for t in (r.logprob, r.stats, r.lse, r.entropy)],
+                                                top, *[None if t is None else t.data_ptr() for t in (r.top_index, r.top_logprob)], ws, ws_bytes, _stream()))
+    return r
+
+
+def _dlogits(logits: torch.Tensor, dt: int, out_dtype: Optional[int], out: Optional[torch.Tensor]):
+    rows, cols = logits.shape
+    if out is None:
+        ot, ld = dt if out_dtype is None else out_dtype, -(-cols // 8) * 8
+        out = torch.empty(rows, ld, dtype=_TORCH[ot], device=logits.device)
+        return (out if ld == cols else out[:, :cols]), ot, out.data_ptr(), ld
+    ot, op, ldd = _matrix(out, "out", (rows, cols))
+    if out_dtype is not None and ot != out_dtype:
+        raise ValueError("out must be of type out_dtype")
+    return out, ot, op, -(-cols // 8) * 8 if rows == 1 else ldd
+
+
+def nvfp4_logprob_backward(logits: torch.Tensor, targets: Optional[torch.Tensor], stats: torch.Tensor, g_logprob: Optional[torch.Tensor] = None,
+                           g_lse: Optional[torch.Tensor] = None, g_entropy: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None, scale: float = 1.0,
+                           out_dtype: Optional[int] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient of the logits from those of logprob, lse and entropy (float32 [rows] each).  stats, and entropy with g_entropy, are the forward pass's.
+    out: may be the logits.  A result that is allocated here has rows at multiples of 8 elements."""
+    _here(logits, targets, stats, g_logprob, g_lse, g_entropy, entropy, out)
+    dt, zp, ld = _matrix(logits, "logits")
+    rows, cols = logits.shape
+    kind, tp = (INDEX_I64, None) if targets is None else _indices(targets, rows, "targets")
+    if stats.dtype != torch.float32 or stats.shape != (rows, 2) or not stats.is_contiguous():
+        raise ValueError("stats must be what the forward pass gave: contiguous float32 [rows, 2]")
+    if ld % 8 and rows == 1:
+        ld = -(-cols // 8) * 8
+    g = [_vector(t, rows, what) for t, what in ((g_logprob, "g_logprob"), (g_lse, "g_lse"), (g_entropy, "g_entropy"), (entropy, "entropy"))]
+    out, ot, op, ldd = _dlogits(logits, dt, out_dtype, out)
+    _check(load_library().nvfp4_logprob_backward(zp, dt, ld, rows, cols, scale, tp, kind, stats.data_ptr(), *g, op, ot, ldd, _stream()))
+    return out
+
+
+def nvfp4_logprob_with_gradient(logits: torch.Tensor, targets: torch.Tensor, g_logprob: torch.Tensor, scale: float = 1.0, out_dtype: Optional[int] = None,
+                                out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> LogProbs:
+    """Log probabilities of the targets and, for a gradient of theirs that is known beforehand (-1 / tokens for a mean loss), that of the logits in one go."""
+    _here(logits, targets, g_logprob, out)
+    dt, zp, ld = _matrix(logits, "logits")
+    (rows, cols), device = logits.shape, logits.device
+    if ld % 8 and rows == 1:
+        ld = -(-cols // 8) * 8
+    kind, tp = _indices(targets, rows, "targets")
+    gp = _vector(g_logprob, rows, "g_logprob")
+    out, ot, op, ldd = _dlogits(logits, dt, out_dtype, out)
+    ws, ws_bytes, workspace = _scratch(workspace, logprob_workspace_bytes(rows, cols), device)
+    logprob, lse = torch.empty(rows, dtype=torch.float32, device=device), torch.empty(rows, dtype=torch.float32, device=device)
+    stats = torch.empty(rows, 2, dtype=torch.float32, device=device)
+    _check(load_library().nvfp4_logprob_with_gradient(zp, dt, ld, rows, cols, scale, tp, kind, gp, logprob.data_ptr(), stats.data_ptr(), lse.data_ptr(), op, ot, ldd,
+                                                      ws, ws_bytes, _stream()))
+    return LogProbs(logprob, lse, stats, dlogits=out)
+
+
+class Gradients:
+    """The gradients of a model as one list, laid out on the device once for all steps that use these tensors: float32 or bf16, contiguous of any shape, or
+    2-D with contiguous rows.  outs: where the clipped ones go (same shapes, any of the two types); default: in their place."""
+    __slots__ = ("tensors", "outs", "desc", "ref", "table", "workspace_bytes", "device")
+
+    def __init__(self, tensors, outs=None):
+        self.tensors, self.outs = list(tensors), None if outs is None else list(outs)
+        if self.outs is not None and len(self.outs) != len(self.tensors):
+            raise ValueError("there must be as many outs as tensors")
+        for t in self.tensors + (self.outs or []):
+            if t.dtype not in _DTYPES or not t.is_cuda or not (t.is_contiguous() or (t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1))):
+                raise ValueError("gradients must be float32 or bf16 CUDA tensors, contiguous or 2-D with contiguous rows")
+            if t.is_cuda and t.device != self.tensors[0].device:
+                raise ValueError("gradients must be on one device")
+        array = (GradStruct * max(len(self.tensors), 1))()
+        for i, t in enumerate(self.tensors):
+            o = t if self.outs is None else self.outs[i]
+            if o.shape != t.shape:
+                raise ValueError("an out must have its tensor's shape")
+            one = t.is_contiguous() and o.is_contiguous()
+            rows, cols = (1, t.numel()) if one else t.shape
+            lds = [cols if v.is_contiguous() else v.stride(0) for v in (t, o)]
+            array[i] = GradStruct(t.data_ptr(), None if self.outs is None else o.data_ptr(), rows, cols, *lds, _DTYPES[t.dtype], _DTYPES[o.dtype])
+        table, ws = ctypes.c_size_t(), ctypes.c_size_t()
+        n, self.desc = len(self.tensors), GradListStruct()
+        _check(load_library().nvfp4_grad_list_sizes(array, n, ctypes.addressof(table), ctypes.addressof(ws)))
+        host = torch.zeros(max(table.value, 16), dtype=torch.uint8)
+        _check(load_library().nvfp4_grad_list_build(array, n, host.data_ptr(), host.numel(), ctypes.byref(self.desc)))
+        self.device = self.tensors[0].device if n else torch.device("cuda", _current_device())
+        self.table, self.workspace_bytes = host.to(self.device), ws.value
+        self.desc.table = self.table.data_ptr()
+        self.ref = ctypes.byref(self.desc)
+
+
+def nvfp4_grad_sumsq(gradients: Gradients, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The sum of all squares, float64 [1].  Sums of several lists, or of other GPUs' shards, may be added before nvfp4_grad_clip."""
+    _here(gradients.table, out)
+    if out is None:
+        out = torch.empty(1, dtype=torch.float64, device=gradients.device)
+    elif out.dtype != torch.float64 or out.numel() != 1:
+        raise ValueError("out must be a float64 CUDA tensor of one element")
+    ws, ws_bytes, workspace = _scratch(workspace, gradients.workspace_bytes, gradients.device)
+    _check(load_library().nvfp4_grad_sumsq(gradients.ref, out.data_ptr(), ws, ws_bytes, _stream()))
+    return out
+
+
+def nvfp4_grad_clip(gradients: Gradients, sumsq: torch.Tensor, max_norm: float, norm: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Scales the gradients so that their norm, the root of sumsq, is at most max_norm; returns the norm, float32 [1]."""
+    _here(gradients.table, sumsq, norm)
+    if sumsq.dtype != torch.float64 or sumsq.numel() != 1:
+        raise ValueError("sumsq must be a float64 CUDA tensor of one element")
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device=gradients.device)
+    elif norm.dtype != torch.float32 or norm.numel() != 1:
+        raise ValueError("norm must be a float32 CUDA tensor of one element")
+    _check(load_library().nvfp4_grad_clip(gradients.ref, sumsq.data_ptr(), max_norm, norm.data_ptr(), _stream()))
+    return norm
 
 
 def nvfp4_selftest_conversions() -> list:

@@ -3,6 +3,8 @@
 #include "nvfp4.h"
 #include "nvfp4_internal.h"
 
+#include <algorithm>
+
 // Scratch of nvfp4_quantize_static, the entry point for callers that cannot allocate: the quantizer's workspace (the
 // amax pass's per-workgroup maxima and their fold) in device memory that belongs to the library's code object.  Every
 // GPU the library runs on holds its own copy of this array, at its own address, until the process ends.  In host
@@ -673,6 +675,294 @@ int nvfp4_internal_gemm_epilogue_direct(const nvfp4_qtensor* a, const nvfp4_qten
   if (rc != NVFP4_OK) return rc;
   if (g.mx) return NVFP4_ERR_INVALID_ARG;
   return launch_gemm_direct(g, shape, static_cast<hipStream_t>(stream)) == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
+}
+
+// ---------------------------------------------------------------- the ends of a training step
+
+namespace {
+
+constexpr int64_t kMostTokens = 0x3fffffff, kMostGrads = 1 << 20;
+constexpr int kMostAlternatives = 32;
+constexpr int64_t kUnitElements = 8192, kMostUnitElements = 1 << 24, kUnits = 4096;
+
+bool index_kind(int t) { return t == NVFP4_INDEX_I32 || t == NVFP4_INDEX_I64; }
+bool is_finite(float v) { return v - v == 0.0f; }
+
+// Token numbers that have to be there (unless there are none of them).
+int check_index(const void* p, int type, int64_t n, bool may_be_null) {
+  if (!p) return may_be_null || n == 0 ? NVFP4_OK : NVFP4_ERR_INVALID_ARG;
+  return aligned(p, type == NVFP4_INDEX_I64 ? 8 : 4) ? NVFP4_OK : NVFP4_ERR_INVALID_ARG;
+}
+
+int check_workspace(const void* workspace, size_t bytes, size_t need) {
+  return need && (!workspace || !aligned(workspace, 16) || bytes < need) ? NVFP4_ERR_WORKSPACE : NVFP4_OK;
+}
+
+int check_embedding(int64_t tokens, int64_t vocab, int64_t cols) {
+  if (tokens < 0 || tokens > kMostTokens || vocab <= 0 || vocab >= 0x7fffffff) return NVFP4_ERR_BAD_SHAPE;
+  return cols > 0 && cols <= kMostNormCols && cols % 16 == 0 ? NVFP4_OK : NVFP4_ERR_BAD_SHAPE;
+}
+
+// (columns of any number: a vocabulary need not be a multiple of anything)
+bool logits_shape(int64_t rows, int64_t cols) { return rows >= 0 && rows <= 0x7fffffff && cols > 0 && cols < 0x40000000; }
+
+int check_logits(const void* logits, int dtype, int64_t ld, int64_t rows, int64_t cols, float scale, const void* targets, int index_type) {
+  if (!element_type(dtype) || !index_kind(index_type) || !is_finite(scale) || !(scale > 0.0f)) return NVFP4_ERR_INVALID_ARG;
+  if (!logits_shape(rows, cols)) return NVFP4_ERR_BAD_SHAPE;
+  const int rc = check_tensor(logits, rows, cols, ld, false);
+  return rc == NVFP4_OK ? check_index(targets, index_type, rows, true) : rc;
+}
+
+void fill_forward(LogprobForward& a, const void* logits, int dtype, int64_t ld, int64_t rows, int64_t cols, float scale, const void* targets, int index_type,
+                  float* logprob, float* stats, float* lse) {
+  a.z = logits, a.targets = targets;
+  a.rows = rows, a.cols = cols, a.ld = ld, a.scale = scale;
+  a.bf16 = dtype == NVFP4_OUT_BF16, a.i64 = index_type == NVFP4_INDEX_I64;
+  a.logprob = logprob, a.stats = stats, a.lse = lse;
+}
+
+void fill_backward(LogprobBackward& a, const void* logits, int dtype, int64_t ld, int64_t rows, int64_t cols, float scale, const void* targets, int index_type,
+                   const float* stats, const float* g_logprob, void* dlogits, int d_dtype, int64_t ldd) {
+  a.z = logits, a.targets = targets, a.stats = stats, a.g_logprob = g_logprob, a.dz = dlogits;
+  a.rows = rows, a.cols = cols, a.ld = ld, a.ldd = ldd, a.scale = scale;
+  a.bf16 = dtype == NVFP4_OUT_BF16, a.out_bf16 = d_dtype == NVFP4_OUT_BF16, a.i64 = index_type == NVFP4_INDEX_I64;
+}
+
+int64_t grad_elements(const nvfp4_grad& g) { return g.rows * g.cols; }
+size_t element_size(int dtype) { return dtype == NVFP4_OUT_BF16 ? 2 : 4; }
+
+int check_grads(const nvfp4_grad* g, int64_t n) {
+  if (n < 0 || n > kMostGrads || (n && !g)) return NVFP4_ERR_INVALID_ARG;
+  int64_t total = 0;
+  for (int64_t i = 0; i < n; ++i) {
+    if (!element_type(g[i].dtype) || !element_type(g[i].out_dtype)) return NVFP4_ERR_INVALID_ARG;
+    if (g[i].rows < 0 || g[i].rows > 0x7fffffff || g[i].cols < 0 || g[i].cols > (int64_t{1} << 40)) return NVFP4_ERR_BAD_SHAPE;
+    if (g[i].cols && g[i].rows > (int64_t{1} << 40) / g[i].cols) return NVFP4_ERR_BAD_SHAPE;
+    if (grad_elements(g[i]) == 0) continue;
+    if ((total += grad_elements(g[i])) > (int64_t{1} << 40)) return NVFP4_ERR_BAD_SHAPE;
+    if (g[i].rows > 1 && (g[i].ld < g[i].cols || g[i].ld > (int64_t{1} << 40))) return NVFP4_ERR_BAD_SHAPE;
+    if (!g[i].data || !aligned(g[i].data, element_size(g[i].dtype))) return NVFP4_ERR_INVALID_ARG;
+    if (!g[i].out) {
+      if (g[i].out_dtype != g[i].dtype) return NVFP4_ERR_INVALID_ARG;
+      continue;
+    }
+    if (g[i].rows > 1 && (g[i].ld_out < g[i].cols || g[i].ld_out > (int64_t{1} << 40))) return NVFP4_ERR_BAD_SHAPE;
+    if (!aligned(g[i].out, element_size(g[i].out_dtype))) return NVFP4_ERR_INVALID_ARG;
+    if (g[i].out == g[i].data && (g[i].out_dtype != g[i].dtype || (g[i].rows > 1 && g[i].ld_out != g[i].ld))) return NVFP4_ERR_INVALID_ARG;
+  }
+  return NVFP4_OK;
+}
+
+// Elements of a unit of work: so many that some 4096 units hold everything, and no fewer than keep a workgroup busy.
+int64_t unit_elements(const nvfp4_grad* g, int64_t n) {
+  int64_t total = 0;
+  for (int64_t i = 0; i < n; ++i) total += grad_elements(g[i]);
+  const int64_t each = (total / kUnits + kUnitElements - 1) / kUnitElements * kUnitElements;
+  return each < kUnitElements ? kUnitElements : each > kMostUnitElements ? kMostUnitElements : each;
+}
+
+GradTensor grad_tensor(const nvfp4_grad& g, int64_t each) {
+  GradTensor t{};
+  t.data = g.data, t.out = g.out ? g.out : const_cast<void*>(g.data);
+  const int out_dtype = g.out_dtype;
+  const int64_t ld_out = g.out ? g.ld_out : g.ld;
+  if (g.rows == 1 || (g.ld == g.cols && ld_out == g.cols)) {
+    t.rows = 1, t.cols = grad_elements(g), t.ld = t.ld_out = t.cols;
+  } else {
+    t.rows = static_cast<int32_t>(g.rows), t.cols = g.cols, t.ld = g.ld, t.ld_out = ld_out;
+  }
+  t.unit_cols = static_cast<int32_t>(t.cols < each ? t.cols : each);
+  const int64_t rows = t.cols < each ? each / t.cols : 1;
+  t.unit_rows = static_cast<int32_t>(rows < t.rows ? rows : t.rows);
+  const size_t in = element_size(g.dtype), to = element_size(out_dtype);
+  const bool wide = aligned(t.data, 16) && aligned(t.out, 16) &&
+                    (t.rows == 1 || (t.ld * static_cast<int64_t>(in) % 16 == 0 && t.ld_out * static_cast<int64_t>(to) % 16 == 0));
+  t.flags = (in == 2 ? kGradBf16 : 0) | (to == 2 ? kGradOutBf16 : 0) | (wide ? kGradWide : 0);
+  return t;
+}
+
+int64_t units_of(const GradTensor& t) { return ((t.rows + t.unit_rows - 1) / t.unit_rows) * ((t.cols + t.unit_cols - 1) / t.unit_cols); }
+
+int64_t grad_units(const nvfp4_grad* g, int64_t n) {
+  const int64_t each = unit_elements(g, n);
+  int64_t units = 0;
+  for (int64_t i = 0; i < n; ++i)
+    if (grad_elements(g[i])) units += units_of(grad_tensor(g[i], each));
+  return units;
+}
+
+size_t grad_table_bytes(int64_t n, int64_t units) { return static_cast<size_t>(n) * sizeof(GradTensor) + static_cast<size_t>(units) * 4; }
+
+int check_list(const nvfp4_grad_list* list) {
+  if (!list || list->tensors < 0 || list->units < 0 || list->tensors > kMostGrads || list->units > 0xffffff) return NVFP4_ERR_INVALID_ARG;
+  return list->units && (!list->table || !aligned(list->table, 16)) ? NVFP4_ERR_INVALID_ARG : NVFP4_OK;
+}
+const GradTensor* tensors_of(const nvfp4_grad_list* list) { return static_cast<const GradTensor*>(list->table); }
+const int32_t* map_of(const nvfp4_grad_list* list) { return reinterpret_cast<const int32_t*>(tensors_of(list) + list->tensors); }
+
+}  // namespace
+
+int nvfp4_embedding_forward(const void* ids, int index_type, int64_t tokens, const void* table, int table_dtype, int64_t vocab, int64_t cols, int64_t ldt,
+                            float scale, void* out, int out_dtype, int64_t ldo, nvfp4_stream_t stream) {
+  if (!index_kind(index_type) || !element_type(table_dtype) || !element_type(out_dtype) || !is_finite(scale)) return NVFP4_ERR_INVALID_ARG;
+  int rc = check_embedding(tokens, vocab, cols);
+  if (rc == NVFP4_OK) rc = check_index(ids, index_type, tokens, false);
+  if (rc == NVFP4_OK) rc = check_tensor(table, vocab, cols, ldt, false);
+  if (rc == NVFP4_OK) rc = check_tensor(out, tokens, cols, ldo, false);
+  if (rc != NVFP4_OK) return rc;
+  EmbeddingForward a{};
+  a.ids = ids, a.table = table, a.out = out;
+  a.tokens = tokens, a.vocab = vocab, a.cols = cols, a.ldt = ldt, a.ldo = ldo, a.scale = scale;
+  a.i64 = index_type == NVFP4_INDEX_I64, a.table_bf16 = table_dtype == NVFP4_OUT_BF16, a.out_bf16 = out_dtype == NVFP4_OUT_BF16;
+  return launch_embedding_forward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
+}
+
+int nvfp4_embedding_workspace_bytes(int64_t tokens, int64_t vocab, int64_t cols, size_t* workspace_bytes) {
+  const int rc = check_embedding(tokens, vocab, cols);
+  if (rc != NVFP4_OK) return rc;
+  if (!workspace_bytes) return NVFP4_ERR_INVALID_ARG;
+  *workspace_bytes = embedding_workspace_bytes(tokens, vocab, cols);
+  return NVFP4_OK;
+}
+
+int nvfp4_embedding_backward(const void* dout, int dtype, int64_t ldd, const void* ids, int index_type, int64_t tokens, int64_t vocab, int64_t cols, float scale,
+                             float* dtable, int64_t ldt, int accumulate, void* workspace, size_t workspace_bytes, nvfp4_stream_t stream) {
+  if (!index_kind(index_type) || !element_type(dtype) || !is_finite(scale)) return NVFP4_ERR_INVALID_ARG;
+  int rc = check_embedding(tokens, vocab, cols);
+  if (rc == NVFP4_OK) rc = check_index(ids, index_type, tokens, false);
+  if (rc == NVFP4_OK) rc = check_tensor(dout, tokens, cols, ldd, false);
+  if (rc == NVFP4_OK) rc = check_tensor(dtable, vocab, cols, ldt, false);
+  if (rc == NVFP4_OK) rc = check_workspace(workspace, workspace_bytes, embedding_workspace_bytes(tokens, vocab, cols));
+  if (rc != NVFP4_OK) return rc;
+  EmbeddingBackward a{};
+  a.ids = ids, a.dout = dout, a.dtable = dtable;
+  a.tokens = tokens, a.vocab = vocab, a.cols = cols, a.ldd = ldd, a.ldt = ldt, a.scale = scale;
+  a.i64 = index_type == NVFP4_INDEX_I64, a.bf16 = dtype == NVFP4_OUT_BF16, a.accumulate = accumulate != 0;
+  return launch_embedding_backward(a, workspace, static_cast<hipStream_t>(stream)) == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
+}
+
+int nvfp4_logprob_workspace_bytes(int64_t rows, int64_t cols, int top, size_t* workspace_bytes) {
+  if (!logits_shape(rows, cols) || top < 0 || top > kMostAlternatives || top > cols) return NVFP4_ERR_BAD_SHAPE;
+  if (!workspace_bytes) return NVFP4_ERR_INVALID_ARG;
+  *workspace_bytes = logprob_workspace_bytes(rows, cols, top);
+  return NVFP4_OK;
+}
+
+int nvfp4_logprob_forward(const void* logits, int dtype, int64_t ld, int64_t rows, int64_t cols, float scale, const void* targets, int index_type, float* logprob,
+                          float* stats, float* lse, float* entropy, int top, int32_t* top_index, float* top_logprob, void* workspace, size_t workspace_bytes,
+                          nvfp4_stream_t stream) {
+  int rc = check_logits(logits, dtype, ld, rows, cols, scale, targets, index_type);
+  if (rc != NVFP4_OK) return rc;
+  if (top < 0 || top > kMostAlternatives || top > cols) return NVFP4_ERR_BAD_SHAPE;
+  if ((logprob && !targets && rows) || (top && rows && (!top_index || !top_logprob))) return NVFP4_ERR_INVALID_ARG;
+  if (!aligned(logprob, 4) || !aligned(stats, 4) || !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(top_index, 4) || !aligned(top_logprob, 4))
+    return NVFP4_ERR_INVALID_ARG;
+  rc = check_workspace(workspace, workspace_bytes, logprob_workspace_bytes(rows, cols, top));
+  if (rc != NVFP4_OK) return rc;
+  LogprobForward a{};
+  fill_forward(a, logits, dtype, ld, rows, cols, scale, targets, index_type, logprob, stats, lse);
+  a.entropy = entropy;
+  a.top = top, a.top_index = top_index, a.top_logprob = top_logprob;
+  return launch_logprob_forward(a, workspace, static_cast<hipStream_t>(stream)) == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
+}
+
+int nvfp4_logprob_backward(const void* logits, int dtype, int64_t ld, int64_t rows, int64_t cols, float scale, const void* targets, int index_type,
+                           const float* stats, const float* g_logprob, const float* g_lse, const float* g_entropy, const float* entropy, void* dlogits,
+                           int d_dtype, int64_t ldd, nvfp4_stream_t stream) {
+  int rc = check_logits(logits, dtype, ld, rows, cols, scale, targets, index_type);
+  if (rc != NVFP4_OK) return rc;
+  if (!element_type(d_dtype)) return NVFP4_ERR_INVALID_ARG;
+  rc = check_tensor(dlogits, rows, cols, ldd, false);
+  if (rc != NVFP4_OK) return rc;
+  if (rows && (!stats || (g_logprob && !targets) || (g_entropy && !entropy))) return NVFP4_ERR_INVALID_ARG;
+  if (!aligned(stats, 4) || !aligned(g_logprob, 4) || !aligned(g_lse, 4) || !aligned(g_entropy, 4) || !aligned(entropy, 4)) return NVFP4_ERR_INVALID_ARG;
+  LogprobBackward a{};
+  fill_backward(a, logits, dtype, ld, rows, cols, scale, targets, index_type, stats, g_logprob, dlogits, d_dtype, ldd);
+  a.g_lse = g_lse, a.g_entropy = g_entropy, a.entropy = entropy;
+  return launch_logprob_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
+}
+
+int nvfp4_logprob_with_gradient(const void* logits, int dtype, int64_t ld, int64_t rows, int64_t cols, float scale, const void* targets, int index_type,
+                                const float* g_logprob, float* logprob, float* stats, float* lse, void* dlogits, int d_dtype, int64_t ldd, void* workspace,
+                                size_t workspace_bytes, nvfp4_stream_t stream) {
+  int rc = check_logits(logits, dtype, ld, rows, cols, scale, targets, index_type);
+  if (rc != NVFP4_OK) return rc;
+  if (!element_type(d_dtype)) return NVFP4_ERR_INVALID_ARG;
+  rc = check_tensor(dlogits, rows, cols, ldd, false);
+  if (rc != NVFP4_OK) return rc;
+  if (rows && (!targets || !g_logprob || !stats)) return NVFP4_ERR_INVALID_ARG;
+  if (!aligned(g_logprob, 4) || !aligned(logprob, 4) || !aligned(stats, 4) || !aligned(lse, 4)) return NVFP4_ERR_INVALID_ARG;
+  rc = check_workspace(workspace, workspace_bytes, logprob_workspace_bytes(rows, cols, 0));
+  if (rc != NVFP4_OK) return rc;
+  LogprobForward f{};
+  fill_forward(f, logits, dtype, ld, rows, cols, scale, targets, index_type, logprob, stats, lse);
+  LogprobBackward b{};
+  fill_backward(b, logits, dtype, ld, rows, cols, scale, targets, index_type, stats, g_logprob, dlogits, d_dtype, ldd);
+  return launch_logprob_with_gradient(f, b, workspace, static_cast<hipStream_t>(stream)) == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
+}
+
+int nvfp4_grad_list_sizes(const nvfp4_grad* tensors, int64_t n, size_t* table_bytes, size_t* workspace_bytes) {
+  const int rc = check_grads(tensors, n);
+  if (rc != NVFP4_OK) return rc;
+  const int64_t units = grad_units(tensors, n);
+  if (table_bytes) *table_bytes = grad_table_bytes(n, units);
+  if (workspace_bytes) *workspace_bytes = static_cast<size_t>(units) * 8;
+  return NVFP4_OK;
+}
+
+int nvfp4_grad_list_build(const nvfp4_grad* tensors, int64_t n, void* table_host, size_t table_bytes, nvfp4_grad_list* list) {
+  const int rc = check_grads(tensors, n);
+  if (rc != NVFP4_OK) return rc;
+  const int64_t units = grad_units(tensors, n);
+  if (!list || (n && !table_host) || !aligned(table_host, 8)) return NVFP4_ERR_INVALID_ARG;
+  if (table_bytes < grad_table_bytes(n, units)) return NVFP4_ERR_WORKSPACE;
+  // No element is written for two tensors: first and last byte of each, in order (of one whose rows lie apart its first element, since others may lie between its rows).
+  struct Range {
+    uintptr_t first, end;
+  };
+  Range* ranges = static_cast<Range*>(table_host);
+  int64_t written = 0;
+  for (int64_t i = 0; i < n; ++i) {
+    const nvfp4_grad& g = tensors[i];
+    if (grad_elements(g) == 0) continue;
+    const uintptr_t first = reinterpret_cast<uintptr_t>(g.out ? g.out : g.data);
+    const bool whole = g.rows == 1 || (g.out ? g.ld_out : g.ld) == g.cols;
+    ranges[written++] = Range{first, first + (whole ? static_cast<size_t>(grad_elements(g)) : 1) * element_size(g.out_dtype)};
+  }
+  std::sort(ranges, ranges + written, [](const Range& a, const Range& b) { return a.first < b.first; });
+  for (int64_t i = 1; i < written; ++i) {
+    if (ranges[i].first < ranges[i - 1].end) return NVFP4_ERR_INVALID_ARG;
+  }
+  const int64_t each = unit_elements(tensors, n);
+  GradTensor* t = static_cast<GradTensor*>(table_host);
+  int32_t* map = reinterpret_cast<int32_t*>(t + n);
+  int64_t unit = 0;
+  for (int64_t i = 0; i < n; ++i) {
+    t[i] = GradTensor{};
+    if (grad_elements(tensors[i]) == 0) continue;
+    t[i] = grad_tensor(tensors[i], each);
+    t[i].first_unit = static_cast<int32_t>(unit);
+    for (int64_t u = units_of(t[i]); u > 0; --u) map[unit++] = static_cast<int32_t>(i);
+  }
+  list->tensors = n, list->units = units, list->table = nullptr;
+  return NVFP4_OK;
+}
+
+int nvfp4_grad_sumsq(const nvfp4_grad_list* list, double* sumsq, void* workspace, size_t workspace_bytes, nvfp4_stream_t stream) {
+  int rc = check_list(list);
+  if (rc == NVFP4_OK && (!sumsq || !aligned(sumsq, 8))) rc = NVFP4_ERR_INVALID_ARG;
+  if (rc == NVFP4_OK) rc = check_workspace(workspace, workspace_bytes, static_cast<size_t>(list->units) * 8);
+  if (rc != NVFP4_OK) return rc;
+  const hipError_t e = launch_grad_sumsq(tensors_of(list), map_of(list), list->units, sumsq, static_cast<double*>(workspace), static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
+}
+
+int nvfp4_grad_clip(const nvfp4_grad_list* list, const double* sumsq, float max_norm, float* norm, nvfp4_stream_t stream) {
+  const int rc = check_list(list);
+  if (rc != NVFP4_OK) return rc;
+  if (!sumsq || !aligned(sumsq, 8) || !aligned(norm, 4) || !(max_norm >= 0.0f)) return NVFP4_ERR_INVALID_ARG;
+  const hipError_t e = launch_grad_clip(tensors_of(list), map_of(list), list->units, sumsq, max_norm, norm, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
 }
 
 int nvfp4_selftest_conversions(uint64_t* mismatches, nvfp4_stream_t stream) {

@@ -1,0 +1,435 @@
+// Embedding: rows of a table by token, scaled, and the table's gradient.
+//   forward   out[t] = scale table[id[t]], zeros for an id outside the table
+//   backward  dtable[v] (+)= scale * sum of dout[t] over the tokens t with id[t] = v
+// The gradient sorts the tokens by id (and by position among equal ids), so that every row's sum is taken in a fixed order without atomics and every row is
+// written once.  Sums FP32.  Memory bounds both.
+#include <algorithm>
+
+#include "nvfp4_internal.h"
+#include "checkpoint8.h"
+
+namespace nvfp4 {
+
+namespace {
+
+__device__ __forceinline__ int64_t id_at(const void* ids, bool i64, int64_t t) {
+  return i64 ? static_cast<const int64_t*>(ids)[t] : static_cast<const int32_t*>(ids)[t];
+}
+
+// ---------------------------------------------------------------- forward
+// A workgroup takes 1024 consecutive groups of eight columns, of as many tokens as that is; a thread four of them.
+constexpr int kGroupsEach = 4;
+
+template <bool kTableBf16, bool kOutBf16>
+__global__ __launch_bounds__(256) void embedding_forward_kernel(EmbeddingForward a) {
+  const uint32_t groups = static_cast<uint32_t>(a.cols >> 3);
+  const uint64_t first = static_cast<uint64_t>(blockIdx.x) * (256 * kGroupsEach);
+  const int64_t token0 = a.token0 + static_cast<int64_t>(first / groups);
+  const uint32_t group0 = static_cast<uint32_t>(first % groups);
+  Eight<kTableBf16> x[kGroupsEach];
+  int64_t token[kGroupsEach], id[kGroupsEach];
+  int col[kGroupsEach];
+#pragma unroll
+  for (int u = 0; u < kGroupsEach; ++u) {
+    const uint32_t g = group0 + threadIdx.x + 256u * u;
+    token[u] = token0 + g / groups;
+    col[u] = static_cast<int>(g % groups) * 8;
+    id[u] = token[u] < a.tokens ? id_at(a.ids, a.i64, token[u]) : -1;
+  }
+#pragma unroll
+  for (int u = 0; u < kGroupsEach; ++u) {
+    if (id[u] < 0 || id[u] >= a.vocab) id[u] = -1;
+    else x[u].load(static_cast<const char*>(a.table) + id[u] * a.ldt * (kTableBf16 ? 2 : 4), col[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < kGroupsEach; ++u) {
+    if (token[u] >= a.tokens) continue;
+    float v[8] = {};
+    if (id[u] >= 0) {
+      x[u].get(v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= a.scale;
+    }
+    store8(static_cast<char*>(a.out) + token[u] * a.ldo * (kOutBf16 ? 2 : 4), col[u], kOutBf16, v);
+  }
+}
+
+// ---------------------------------------------------------------- tokens in order of their ids
+// A key is the id, or the number of rows for an id outside the table: those come last and belong to no row.
+__device__ __forceinline__ uint32_t key_of(const void* ids, bool i64, int64_t t, int64_t vocab) {
+  const int64_t id = id_at(ids, i64, t);
+  return static_cast<uint32_t>(id >= 0 && id < vocab ? id : vocab);
+}
+
+// Up to kFewTokens: a token's place is the number of tokens before it, counted.  32 tokens to a workgroup, eight threads to a token; two operations a pair.
+constexpr int kFewTokens = 8192, kTile = 2048;
+
+__global__ __launch_bounds__(256) void rank_kernel(const void* ids, bool i64, int n, int64_t vocab, uint32_t* __restrict__ keys, uint32_t* __restrict__ order) {
+  __shared__ __attribute__((aligned(16))) uint32_t tile[kTile];
+  const int t = static_cast<int>(blockIdx.x) * 32 + (threadIdx.x >> 3), part = threadIdx.x & 7;
+  const uint32_t key = t < n ? key_of(ids, i64, t, vocab) : 0u;
+  uint32_t before = 0u;
+  for (int base = 0; base < n; base += kTile) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < kTile; i += 256) tile[i] = base + i < n ? key_of(ids, i64, base + i, vocab) : 0xFFFFFFFFu;
+    __syncthreads();
+    const int used = min(kTile, n - base);
+    const uint4* four = reinterpret_cast<const uint4*>(tile);
+    if (static_cast<int>(blockIdx.x) * 32 >= base + kTile || base >= static_cast<int>(blockIdx.x) * 32 + 32) {
+      const uint32_t bound = key + (base < t);   // among equal keys those in front come first
+#pragma unroll 4
+      for (int i = part; i * 4 < used; i += 8) {
+        const uint4 k = four[i];
+        before += (k.x < bound) + (k.y < bound) + (k.z < bound) + (k.w < bound);
+      }
+    } else {
+      for (int i = part; i * 4 < used; i += 8) {
+        const uint4 k = four[i];
+        const int at = t - base - i * 4;
+        before += (k.x < key + (at > 0)) + (k.y < key + (at > 1)) + (k.z < key + (at > 2)) + (k.w < key + (at > 3));
+      }
+    }
+  }
+#pragma unroll
+  for (int off = 1; off < 8; off <<= 1) before += __shfl_xor(before, off, 64);
+  if (part == 0 && t < n) keys[before] = key, order[before] = static_cast<uint32_t>(t);
+}
+
+// More: passes over digits of up to nine bits, each stable: count the digits of a tile, sum up, put in place.  A tile of 2048 belongs to a workgroup, whose
+// wavefronts have 512 consecutive keys each.
+constexpr int kMostDigits = 512;
+struct SortPass {
+  const void* ids;                      // first pass: keys are made from these
+  const uint32_t *keys, *order;         // later ones
+  uint32_t *counts, *to_keys, *to_order;
+  int64_t vocab;
+  int n, tiles, shift, digits;
+  bool i64, first;
+};
+
+__device__ __forceinline__ uint32_t sort_key(const SortPass& p, int i) { return p.first ? key_of(p.ids, p.i64, i, p.vocab) : p.keys[i]; }
+
+__global__ __launch_bounds__(256) void sort_count_kernel(SortPass p) {
+  __shared__ uint32_t count[kMostDigits];
+  for (int d = threadIdx.x; d < p.digits; d += 256) count[d] = 0u;
+  __syncthreads();
+  const int base = static_cast<int>(blockIdx.x) * kTile;
+  for (int i = threadIdx.x; i < kTile && base + i < p.n; i += 256) atomicAdd(&count[(sort_key(p, base + i) >> p.shift) & (p.digits - 1)], 1u);
+  __syncthreads();
+  for (int d = threadIdx.x; d < p.digits; d += 256) p.counts[static_cast<int64_t>(d) * p.tiles + blockIdx.x] = count[d];
+}
+
+// counts[i] <- sum of those before; one workgroup.
+__global__ __launch_bounds__(1024) void sort_scan_kernel(uint32_t* counts, int n) {
+  __shared__ uint32_t wave_total[16];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  uint32_t carry = 0u;
+  for (int base = 0; base < n; base += 4096) {
+    uint32_t v[4], sum = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int at = base + t * 4 + i;
+      v[i] = at < n ? counts[at] : 0u;
+      sum += v[i];
+    }
+    uint32_t up = sum;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const uint32_t o = __shfl_up(up, off, 64);
+      if (lane >= off) up += o;
+    }
+    if (lane == 63) wave_total[wave] = up;
+    __syncthreads();
+    uint32_t before = carry + up - sum, total = 0u;
+    for (int w = 0; w < 16; ++w) {
+      if (w < wave) before += wave_total[w];
+      total += wave_total[w];
+    }
+    carry += total;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int at = base + t * 4 + i;
+      if (at < n) counts[at] = before;
+      before += v[i];
+    }
+    __syncthreads();
+  }
+}
+
+__global__ __launch_bounds__(256) void sort_place_kernel(SortPass p) {
+  __shared__ uint32_t next[4][kMostDigits];   // where a wavefront's next key of a digit goes
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  for (int d = threadIdx.x; d < 4 * kMostDigits; d += 256) next[0][d] = 0u;
+  __syncthreads();
+  const int base = static_cast<int>(blockIdx.x) * kTile + wave * 512;
+  uint32_t key[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    const int i = base + r * 64 + lane;
+    key[r] = i < p.n ? sort_key(p, i) : 0u;
+    if (i < p.n) atomicAdd(&next[wave][(key[r] >> p.shift) & (p.digits - 1)], 1u);
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < p.digits; d += 256) {
+    uint32_t at = p.counts[static_cast<int64_t>(d) * p.tiles + blockIdx.x];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t n = next[w][d];
+      next[w][d] = at;
+      at += n;
+    }
+  }
+  __syncthreads();
+  volatile uint32_t* mine = next[wave];   // (a wavefront's own: its LDS operations are done in order)
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    const int i = base + r * 64 + lane;
+    const bool in = i < p.n;
+    const uint32_t digit = (key[r] >> p.shift) & (p.digits - 1);
+    uint64_t same = __ballot(in);
+#pragma unroll
+    for (int b = 0; b < 9; ++b) {
+      const bool bit = (digit >> b) & 1u;
+      const uint64_t with = __ballot(bit);
+      same &= bit ? with : ~with;
+    }
+    const uint64_t below = same & ((uint64_t{1} << lane) - 1);
+    uint32_t to = 0u;
+    if (in) to = mine[digit] + static_cast<uint32_t>(__popcll(below));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (in && below == 0) mine[digit] = to + static_cast<uint32_t>(__popcll(same));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (in) {
+      p.to_keys[to] = key[r];
+      p.to_order[to] = p.first ? static_cast<uint32_t>(i) : p.order[i];
+    }
+  }
+}
+
+// ---------------------------------------------------------------- sums
+struct SumArgs {
+  EmbeddingBackward a;
+  const uint32_t *keys, *order;   // n of them, in order
+  float* partials;                // [chunks, 2, cols]: sum of a chunk's first row if that has begun before, of its last if that goes on behind
+  int n, chunk, chunks, strips;   // strips of 512 columns
+  int zero_groups;                // workgroups that write rows without a token
+};
+
+__device__ __forceinline__ int lower_bound(const uint32_t* keys, int n, uint32_t key) {
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (keys[mid] < key) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
+}
+
+constexpr int kZeroRows = 32, kAhead = 8;
+
+// The first workgroups: a wavefront adds a chunk of consecutive tokens over 512 columns, eight to a lane, and stores each row as it ends.  The rest, where the
+// gradient is stored and not added to: 32 rows each, zeros where no token is.
+template <bool kBf16>
+__global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs s) {
+  const EmbeddingBackward& a = s.a;
+  const int lane = threadIdx.x & 63;
+  const int64_t sums = (static_cast<int64_t>(s.chunks) * s.strips + 3) / 4;
+  if (blockIdx.x >= sums) {
+    for (int64_t row0 = (blockIdx.x - sums) * kZeroRows; row0 < a.vocab; row0 += static_cast<int64_t>(s.zero_groups) * kZeroRows) {
+      bool absent = false;
+      if (lane < kZeroRows && row0 + lane < a.vocab) {
+        const int at = lower_bound(s.keys, s.n, static_cast<uint32_t>(row0 + lane));
+        absent = at == s.n || s.keys[at] != static_cast<uint32_t>(row0 + lane);
+      }
+      for (uint64_t left = __ballot(absent); left; left &= left - 1) {
+        float* to = a.dtable + (row0 + __builtin_ctzll(left)) * a.ldt;
+        for (int64_t col = threadIdx.x * 4; col < a.cols; col += 1024) *reinterpret_cast<float4v*>(to + col) = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+      }
+    }
+    return;
+  }
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (unit >= static_cast<int64_t>(s.chunks) * s.strips) return;
+  const int chunk = static_cast<int>(unit / s.strips), first = chunk * s.chunk, last = min(first + s.chunk, s.n);
+  const int64_t col = static_cast<int64_t>(unit % s.strips) * 512 + lane * 8;
+  const bool in = col < a.cols;
+  const uint32_t vocab = static_cast<uint32_t>(a.vocab);
+  uint32_t key = s.keys[first];
+  const uint32_t behind = last < s.n ? s.keys[last] : 0xFFFFFFFFu;
+  bool begun = first > 0 && s.keys[first - 1] == key;
+  float sum[8] = {};
+  auto finish = [&](bool goes_on) {
+    if (key >= vocab || !in) return;
+    if (begun || goes_on) {
+      store8(s.partials + (static_cast<int64_t>(chunk) * 2 + (begun ? 0 : 1)) * a.cols, col, false, sum);
+      return;
+    }
+    float* row = a.dtable + static_cast<int64_t>(key) * a.ldt;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = a.scale * sum[i];
+    if (a.accumulate) {
+      Eight<false> old;
+      float o[8];
+      old.load(row, col);
+      old.get(o);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += o[i];
+    }
+    store8(row, col, false, v);
+  };
+  for (int at = first; at < last; at += kAhead) {
+    Eight<kBf16> x[kAhead];
+    uint32_t k[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int i = min(at + u, last - 1);
+      k[u] = s.keys[i];
+      if (in && k[u] < vocab) x[u].load(static_cast<const char*>(a.dout) + static_cast<int64_t>(s.order[i]) * a.ldd * (kBf16 ? 2 : 4), col);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (at + u >= last) break;
+      if (k[u] != key) {
+        finish(false);
+        key = k[u];
+        begun = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+      }
+      if (in && k[u] < vocab) {
+        float v[8];
+        x[u].get(v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += v[i];
+      }
+    }
+  }
+  finish(behind == key);
+}
+
+// Rows whose tokens reach over chunks: the chunk in which one begins adds up, in order, what the chunks have left of it.  A wavefront to a chunk and 256 columns.
+__global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs s) {
+  const EmbeddingBackward& a = s.a;
+  const int chunk = static_cast<int>(blockIdx.x), first = chunk * s.chunk, last = first + s.chunk;
+  if (last >= s.n) return;
+  const uint32_t key = s.keys[last - 1];
+  if (key >= static_cast<uint32_t>(a.vocab) || s.keys[last] != key || (first > 0 && s.keys[first - 1] == key)) return;
+  const int64_t col = static_cast<int64_t>(blockIdx.y) * 1024 + threadIdx.x * 4;
+  if (col >= a.cols) return;
+  const int end = lower_bound(s.keys, s.n, key + 1), final_chunk = (end - 1) / s.chunk;
+  const float* from = s.partials + static_cast<int64_t>(chunk) * 2 * a.cols + col;
+  float4v sum = *reinterpret_cast<const float4v*>(from + a.cols);
+#pragma unroll 8
+  for (int c = 1; c <= final_chunk - chunk; ++c) sum += *reinterpret_cast<const float4v*>(from + static_cast<int64_t>(c) * 2 * a.cols);
+  float4v* to = reinterpret_cast<float4v*>(a.dtable + static_cast<int64_t>(key) * a.ldt + col);
+  sum = a.scale * sum;
+  *to = a.accumulate ? *to + sum : sum;
+}
+
+__global__ __launch_bounds__(256) void embedding_zero_kernel(float* dtable, int64_t ldt, int64_t rows, int64_t cols) {
+  for (int64_t row = blockIdx.x; row < rows; row += gridDim.x)
+    for (int64_t col = threadIdx.x * 4; col < cols; col += 1024) *reinterpret_cast<float4v*>(dtable + row * ldt + col) = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+}
+
+// ---------------------------------------------------------------- launches
+
+struct SumPlan {
+  int chunk, chunks, tiles, passes, digit_bits;
+  size_t keys, order, counts, partials, bytes;   // places in the workspace, in words; two of keys and order each where there are passes
+};
+SumPlan plan(int64_t n, int64_t vocab, int64_t cols) {
+  SumPlan p{};
+  // Chunks of sixteen tokens, longer from 8192 on so that the partial sums stay few.
+  p.chunk = static_cast<int>(std::max<int64_t>(16, (n + 511) / 512));
+  p.chunks = static_cast<int>((n + p.chunk - 1) / p.chunk);
+  size_t at = 0;
+  auto take = [&at](size_t words) {
+    const size_t here = at;
+    at += (words + 3) / 4 * 4;
+    return here;
+  };
+  const bool few = n <= kFewTokens;
+  p.keys = take(static_cast<size_t>(n) * (few ? 1 : 2));
+  p.order = take(static_cast<size_t>(n) * (few ? 1 : 2));
+  if (!few) {
+    int bits = 1;
+    while ((vocab >> bits) != 0) ++bits;
+    p.passes = (bits + 8) / 9;
+    p.digit_bits = (bits + p.passes - 1) / p.passes;
+    p.tiles = static_cast<int>((n + kTile - 1) / kTile);
+    p.counts = take(static_cast<size_t>(p.tiles) << p.digit_bits);
+  }
+  p.partials = take(static_cast<size_t>(p.chunks) * 2 * static_cast<size_t>(cols));
+  p.bytes = at * 4;
+  return p;
+}
+
+}  // namespace
+
+size_t embedding_workspace_bytes(int64_t tokens, int64_t vocab, int64_t cols) { return tokens ? plan(tokens, vocab, cols).bytes : 0; }
+
+hipError_t launch_embedding_forward(const EmbeddingForward& all, hipStream_t s) {
+  EmbeddingForward a = all;
+  const int64_t groups = a.cols / 8, most = std::max<int64_t>(1, (int64_t{1} << 33) / groups);   // tokens of a launch, which holds 2^32 threads
+  for (; a.token0 < all.tokens; a.token0 += most) {
+    a.tokens = std::min(all.tokens, a.token0 + most);
+    const unsigned wgs = static_cast<unsigned>(((a.tokens - a.token0) * groups + 256 * kGroupsEach - 1) / (256 * kGroupsEach));
+#define NVFP4_EMBED(T, O) hipLaunchKernelGGL((embedding_forward_kernel<T, O>), dim3(wgs), dim3(256), 0, s, a)
+    if (a.table_bf16) {
+      if (a.out_bf16) NVFP4_EMBED(true, true); else NVFP4_EMBED(true, false);
+    } else {
+      if (a.out_bf16) NVFP4_EMBED(false, true); else NVFP4_EMBED(false, false);
+    }
+#undef NVFP4_EMBED
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_embedding_backward(const EmbeddingBackward& a, void* workspace, hipStream_t s) {
+  if (a.tokens == 0) {
+    if (a.accumulate || a.vocab == 0) return hipSuccess;
+    hipLaunchKernelGGL(embedding_zero_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(a.vocab, 4096))), dim3(256), 0, s, a.dtable, a.ldt, a.vocab, a.cols);
+    return hipGetLastError();
+  }
+  const int n = static_cast<int>(a.tokens);
+  const SumPlan p = plan(n, a.vocab, a.cols);
+  uint32_t* words = static_cast<uint32_t*>(workspace);
+  uint32_t *keys = words + p.keys, *order = words + p.order;
+  hipError_t e;
+  if (n <= kFewTokens) {
+    hipLaunchKernelGGL(rank_kernel, dim3((n + 31) / 32), dim3(256), 0, s, a.ids, a.i64, n, a.vocab, keys, order);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  } else {
+    SortPass q{};
+    q.ids = a.ids, q.i64 = a.i64, q.vocab = a.vocab, q.n = n, q.tiles = p.tiles, q.digits = 1 << p.digit_bits, q.counts = words + p.counts;
+    for (int pass = 0; pass < p.passes; ++pass) {
+      q.first = pass == 0, q.shift = pass * p.digit_bits;
+      q.keys = keys, q.order = order;
+      keys = words + p.keys + (pass & 1 ? n : 0), order = words + p.order + (pass & 1 ? n : 0);
+      q.to_keys = keys, q.to_order = order;
+      hipLaunchKernelGGL(sort_count_kernel, dim3(p.tiles), dim3(256), 0, s, q);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      hipLaunchKernelGGL(sort_scan_kernel, dim3(1), dim3(1024), 0, s, q.counts, p.tiles << p.digit_bits);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      hipLaunchKernelGGL(sort_place_kernel, dim3(p.tiles), dim3(256), 0, s, q);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  SumArgs u{};
+  u.a = a, u.keys = keys, u.order = order, u.partials = reinterpret_cast<float*>(words + p.partials);
+  u.n = n, u.chunk = p.chunk, u.chunks = p.chunks, u.strips = static_cast<int>((a.cols + 511) / 512);
+  u.zero_groups = a.accumulate ? 0 : static_cast<int>(std::min<int64_t>((a.vocab + kZeroRows - 1) / kZeroRows, 1 << 16));
+  const int64_t wgs = (static_cast<int64_t>(u.chunks) * u.strips + 3) / 4 + u.zero_groups;
+  if (a.bf16) hipLaunchKernelGGL(embedding_sum_kernel<true>, dim3(static_cast<unsigned>(wgs)), dim3(256), 0, s, u);
+  else hipLaunchKernelGGL(embedding_sum_kernel<false>, dim3(static_cast<unsigned>(wgs)), dim3(256), 0, s, u);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (u.chunks > 1) hipLaunchKernelGGL(embedding_join_kernel, dim3(u.chunks, static_cast<unsigned>((a.cols + 1023) / 1024)), dim3(256), 0, s, u);
+  return hipGetLastError();
+}
+
+}  // namespace nvfp4

@@ -1,0 +1,533 @@
+// Log probabilities of given tokens, with entropy and the best alternatives, and the gradient of the logits.
+//   d_j = z_j - max z;  s = sum exp(scale d_j);  lse = scale max z + ln s;  p_j = exp(scale d_j) / s
+//   logprob = scale d_t - ln s;  entropy H = ln s - sum p_j scale d_j
+//   dz_j = scale (g [j = t] + p_j (g_lse - g - g_H (ln p_j + H)))
+// One pass over a row: every thread keeps a running maximum, the sum of exponentials relative to it and (for H) the sum of d exp(d), rescaled when the maximum
+// moves, a batch of 32 values at a time.  All of it FP32.  Masked values may be -infinity (probability 0) or the type's lowest value: the maximum
+// is kept apart from the logarithm of the sum, so that neither a large maximum nor a row of lowest values loses what the sum says.
+#include <algorithm>
+
+#include "nvfp4_internal.h"
+#include "checkpoint8.h"
+
+namespace nvfp4 {
+
+namespace {
+
+constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+constexpr float kLowest = -3.4028234663852886e38f;
+constexpr float kFar = -200.0f;   // 2^kFar is 0: exponents are held above it where they are factors, since 0 * -infinity is not 0
+constexpr float kInfinity = __builtin_huge_valf();
+constexpr int kMostThreads = 512, kMostParts = 64, kMostTop = 32, kCandidates = 1024;
+
+__device__ __forceinline__ int64_t index_at(const void* p, bool i64, int64_t i) {
+  return i64 ? static_cast<const int64_t*>(p)[i] : static_cast<const int32_t*>(p)[i];
+}
+
+// ---------------------------------------------------------------- sums of exponentials relative to a maximum
+// s = sum 2^((z - m) c);  e = sum (z - m) c 2^((z - m) c), c = scale log2(e).  Nothing but -infinity: m = kLowest, s = 0.
+// A NaN or +infinity makes s NaN, and s stays so.
+struct Sum {
+  float m, s, e;
+};
+
+__device__ __forceinline__ float far_at_most(float t) { return __builtin_fmaxf(t, kFar); }
+
+template <bool kEntropy>
+__device__ __forceinline__ void move_to(Sum& a, float m, float c) {
+  const float t = far_at_most((a.m - m) * c), f = __builtin_amdgcn_exp2f(t);
+  if (kEntropy) a.e = (a.e + a.s * t) * f;
+  a.s *= f;
+  a.m = m;
+}
+
+template <bool kEntropy>
+__device__ __forceinline__ void join(Sum& a, Sum b, float c) {
+  const float m = __builtin_fmaxf(a.m, b.m);
+  move_to<kEntropy>(a, m, c);
+  move_to<kEntropy>(b, m, c);
+  a.s += b.s;
+  if (kEntropy) a.e += b.e;
+}
+
+template <bool kEntropy, int kN>
+__device__ __forceinline__ void add(Sum& a, const float (&v)[kN], float c) {
+  float m = v[0];
+#pragma unroll
+  for (int i = 1; i < kN; ++i) m = __builtin_fmaxf(m, v[i]);
+  move_to<kEntropy>(a, __builtin_fmaxf(a.m, m), c);
+  float s[4] = {}, e[4] = {};   // four chains: shorter ones lose less
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    const float t = (v[i] - a.m) * c, p = __builtin_amdgcn_exp2f(t);
+    s[i & 3] += p;
+    if (kEntropy) e[i & 3] = __builtin_fmaf(p, far_at_most(t), e[i & 3]);
+  }
+  a.s += (s[0] + s[1]) + (s[2] + s[3]);
+  if (kEntropy) a.e += (e[0] + e[1]) + (e[2] + e[3]);
+}
+
+template <bool kEntropy>
+__device__ __forceinline__ Sum wave_join(Sum a, float c) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    Sum b;
+    b.m = __shfl_xor(a.m, off, 64);
+    b.s = __shfl_xor(a.s, off, 64);
+    b.e = kEntropy ? __shfl_xor(a.e, off, 64) : 0.0f;
+    join<kEntropy>(a, b, c);
+  }
+  return a;
+}
+
+// Of a workgroup's threads, the same in all of them.
+template <bool kEntropy>
+__device__ __forceinline__ Sum workgroup_join(Sum a, float c, Sum* lds) {
+  a = wave_join<kEntropy>(a, c);
+  const int waves = blockDim.x >> 6;
+  if (waves == 1) return a;
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = a;
+  __syncthreads();
+  a = lds[0];
+  for (int w = 1; w < waves; ++w) join<kEntropy>(a, lds[w], c);
+  return a;
+}
+
+// Eight columns from 8 g on; those past the end of the row are not there (-infinity).
+template <bool kBf16>
+__device__ __forceinline__ void rest_of_row(const void* row, int g, int cols, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int col = g * 8 + i;
+    v[i] = -kInfinity;
+    if (col < cols) v[i] = kBf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(row)[col]) << 16) : static_cast<const float*>(row)[col];
+  }
+}
+
+// A thread's share of groups [g0, g1) of eight columns.
+template <bool kBf16, bool kEntropy>
+__device__ __forceinline__ Sum sum_of_groups(const void* row, int g0, int g1, int cols, float c) {
+  const int step = blockDim.x, whole = min(g1, cols >> 3);
+  Sum a{kLowest, 0.0f, 0.0f};
+  int g = g0 + static_cast<int>(threadIdx.x);
+  for (; g + 3 * step < whole; g += 4 * step) {
+    Eight<kBf16> x[4];
+    float v[32];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x[u].load(row, static_cast<int64_t>(g + u * step) * 8);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      float w[8];
+      x[u].get(w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[u * 8 + i] = w[i];
+    }
+    add<kEntropy>(a, v, c);
+  }
+  for (; g < g1; g += step) {
+    float v[8];
+    if (g < whole) {
+      Eight<kBf16> x;
+      x.load(row, static_cast<int64_t>(g) * 8);
+      x.get(v);
+    } else {
+      rest_of_row<kBf16>(row, g, cols, v);
+    }
+    add<kEntropy>(a, v, c);
+  }
+  return a;
+}
+
+// What the backward pass starts from.  A row without a value above -infinity has no distribution: {0, +infinity} makes every probability 0 there.
+struct RowStats {
+  float m, logsum;
+  __device__ __forceinline__ explicit RowStats(const Sum& a) : m(a.s == 0.0f ? 0.0f : a.m), logsum(a.s == 0.0f ? kInfinity : logf(a.s)) {}
+  __device__ __forceinline__ float logprob(float z, float scale) const { return (z - m) * scale - logsum; }
+};
+
+template <bool kBf16>
+__device__ __forceinline__ float value_at(const void* row, int64_t col) {
+  return kBf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(row)[col]) << 16) : static_cast<const float*>(row)[col];
+}
+
+__device__ __forceinline__ void write_row(const LogprobForward& a, int64_t row, const Sum& sum, const RowStats& r, float at_target, bool counted) {
+  const bool empty = sum.s == 0.0f;
+  if (a.stats) a.stats[2 * row] = r.m, a.stats[2 * row + 1] = r.logsum;
+  if (a.lse) a.lse[row] = empty ? -kInfinity : r.m * a.scale + r.logsum;
+  if (a.entropy) a.entropy[row] = empty ? 0.0f : r.logsum - kLn2 * (sum.e / sum.s);
+  if (a.logprob) a.logprob[row] = counted ? r.logprob(at_target, a.scale) : 0.0f;
+}
+
+// ---------------------------------------------------------------- best alternatives
+// A value and its column as one number, the greater the better: values in order (a NaN below -infinity; -0 is 0), the lower column first among equal ones.
+__device__ __forceinline__ uint32_t order_of(float z) {
+  const uint32_t u = __float_as_uint(z + 0.0f);
+  return z != z ? 0u : u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ uint64_t place(float z, int col) { return static_cast<uint64_t>(order_of(z)) << 32 | (0xFFFFFFFFu - static_cast<uint32_t>(col)); }
+__device__ __forceinline__ float value_of(uint64_t place) {
+  const uint32_t k = static_cast<uint32_t>(place >> 32);
+  return k == 0u ? __uint_as_float(0x7FC00000u) : __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+__device__ __forceinline__ int column_of(uint64_t place) { return static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(place)); }
+
+struct TopShared {
+  float group[kMostThreads / 64][64];
+  uint64_t best[kMostThreads / 64];
+  uint64_t found[kCandidates];
+  uint16_t threads[kMostThreads];
+  uint32_t bound, n_threads, n_found;
+};
+
+// The k best of groups [g0, g1) to emit(rank, place).  `own`: the largest value that this thread has seen in sum_of_groups.
+// The k-th largest of 64 maxima over disjoint columns bounds the k-th best from below; only threads whose maximum reaches it hold candidates, some
+// k of them, and their columns are read once more by the whole workgroup.  Candidates take their rank by counting the better ones.
+// Where too many reach the bound (rows that are masked or equal nearly everywhere) the best is taken k times over instead.
+template <bool kBf16, typename Emit>
+__device__ __forceinline__ void take_best(const void* row, int g0, int g1, int cols, float own, int k, TopShared& s, Emit emit) {
+  const int t = threadIdx.x, T = blockDim.x, waves = T >> 6;
+  s.group[t >> 6][t & 63] = own;
+  if (t == 0) s.n_threads = s.n_found = 0u;
+  __syncthreads();
+  if (t < 64) {
+    float m = s.group[0][t];
+    for (int w = 1; w < waves; ++w) m = __builtin_fmaxf(m, s.group[w][t]);
+    int better = 0;
+    for (int i = 0; i < 64; ++i) {
+      const float o = __shfl(m, i, 64);
+      better += o > m || (o == m && i < t);
+    }
+    if (better == k - 1) s.bound = m > kLowest ? order_of(m) : 0u;   // (at kLowest the groups may be empty)
+  }
+  __syncthreads();
+  const uint32_t bound = s.bound;
+  const bool all = bound == 0u;
+  if (!all && order_of(own) >= bound) s.threads[atomicAdd(&s.n_threads, 1u)] = static_cast<uint16_t>(t);
+  __syncthreads();
+  const int turns = (g1 - g0 + T - 1) / T, items = (all ? T : static_cast<int>(s.n_threads)) * turns;
+  const bool few = !all || (g1 - g0) * 8 <= kCandidates;
+  if (few) {
+    for (int i = t; i < items; i += T) {
+      const int g = g0 + (all ? i : s.threads[i / turns] + i % turns * T);
+      if (g >= g1) continue;
+      float v[8];
+      if (g < cols >> 3) {
+        Eight<kBf16> x;
+        x.load(row, static_cast<int64_t>(g) * 8);
+        x.get(v);
+      } else {
+        rest_of_row<kBf16>(row, g, cols, v);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (g * 8 + j < cols && order_of(v[j]) >= bound) {
+          const uint32_t at = atomicAdd(&s.n_found, 1u);
+          if (at < kCandidates) s.found[at] = place(v[j], g * 8 + j);
+        }
+      }
+    }
+  }
+  __syncthreads();
+  const int n = static_cast<int>(s.n_found);
+  if (few && n <= kCandidates) {
+    for (int i = t; i < n; i += T) {
+      const uint64_t mine = s.found[i];
+      int better = 0;
+      for (int j = 0; j < n; ++j) better += s.found[j] > mine;
+      if (better < k) emit(better, mine);
+    }
+    if (n < k && t < k && t >= n) emit(t, 0ull);
+    return;
+  }
+  uint64_t last = ~0ull;
+  for (int r = 0; r < k; ++r) {
+    uint64_t best = 0ull;
+    for (int g = g0 + t; g < g1; g += T) {
+      float v[8];
+      rest_of_row<kBf16>(row, g, cols, v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint64_t p = place(v[j], g * 8 + j);
+        if (g * 8 + j < cols && p < last && p > best) best = p;
+      }
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+      const uint64_t o = __shfl_xor(static_cast<unsigned long long>(best), off, 64);
+      best = o > best ? o : best;
+    }
+    if ((t & 63) == 0) s.best[t >> 6] = best;
+    __syncthreads();
+    best = s.best[0];
+    for (int w = 1; w < waves; ++w) best = s.best[w] > best ? s.best[w] : best;
+    if (t == 0) emit(r, best);
+    last = best;
+    __syncthreads();
+  }
+}
+
+__device__ __forceinline__ void write_alternative(const LogprobForward& a, int64_t row, int rank, uint64_t p, const RowStats& r) {
+  a.top_index[row * a.top + rank] = column_of(p);
+  a.top_logprob[row * a.top + rank] = r.logprob(value_of(p), a.scale);
+}
+
+// ---------------------------------------------------------------- forward
+// A workgroup takes a row, or one of `parts` pieces of it, whose sums and best go to the second launch.
+template <bool kBf16, bool kEntropy, bool kTop>
+__global__ __launch_bounds__(kMostThreads) void logprob_forward_kernel(LogprobForward a) {
+  __shared__ Sum sums[kMostThreads / 64];
+  const int part = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.parts));
+  const int64_t row = a.row0 + blockIdx.x / static_cast<unsigned>(a.parts);
+  const int cols = static_cast<int>(a.cols), groups = (cols + 7) >> 3, each = (groups + a.parts - 1) / a.parts;
+  const int g0 = min(part * each, groups), g1 = min(g0 + each, groups);
+  const void* z = static_cast<const char*>(a.z) + row * a.ld * (kBf16 ? 2 : 4);
+  const float c = a.scale * kLog2E;
+  bool counted = false;
+  float at_target = 0.0f;
+  if (a.parts == 1 && threadIdx.x == 0 && a.targets) {   // (asked for ahead of the row)
+    const int64_t target = index_at(a.targets, a.i64, row);
+    counted = target >= 0 && target < cols;
+    if (counted) at_target = value_at<kBf16>(z, target);
+  }
+  const Sum mine = sum_of_groups<kBf16, kEntropy>(z, g0, g1, cols, c);
+  const Sum all = workgroup_join<kEntropy>(mine, c, sums);
+  if (a.parts > 1) {
+    float* to = a.partial + (row * a.parts + part) * 4;
+    if (threadIdx.x == 0) *reinterpret_cast<float4v*>(to) = float4v{all.m, all.s, kEntropy ? all.e : 0.0f, 0.0f};
+    if constexpr (kTop) {
+      __shared__ TopShared s;
+      uint64_t* best = a.best + (row * a.parts + part) * a.top;
+      take_best<kBf16>(z, g0, g1, cols, mine.m, a.top, s, [&](int rank, uint64_t p) { best[rank] = p; });
+    }
+    return;
+  }
+  const RowStats r(all);
+  if (threadIdx.x == 0) write_row(a, row, all, r, at_target, counted);
+  if constexpr (kTop) {
+    __shared__ TopShared s;
+    take_best<kBf16>(z, g0, g1, cols, mine.m, a.top, s, [&](int rank, uint64_t p) { write_alternative(a, row, rank, p, r); });
+  }
+}
+
+// The pieces of a row together, one workgroup to a row.
+template <bool kBf16, bool kEntropy, bool kTop>
+__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobForward a) {
+  const int64_t row = a.row0 + blockIdx.x;
+  const int t = threadIdx.x, parts = a.parts, k = a.top;
+  const float c = a.scale * kLog2E;
+  const void* z = static_cast<const char*>(a.z) + row * a.ld * (kBf16 ? 2 : 4);
+  bool counted = false;
+  float at_target = 0.0f;
+  if (t == 0 && a.targets) {
+    const int64_t target = index_at(a.targets, a.i64, row);
+    counted = target >= 0 && target < a.cols;
+    if (counted) at_target = value_at<kBf16>(z, target);
+  }
+  Sum mine{kLowest, 0.0f, 0.0f};
+  if ((t & 63) < parts) {   // (every wavefront the same)
+    const float4v v = *reinterpret_cast<const float4v*>(a.partial + (row * parts + (t & 63)) * 4);
+    mine = Sum{v[0], v[1], v[2]};
+  }
+  const Sum all = wave_join<kEntropy>(mine, c);
+  const RowStats r(all);
+  if (t == 0) write_row(a, row, all, r, at_target, counted);
+  if constexpr (kTop) {
+    __shared__ uint64_t best[kMostParts * kMostTop], found[kMostParts * kMostTop];
+    __shared__ uint64_t bound;
+    __shared__ int n_found;
+    const int n = parts * k;
+    for (int i = t; i < n; i += 256) best[i] = a.best[row * n + i];
+    if (t == 0) bound = 0ull, n_found = 0;
+    __syncthreads();
+    if (t < parts && parts >= k) {   // the k-th largest of the pieces' first
+      const uint64_t first = best[t * k];
+      int better = 0;
+      for (int i = 0; i < parts; ++i) better += best[i * k] > first || (best[i * k] == first && i < t);
+      if (better == k - 1) bound = first;
+    }
+    __syncthreads();
+    for (int i = t; i < n; i += 256)
+      if (best[i] >= bound && best[i] != 0ull) found[atomicAdd(&n_found, 1)] = best[i];
+    __syncthreads();
+    for (int i = t; i < n_found; i += 256) {
+      const uint64_t p = found[i];
+      int better = 0;
+      for (int j = 0; j < n_found; ++j) better += found[j] > p;
+      if (better < k) write_alternative(a, row, better, p, r);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- gradient of the logits
+
+// What is the same for a row: dz_j = p_j (a - b log2 p_j), log2 p_j = (z_j - m) c - l; and what the target's column gets on top.
+struct RowGradient {
+  float m, l, a, b, at_target;
+  int target;   // -1: none
+  __device__ __forceinline__ RowGradient(float m_, float logsum, float scale, float g, float g_lse, float g_entropy, float entropy, int64_t target_, int cols) {
+    const bool counted = target_ >= 0 && target_ < cols;
+    if (!counted) g = 0.0f;
+    m = m_, l = logsum * kLog2E;
+    a = scale * (g_lse - g - (g_entropy != 0.0f ? g_entropy * entropy : 0.0f));
+    b = scale * g_entropy * kLn2;
+    at_target = scale * g;
+    target = counted && logsum != kInfinity ? static_cast<int>(target_) : -1;
+  }
+  template <bool kEntropy>
+  __device__ __forceinline__ void of(float (&v)[8], int g, float c) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float t = (v[i] - m) * c - l, p = __builtin_amdgcn_exp2f(t);
+      v[i] = p * (kEntropy ? a - b * far_at_most(t) : a);
+    }
+    if (g == target >> 3) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += i == (target & 7) ? at_target : 0.0f;
+    }
+  }
+};
+
+template <bool kInBf16, bool kOutBf16, bool kEntropy>
+__device__ __forceinline__ void gradient_of_rest(const void* z, void* dz, int g, int cols, const RowGradient& r, float c) {
+  float v[8];
+  rest_of_row<kInBf16>(z, g, cols, v);
+  r.of<kEntropy>(v, g, c);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int col = g * 8 + i;
+    if (col < cols) {
+      if (kOutBf16) static_cast<uint16_t*>(dz)[col] = static_cast<uint16_t>(f32_to_bf16(v[i]));
+      else static_cast<float*>(dz)[col] = v[i];
+    }
+  }
+}
+
+// Groups [g0, g1) of a row by the workgroup's threads, from the end to the front.
+template <bool kInBf16, bool kOutBf16, bool kEntropy>
+__device__ __forceinline__ void gradient_of_groups(const void* z, void* dz, int g0, int g1, int cols, const RowGradient& r, float c) {
+  const int step = blockDim.x, whole = min(g1, cols >> 3);
+  if (whole < g1 && threadIdx.x == 0) gradient_of_rest<kInBf16, kOutBf16, kEntropy>(z, dz, whole, cols, r, c);
+  int g = whole - 1 - static_cast<int>(threadIdx.x);
+  for (; g - 3 * step >= g0; g -= 4 * step) {
+    Eight<kInBf16> x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x[u].load(z, static_cast<int64_t>(g - u * step) * 8);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      float v[8];
+      x[u].get(v);
+      r.of<kEntropy>(v, g - u * step, c);
+      store8(dz, static_cast<int64_t>(g - u * step) * 8, kOutBf16, v);
+    }
+  }
+  for (; g >= g0; g -= step) {
+    Eight<kInBf16> x;
+    float v[8];
+    x.load(z, static_cast<int64_t>(g) * 8);
+    x.get(v);
+    r.of<kEntropy>(v, g, c);
+    store8(dz, static_cast<int64_t>(g) * 8, kOutBf16, v);
+  }
+}
+
+template <bool kInBf16, bool kOutBf16, bool kEntropy>
+__global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobBackward a) {
+  const int part = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.parts));
+  const int64_t row = a.row0 + blockIdx.x / static_cast<unsigned>(a.parts);
+  const int cols = static_cast<int>(a.cols), groups = (cols + 7) >> 3, each = (groups + a.parts - 1) / a.parts;
+  const int g0 = min(part * each, groups), g1 = min(g0 + each, groups);
+  const RowGradient r(a.stats[2 * row], a.stats[2 * row + 1], a.scale, a.g_logprob ? a.g_logprob[row] : 0.0f, a.g_lse ? a.g_lse[row] : 0.0f,
+                      kEntropy ? a.g_entropy[row] : 0.0f, kEntropy ? a.entropy[row] : 0.0f, a.targets ? index_at(a.targets, a.i64, row) : -1, cols);
+  gradient_of_groups<kInBf16, kOutBf16, kEntropy>(static_cast<const char*>(a.z) + row * a.ld * (kInBf16 ? 2 : 4),
+                                                  static_cast<char*>(a.dz) + row * a.ldd * (kOutBf16 ? 2 : 4), g0, g1, cols, r, a.scale * kLog2E);
+}
+
+// ---------------------------------------------------------------- launches
+
+// A launch holds 2^32 threads: rows of one, with `each` threads to a row.
+int64_t rows_at_once(int64_t each) { return std::max<int64_t>(1, 0xfffffff0 / each); }
+
+constexpr int64_t kCUs = 256;
+
+struct ForwardShape {
+  int parts, threads;
+};
+ForwardShape forward_shape(int64_t rows, int64_t cols) {
+  const int64_t groups = (cols + 7) / 8;
+  if (rows < 2 * kCUs && groups > 512) {
+    const int64_t parts = std::min<int64_t>({kMostParts, 4 * kCUs / std::max<int64_t>(rows, 1), groups / 256});
+    if (parts > 1) return {static_cast<int>(parts), 256};
+  }
+  return {1, groups >= 2048 ? 512 : groups >= 512 ? 256 : 64};
+}
+
+template <bool... kFlags>
+hipError_t forward_with(const LogprobForward& a, int threads, hipStream_t s) {
+  if constexpr (sizeof...(kFlags) == 3) {
+    const int64_t most = rows_at_once(static_cast<int64_t>(a.parts) * std::max(threads, 256));
+    LogprobForward p = a;
+    for (p.row0 = 0; p.row0 < a.rows; p.row0 += most) {
+      const unsigned rows = static_cast<unsigned>(std::min(most, a.rows - p.row0));
+      hipLaunchKernelGGL((logprob_forward_kernel<kFlags...>), dim3(rows * static_cast<unsigned>(a.parts)), dim3(threads), 0, s, p);
+      hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      if (a.parts == 1) continue;
+      hipLaunchKernelGGL((logprob_join_kernel<kFlags...>), dim3(rows), dim3(256), 0, s, p);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  } else {
+    const bool flags[] = {a.bf16, a.entropy != nullptr, a.top > 0};
+    return flags[sizeof...(kFlags)] ? forward_with<kFlags..., true>(a, threads, s) : forward_with<kFlags..., false>(a, threads, s);
+  }
+}
+
+template <bool... kFlags>
+hipError_t backward_with(const LogprobBackward& a, int threads, hipStream_t s) {
+  if constexpr (sizeof...(kFlags) == 3) {
+    const int64_t most = rows_at_once(static_cast<int64_t>(a.parts) * threads);
+    LogprobBackward p = a;
+    for (p.row0 = 0; p.row0 < a.rows; p.row0 += most) {
+      const unsigned rows = static_cast<unsigned>(std::min(most, a.rows - p.row0));
+      hipLaunchKernelGGL((logprob_backward_kernel<kFlags...>), dim3(rows * static_cast<unsigned>(a.parts)), dim3(threads), 0, s, p);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  } else {
+    const bool flags[] = {a.bf16, a.out_bf16, a.g_entropy != nullptr};
+    return flags[sizeof...(kFlags)] ? backward_with<kFlags..., true>(a, threads, s) : backward_with<kFlags..., false>(a, threads, s);
+  }
+}
+
+}  // namespace
+
+size_t logprob_workspace_bytes(int64_t rows, int64_t cols, int top) {
+  const int parts = forward_shape(rows, cols).parts;
+  return parts == 1 ? 0 : static_cast<size_t>(rows) * static_cast<size_t>(parts) * (16 + 8 * static_cast<size_t>(top));
+}
+
+hipError_t launch_logprob_forward(const LogprobForward& all, void* workspace, hipStream_t s) {
+  LogprobForward a = all;
+  const ForwardShape shape = forward_shape(a.rows, a.cols);
+  a.parts = shape.parts;
+  a.partial = static_cast<float*>(workspace);
+  a.best = reinterpret_cast<uint64_t*>(a.partial + (a.parts > 1 ? a.rows * a.parts * 4 : 0));
+  return forward_with<>(a, shape.threads, s);
+}
+
+// A workgroup takes 1024 groups of eight columns at a time, or a row that has fewer.
+hipError_t launch_logprob_backward(const LogprobBackward& all, hipStream_t s) {
+  LogprobBackward a = all;
+  const int64_t groups = (a.cols + 7) / 8;
+  a.parts = static_cast<int>((groups + 1023) / 1024);
+  return backward_with<>(a, groups >= 256 ? 256 : 64, s);
+}
+
+hipError_t launch_logprob_with_gradient(const LogprobForward& f, const LogprobBackward& b, void* workspace, hipStream_t s) {
+  const hipError_t e = launch_logprob_forward(f, workspace, s);
+  return e == hipSuccess ? launch_logprob_backward(b, s) : e;
+}
+
+}  // namespace nvfp4

@@ -209,6 +209,71 @@ size_t activation_partial_bytes(int64_t rows, int64_t cols);
 // out <- (out +) the sum of `parts` rows of partial sums, in a fixed order
 hipError_t launch_colsum(const float* partials, int parts, int64_t cols, float* out, bool accumulate, hipStream_t s);
 
+// ---------------------------------------------------------------- the ends of a training step: embedding, log probabilities, gradients' norm
+struct EmbeddingForward {
+  const void* ids;
+  const void* table;
+  void* out;
+  int64_t tokens, vocab, cols, ldt, ldo;
+  float scale;
+  bool i64, table_bf16, out_bf16;
+  int64_t token0 = 0;      // set by the launch
+};
+hipError_t launch_embedding_forward(const EmbeddingForward& a, hipStream_t s);
+struct EmbeddingBackward {
+  const void* ids;
+  const void* dout;
+  float* dtable;
+  int64_t tokens, vocab, cols, ldd, ldt;
+  float scale;
+  bool i64, bf16, accumulate;
+};
+size_t embedding_workspace_bytes(int64_t tokens, int64_t vocab, int64_t cols);
+hipError_t launch_embedding_backward(const EmbeddingBackward& a, void* workspace, hipStream_t s);
+struct LogprobForward {
+  const void* z;
+  const void* targets;            // or null
+  int64_t rows, cols, ld;
+  float scale;
+  bool bf16, i64;
+  float *logprob, *stats, *lse, *entropy;   // each may be null; stats: {largest logit, log of the sum} of each row
+  int top;
+  int32_t* top_index;
+  float* top_logprob;
+  int64_t row0 = 0;               // from here on set by the launch
+  int parts = 1;
+  float* partial = nullptr;
+  uint64_t* best = nullptr;
+};
+size_t logprob_workspace_bytes(int64_t rows, int64_t cols, int top);
+hipError_t launch_logprob_forward(const LogprobForward& a, void* workspace, hipStream_t s);
+struct LogprobBackward {
+  const void* z;
+  const void* targets;                              // or null
+  const float *stats, *entropy;                     // entropy: with g_entropy only
+  const float *g_logprob, *g_lse, *g_entropy;       // each may be null
+  void* dz;
+  int64_t rows, cols, ld, ldd;
+  float scale;
+  bool bf16, out_bf16, i64;
+  int64_t row0 = 0;
+  int parts = 1;
+};
+hipError_t launch_logprob_backward(const LogprobBackward& a, hipStream_t s);
+hipError_t launch_logprob_with_gradient(const LogprobForward& f, const LogprobBackward& b, void* workspace, hipStream_t s);
+// The list of gradients on the device: a GradTensor each, then the number of the tensor that each unit of work belongs to.
+struct GradTensor {
+  const void* data;
+  void* out;
+  int64_t cols, ld, ld_out;
+  int32_t rows, first_unit;
+  int32_t unit_rows, unit_cols;   // of a unit of work; a row has (cols + unit_cols - 1) / unit_cols of them
+  int32_t flags, unused;          // bits: 1 data is bf16, 2 out is bf16, 4 sixteen bytes at a time
+};
+enum { kGradBf16 = 1, kGradOutBf16 = 2, kGradWide = 4 };
+hipError_t launch_grad_sumsq(const GradTensor* tensors, const int32_t* unit_tensor, int64_t units, double* sumsq, double* partials, hipStream_t s);
+hipError_t launch_grad_clip(const GradTensor* tensors, const int32_t* unit_tensor, int64_t units, const double* sumsq, float max_norm, float* norm, hipStream_t s);
+
 hipError_t run_selftest(uint64_t* mismatches_dev, hipStream_t s);
 
 // Host Philox4x32-10, used only to derive the sign diagonal from a seed (16 bits, or 32 for the MXFP4 mode).
