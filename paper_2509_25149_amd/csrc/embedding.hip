@@ -61,37 +61,39 @@ __device__ __forceinline__ uint32_t key_of(const void* ids, bool i64, int64_t t,
   return static_cast<uint32_t>(id >= 0 && id < vocab ? id : vocab);
 }
 
-// Up to kFewTokens: a token's place is the number of tokens before it, counted.  32 tokens to a workgroup, eight threads to a token; two operations a pair.
-constexpr int kFewTokens = 8192, kTile = 2048;
+// Up to kFewTokens: a token's place is the number of tokens before it, counted: two operations a pair.  A workgroup holds all keys and takes 32 tokens, sixteen threads to a token.
+constexpr int kFewTokens = 8192, kTile = 2048, kRankTokens = 32, kRankParts = 16;
 
-__global__ __launch_bounds__(256) void rank_kernel(const void* ids, bool i64, int n, int64_t vocab, uint32_t* __restrict__ keys, uint32_t* __restrict__ order) {
-  __shared__ __attribute__((aligned(16))) uint32_t tile[kTile];
-  const int t = static_cast<int>(blockIdx.x) * 32 + (threadIdx.x >> 3), part = threadIdx.x & 7;
-  const uint32_t key = t < n ? key_of(ids, i64, t, vocab) : 0u;
+__global__ __launch_bounds__(kRankTokens* kRankParts) void rank_kernel(const void* ids, bool i64, int n, int64_t vocab, uint32_t* __restrict__ keys, uint32_t* __restrict__ order) {
+  constexpr int T = kRankTokens * kRankParts;
+  __shared__ __attribute__((aligned(16))) uint32_t all[kFewTokens];
+  const int fours = (n + 3) >> 2;
+#pragma unroll 8
+  for (int i = threadIdx.x; i < fours * 4; i += T) all[i] = i < n ? key_of(ids, i64, i, vocab) : 0xFFFFFFFFu;
+  __syncthreads();
+  const int t = static_cast<int>(blockIdx.x) * kRankTokens + static_cast<int>(threadIdx.x) / kRankParts, part = threadIdx.x % kRankParts;
+  const uint32_t key = t < n ? all[t] : 0u;
+  const uint4* four = reinterpret_cast<const uint4*>(all);
   uint32_t before = 0u;
-  for (int base = 0; base < n; base += kTile) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < kTile; i += 256) tile[i] = base + i < n ? key_of(ids, i64, base + i, vocab) : 0xFFFFFFFFu;
-    __syncthreads();
-    const int used = min(kTile, n - base);
-    const uint4* four = reinterpret_cast<const uint4*>(tile);
-    if (static_cast<int>(blockIdx.x) * 32 >= base + kTile || base >= static_cast<int>(blockIdx.x) * 32 + 32) {
-      const uint32_t bound = key + (base < t);   // among equal keys those in front come first
-#pragma unroll 4
-      for (int i = part; i * 4 < used; i += 8) {
-        const uint4 k = four[i];
-        before += (k.x < bound) + (k.y < bound) + (k.z < bound) + (k.w < bound);
-      }
-    } else {
-      for (int i = part; i * 4 < used; i += 8) {
-        const uint4 k = four[i];
-        const int at = t - base - i * 4;
-        before += (k.x < key + (at > 0)) + (k.y < key + (at > 1)) + (k.z < key + (at > 2)) + (k.w < key + (at > 3));
-      }
-    }
+  // Among equal keys those in front come first: keys up to this token's in front of the workgroup's tokens, less than it behind them.
+  const int mid0 = static_cast<int>(blockIdx.x) * (kRankTokens / 4), mid1 = min(mid0 + kRankTokens / 4, fours);
+#pragma unroll 8
+  for (int i = part; i < mid0; i += kRankParts) {
+    const uint4 k = four[i];
+    before += (k.x <= key) + (k.y <= key) + (k.z <= key) + (k.w <= key);
+  }
+  for (int i = mid0 + part; i < mid1; i += kRankParts) {
+    const uint4 k = four[i];
+    const int at = t - i * 4;
+    before += (k.x < key + (at > 0)) + (k.y < key + (at > 1)) + (k.z < key + (at > 2)) + (k.w < key + (at > 3));
+  }
+#pragma unroll 8
+  for (int i = mid1 + part; i < fours; i += kRankParts) {
+    const uint4 k = four[i];
+    before += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
   }
 #pragma unroll
-  for (int off = 1; off < 8; off <<= 1) before += __shfl_xor(before, off, 64);
+  for (int off = 1; off < kRankParts; off <<= 1) before += __shfl_xor(before, off, 64);
   if (part == 0 && t < n) keys[before] = key, order[before] = static_cast<uint32_t>(t);
 }
 
@@ -402,7 +404,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackward& a, void* workspace
   uint32_t *keys = words + p.keys, *order = words + p.order;
   hipError_t e;
   if (n <= kFewTokens) {
-    hipLaunchKernelGGL(rank_kernel, dim3((n + 31) / 32), dim3(256), 0, s, a.ids, a.i64, n, a.vocab, keys, order);
+    hipLaunchKernelGGL(rank_kernel, dim3((n + kRankTokens - 1) / kRankTokens), dim3(kRankTokens * kRankParts), 0, s, a.ids, a.i64, n, a.vocab, keys, order);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   } else {
     SortPass q{};

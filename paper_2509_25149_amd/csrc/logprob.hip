@@ -179,10 +179,40 @@ struct TopShared {
   uint32_t bound, n_threads, n_found;
 };
 
+// Eight values of a group, those past the end of the row at -infinity.
+template <bool kBf16>
+__device__ __forceinline__ void group_of(const void* row, int g, int cols, float (&v)[8]) {
+  if (g < cols >> 3) {
+    Eight<kBf16> x;
+    x.load(row, static_cast<int64_t>(g) * 8);
+    x.get(v);
+  } else {
+    rest_of_row<kBf16>(row, g, cols, v);
+  }
+}
+
+// The best of a thread's share of groups [g0, g1) that is worse than `last`.
+template <bool kBf16>
+__device__ __forceinline__ uint64_t best_of_share(const void* row, int g0, int g1, int cols, uint64_t last) {
+  uint64_t best = 0ull;
+#pragma unroll 4
+  for (int g = g0 + static_cast<int>(threadIdx.x); g < g1; g += blockDim.x) {
+    float v[8];
+    group_of<kBf16>(row, g, cols, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint64_t p = place(v[j], g * 8 + j);
+      if (g * 8 + j < cols && p < last && p > best) best = p;
+    }
+  }
+  return best;
+}
+
 // The k best of groups [g0, g1) to emit(rank, place).  `own`: the largest value that this thread has seen in sum_of_groups.
 // The k-th largest of 64 maxima over disjoint columns bounds the k-th best from below; only threads whose maximum reaches it hold candidates, some
 // k of them, and their columns are read once more by the whole workgroup.  Candidates take their rank by counting the better ones.
-// Where too many reach the bound (rows that are masked or equal nearly everywhere) the best is taken k times over instead.
+// Where fewer than k values are above -infinity the first columns at -infinity follow.
+// Where too many reach the bound (rows that are equal nearly everywhere) each thread keeps the best of its share, and the best of those is taken k times over.
 template <bool kBf16, typename Emit>
 __device__ __forceinline__ void take_best(const void* row, int g0, int g1, int cols, float own, int k, TopShared& s, Emit emit) {
   const int t = threadIdx.x, T = blockDim.x, waves = T >> 6;
@@ -193,64 +223,56 @@ __device__ __forceinline__ void take_best(const void* row, int g0, int g1, int c
     float m = s.group[0][t];
     for (int w = 1; w < waves; ++w) m = __builtin_fmaxf(m, s.group[w][t]);
     int better = 0;
+#pragma unroll 8
     for (int i = 0; i < 64; ++i) {
       const float o = __shfl(m, i, 64);
       better += o > m || (o == m && i < t);
     }
-    if (better == k - 1) s.bound = m > kLowest ? order_of(m) : 0u;   // (at kLowest the groups may be empty)
+    if (better == k - 1) s.bound = order_of(m);   // (kLowest, above -infinity, for groups of nothing else)
   }
   __syncthreads();
   const uint32_t bound = s.bound;
-  const bool all = bound == 0u;
-  if (!all && order_of(own) >= bound) s.threads[atomicAdd(&s.n_threads, 1u)] = static_cast<uint16_t>(t);
+  if (order_of(own) >= bound) s.threads[atomicAdd(&s.n_threads, 1u)] = static_cast<uint16_t>(t);
   __syncthreads();
-  const int turns = (g1 - g0 + T - 1) / T, items = (all ? T : static_cast<int>(s.n_threads)) * turns;
-  const bool few = !all || (g1 - g0) * 8 <= kCandidates;
-  if (few) {
-    for (int i = t; i < items; i += T) {
-      const int g = g0 + (all ? i : s.threads[i / turns] + i % turns * T);
-      if (g >= g1) continue;
-      float v[8];
-      if (g < cols >> 3) {
-        Eight<kBf16> x;
-        x.load(row, static_cast<int64_t>(g) * 8);
-        x.get(v);
-      } else {
-        rest_of_row<kBf16>(row, g, cols, v);
-      }
+  const int turns = (g1 - g0 + T - 1) / T, items = static_cast<int>(s.n_threads) * turns;
+  for (int i = t; i < items; i += T) {
+    const int g = g0 + s.threads[i / turns] + i % turns * T;
+    if (g >= g1) continue;
+    float v[8];
+    group_of<kBf16>(row, g, cols, v);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (g * 8 + j < cols && order_of(v[j]) >= bound) {
-          const uint32_t at = atomicAdd(&s.n_found, 1u);
-          if (at < kCandidates) s.found[at] = place(v[j], g * 8 + j);
-        }
+    for (int j = 0; j < 8; ++j) {
+      if (g * 8 + j < cols && order_of(v[j]) >= bound) {
+        const uint32_t at = atomicAdd(&s.n_found, 1u);
+        if (at < kCandidates) s.found[at] = place(v[j], g * 8 + j);
       }
     }
   }
   __syncthreads();
-  const int n = static_cast<int>(s.n_found);
-  if (few && n <= kCandidates) {
+  int n = static_cast<int>(s.n_found);
+  if (n < k) {   // everything above -infinity is among them: the first T >= k + 32 columns have enough others, unless they are NaN
+    __syncthreads();
+    const int col = g0 * 8 + t;
+    if (col < min(g1 * 8, cols) && value_at<kBf16>(row, col) == -kInfinity) {
+      const uint32_t at = atomicAdd(&s.n_found, 1u);
+      s.found[at] = place(-kInfinity, col);
+    }
+    __syncthreads();
+    n = static_cast<int>(s.n_found);
+  }
+  if (n >= k && n <= kCandidates) {
     for (int i = t; i < n; i += T) {
       const uint64_t mine = s.found[i];
       int better = 0;
+#pragma unroll 8
       for (int j = 0; j < n; ++j) better += s.found[j] > mine;
       if (better < k) emit(better, mine);
     }
-    if (n < k && t < k && t >= n) emit(t, 0ull);
     return;
   }
-  uint64_t last = ~0ull;
+  uint64_t mine = best_of_share<kBf16>(row, g0, g1, cols, ~0ull);
   for (int r = 0; r < k; ++r) {
-    uint64_t best = 0ull;
-    for (int g = g0 + t; g < g1; g += T) {
-      float v[8];
-      rest_of_row<kBf16>(row, g, cols, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint64_t p = place(v[j], g * 8 + j);
-        if (g * 8 + j < cols && p < last && p > best) best = p;
-      }
-    }
+    uint64_t best = mine;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) {
       const uint64_t o = __shfl_xor(static_cast<unsigned long long>(best), off, 64);
@@ -261,7 +283,7 @@ __device__ __forceinline__ void take_best(const void* row, int g0, int g1, int c
     best = s.best[0];
     for (int w = 1; w < waves; ++w) best = s.best[w] > best ? s.best[w] : best;
     if (t == 0) emit(r, best);
-    last = best;
+    if (best != 0ull && mine == best) mine = best_of_share<kBf16>(row, g0, g1, cols, best);
     __syncthreads();
   }
 }
@@ -339,11 +361,12 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobForward a) {
     for (int i = t; i < n; i += 256) best[i] = a.best[row * n + i];
     if (t == 0) bound = 0ull, n_found = 0;
     __syncthreads();
-    if (t < parts && parts >= k) {   // the k-th largest of the pieces' first
-      const uint64_t first = best[t * k];
+    if (t < parts) {   // with j = ceil(k / parts), the ceil(k / j)-th largest of the pieces' j-th: so many pieces have j each that reach it
+      const int j = (k + parts - 1) / parts, at = (k + j - 1) / j - 1;
+      const uint64_t mine = best[t * k + j - 1];
       int better = 0;
-      for (int i = 0; i < parts; ++i) better += best[i * k] > first || (best[i * k] == first && i < t);
-      if (better == k - 1) bound = first;
+      for (int i = 0; i < parts; ++i) better += best[i * k + j - 1] > mine || (best[i * k + j - 1] == mine && i < t);
+      if (better == at) bound = mine;
     }
     __syncthreads();
     for (int i = t; i < n; i += 256)
@@ -352,6 +375,7 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobForward a) {
     for (int i = t; i < n_found; i += 256) {
       const uint64_t p = found[i];
       int better = 0;
+#pragma unroll 8
       for (int j = 0; j < n_found; ++j) better += found[j] > p;
       if (better < k) write_alternative(a, row, better, p, r);
     }
@@ -442,6 +466,80 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobBackward a
                                                   static_cast<char*>(a.dz) + row * a.ldd * (kOutBf16 ? 2 : 4), g0, g1, cols, r, a.scale * kLog2E);
 }
 
+// Loss and gradient in one launch: a workgroup takes a row, sums over it and goes over it again from its end.  The last groups of eight columns stay on the CU between the two --
+// kKeepRegisters of each thread in registers, kKeepLds in LDS --, those in front are read again, from the L2 or the memory-side cache.
+constexpr int kKeepRegisters = 4, kKeepLds = 4;   // of bf16; half as many of FP32
+
+template <bool kBf16, int kN>
+__device__ __forceinline__ void add_groups(Sum& a, const Eight<kBf16> (&x)[kN], float c) {
+  float v[kN * 8];
+#pragma unroll
+  for (int u = 0; u < kN; ++u) {
+    float w[8];
+    x[u].get(w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[u * 8 + i] = w[i];
+  }
+  add<false>(a, v, c);
+}
+
+template <int T, bool kInBf16, bool kOutBf16>
+__global__ __launch_bounds__(T, 8) void logprob_loss_kernel(LogprobForward f, LogprobBackward b) {
+  constexpr int kRegisters = kInBf16 ? kKeepRegisters : kKeepRegisters / 2, kLds = kInBf16 ? kKeepLds : kKeepLds / 2;
+  __shared__ Sum sums[T / 64];
+  __shared__ Eight<kInBf16> kept[kLds * T];
+  const int64_t row = f.row0 + blockIdx.x;
+  const int t = threadIdx.x, cols = static_cast<int>(f.cols), whole = cols >> 3;
+  const void* z = static_cast<const char*>(f.z) + row * f.ld * (kInBf16 ? 2 : 4);
+  void* dz = static_cast<char*>(b.dz) + row * b.ldd * (kOutBf16 ? 2 : 4);
+  const float c = f.scale * kLog2E;
+  const int64_t target = index_at(f.targets, f.i64, row);
+  const bool counted = target >= 0 && target < cols;
+  const float at_target = counted ? value_at<kInBf16>(z, target) : 0.0f, g = b.g_logprob[row];
+
+  const int again = max(0, whole - (kLds + kRegisters) * T), first = again + t;   // groups [0, again) are read twice
+  Sum mine = sum_of_groups<kInBf16, false>(z, 0, again, again * 8, c);
+#pragma unroll
+  for (int u = 0; u < kLds; ++u) {
+    Eight<kInBf16> x[1];
+    if (first + u * T < whole) {
+      x[0].load(z, static_cast<int64_t>(first + u * T) * 8);
+      kept[u * T + t] = x[0];
+      add_groups(mine, x, c);
+    }
+  }
+  Eight<kInBf16> x[kRegisters][1];
+#pragma unroll
+  for (int u = 0; u < kRegisters; ++u)
+    if (first + (kLds + u) * T < whole) x[u][0].load(z, static_cast<int64_t>(first + (kLds + u) * T) * 8);
+#pragma unroll
+  for (int u = 0; u < kRegisters; ++u)
+    if (first + (kLds + u) * T < whole) add_groups(mine, x[u], c);
+  if ((cols & 7) && t == T - 1) {
+    float v[8];
+    rest_of_row<kInBf16>(z, whole, cols, v);
+    add<false>(mine, v, c);
+  }
+  const Sum all = workgroup_join<false>(mine, c, sums);
+  const RowStats r(all);
+  if (t == 0) write_row(f, row, all, r, at_target, counted);
+  const RowGradient d(r.m, r.logsum, f.scale, g, 0.0f, 0.0f, 0.0f, target, cols);
+  auto store = [&](const Eight<kInBf16>& x, int group) {
+    float v[8];
+    x.get(v);
+    d.of<false>(v, group, c);
+    store8(dz, static_cast<int64_t>(group) * 8, kOutBf16, v);
+  };
+  if ((cols & 7) && t == T - 1) gradient_of_rest<kInBf16, kOutBf16, false>(z, dz, whole, cols, d, c);
+#pragma unroll
+  for (int u = kRegisters - 1; u >= 0; --u)
+    if (first + (kLds + u) * T < whole) store(x[u][0], first + (kLds + u) * T);
+#pragma unroll
+  for (int u = kLds - 1; u >= 0; --u)
+    if (first + u * T < whole) store(kept[u * T + t], first + u * T);
+  gradient_of_groups<kInBf16, kOutBf16, false>(z, dz, 0, again, again * 8, d, c);
+}
+
 // ---------------------------------------------------------------- launches
 
 // A launch holds 2^32 threads: rows of one, with `each` threads to a row.
@@ -501,6 +599,33 @@ hipError_t backward_with(const LogprobBackward& a, int threads, hipStream_t s) {
   }
 }
 
+// By bytes of a row, in whose second pass the part that stays on the CU counts, against rows in flight.  us for 8192 rows with 64 / 256 / 512 / 1024 threads: 8 KB 27 / 31 / 46 / 97,
+// 20 KB 91 / 69 / 75 / 124, 40 KB 185 / 135 / 126 / 169, 80 KB 368 / 295 / 252 / 245, 262 KB 1214 / 1123 / 1054 / 873; 1040 rows of 100 KB 72 / 57 / 55 / 61 (1040 of
+// them do not fit the chip's 512 places for 1024 threads), of 200 KB 147 / 139 / 120 / 108.
+int loss_threads(int64_t rows, int64_t cols, bool bf16) {
+  const int64_t bytes = cols * (bf16 ? 2 : 4);
+  return bytes <= 8 << 10 ? 64 : bytes <= 36 << 10 ? 256 : bytes <= (rows >= 8 * kCUs ? 72 << 10 : 160 << 10) ? 512 : 1024;
+}
+
+template <int T>
+hipError_t loss_of(const LogprobForward& f, const LogprobBackward& b, hipStream_t s) {
+  const int64_t most = rows_at_once(T);
+  LogprobForward p = f;
+  for (p.row0 = 0; p.row0 < f.rows; p.row0 += most) {
+    const unsigned rows = static_cast<unsigned>(std::min(most, f.rows - p.row0));
+#define NVFP4_LOSS(I, O) hipLaunchKernelGGL((logprob_loss_kernel<T, I, O>), dim3(rows), dim3(T), 0, s, p, b)
+    if (f.bf16) {
+      if (b.out_bf16) NVFP4_LOSS(true, true); else NVFP4_LOSS(true, false);
+    } else {
+      if (b.out_bf16) NVFP4_LOSS(false, true); else NVFP4_LOSS(false, false);
+    }
+#undef NVFP4_LOSS
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 }  // namespace
 
 size_t logprob_workspace_bytes(int64_t rows, int64_t cols, int top) {
@@ -526,6 +651,10 @@ hipError_t launch_logprob_backward(const LogprobBackward& all, hipStream_t s) {
 }
 
 hipError_t launch_logprob_with_gradient(const LogprobForward& f, const LogprobBackward& b, void* workspace, hipStream_t s) {
+  if (forward_shape(f.rows, f.cols).parts == 1) {
+    const int threads = loss_threads(f.rows, f.cols, f.bf16);
+    return threads == 64 ? loss_of<64>(f, b, s) : threads == 256 ? loss_of<256>(f, b, s) : threads == 512 ? loss_of<512>(f, b, s) : loss_of<1024>(f, b, s);
+  }
   const hipError_t e = launch_logprob_forward(f, workspace, s);
   return e == hipSuccess ? launch_logprob_backward(b, s) : e;
 }
