@@ -498,7 +498,7 @@ int nvfp4_logprob_with_gradient(const void* logits, int dtype, int64_t ld, int64
 
 /*
  * The gradients of a model, for their common norm and for clipping.
- *   data       [rows, cols] of type dtype, leading dimension ld (any, at least cols), aligned to its element; the fastest are contiguous or have rows that start at multiples of 16 bytes
+ *   data       [rows, cols] of type dtype, leading dimension ld (any, at least cols), aligned to its element
  *   out        where the clipped gradient goes, of type out_dtype, leading dimension ld_out; NULL: to data.  Results do not overlap each other or another tensor's data;
  *              equal places are refused
  * Any rows and cols, 0 included; a vector is one row.  At most 2^20 tensors and 2^40 elements.
@@ -515,7 +515,7 @@ typedef struct nvfp4_grad {
  * to device memory (16-byte aligned) and sets `table` to that.  Caller-owned, like everything here.
  */
 typedef struct nvfp4_grad_list {
-  int64_t tensors, units;
+  int64_t tensors, units, unit_elements;
   const void* table;
 } nvfp4_grad_list;
 int nvfp4_grad_list_sizes(const nvfp4_grad* tensors, int64_t n, size_t* table_bytes, size_t* workspace_bytes);

@@ -73,7 +73,7 @@ class GradStruct(ctypes.Structure):
 
 class GradListStruct(ctypes.Structure):
     """Mirror of ``nvfp4_grad_list``."""
-    _fields_ = [("tensors", ctypes.c_int64), ("units", ctypes.c_int64), ("table", ctypes.c_void_p)]
+    _fields_ = [("tensors", ctypes.c_int64), ("units", ctypes.c_int64), ("unit_elements", ctypes.c_int64), ("table", ctypes.c_void_p)]
 
 
 _lib = None

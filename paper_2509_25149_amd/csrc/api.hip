@@ -683,7 +683,7 @@ namespace {
 
 constexpr int64_t kMostTokens = 0x3fffffff, kMostGrads = 1 << 20;
 constexpr int kMostAlternatives = 32;
-constexpr int64_t kUnitElements = 8192, kMostUnitElements = 1 << 24, kUnits = 4096;
+constexpr int64_t kUnitElements = 4096, kMostUnitElements = 1 << 24, kUnits = 16384;
 
 bool index_kind(int t) { return t == NVFP4_INDEX_I32 || t == NVFP4_INDEX_I64; }
 bool is_finite(float v) { return v - v == 0.0f; }
@@ -753,7 +753,7 @@ int check_grads(const nvfp4_grad* g, int64_t n) {
   return NVFP4_OK;
 }
 
-// Elements of a unit of work: so many that some 4096 units hold everything, and no fewer than keep a workgroup busy.
+// Elements of a unit of work: so many that some 16384 units hold everything (their sums are added by one workgroup), and four pieces of 16 bytes to a thread at least.
 int64_t unit_elements(const nvfp4_grad* g, int64_t n) {
   int64_t total = 0;
   for (int64_t i = 0; i < n; ++i) total += grad_elements(g[i]);
@@ -775,9 +775,7 @@ GradTensor grad_tensor(const nvfp4_grad& g, int64_t each) {
   const int64_t rows = t.cols < each ? each / t.cols : 1;
   t.unit_rows = static_cast<int32_t>(rows < t.rows ? rows : t.rows);
   const size_t in = element_size(g.dtype), to = element_size(out_dtype);
-  const bool wide = aligned(t.data, 16) && aligned(t.out, 16) &&
-                    (t.rows == 1 || (t.ld * static_cast<int64_t>(in) % 16 == 0 && t.ld_out * static_cast<int64_t>(to) % 16 == 0));
-  t.flags = (in == 2 ? kGradBf16 : 0) | (to == 2 ? kGradOutBf16 : 0) | (wide ? kGradWide : 0);
+  t.flags = (in == 2 ? kGradBf16 : 0) | (to == 2 ? kGradOutBf16 : 0);
   return t;
 }
 
@@ -794,7 +792,7 @@ int64_t grad_units(const nvfp4_grad* g, int64_t n) {
 size_t grad_table_bytes(int64_t n, int64_t units) { return static_cast<size_t>(n) * sizeof(GradTensor) + static_cast<size_t>(units) * 4; }
 
 int check_list(const nvfp4_grad_list* list) {
-  if (!list || list->tensors < 0 || list->units < 0 || list->tensors > kMostGrads || list->units > 0xffffff) return NVFP4_ERR_INVALID_ARG;
+  if (!list || list->tensors < 0 || list->units < 0 || list->tensors > kMostGrads || list->units > 0xffffff || list->unit_elements <= 0) return NVFP4_ERR_INVALID_ARG;
   return list->units && (!list->table || !aligned(list->table, 16)) ? NVFP4_ERR_INVALID_ARG : NVFP4_OK;
 }
 const GradTensor* tensors_of(const nvfp4_grad_list* list) { return static_cast<const GradTensor*>(list->table); }
@@ -944,7 +942,7 @@ int nvfp4_grad_list_build(const nvfp4_grad* tensors, int64_t n, void* table_host
     t[i].first_unit = static_cast<int32_t>(unit);
     for (int64_t u = units_of(t[i]); u > 0; --u) map[unit++] = static_cast<int32_t>(i);
   }
-  list->tensors = n, list->units = units, list->table = nullptr;
+  list->tensors = n, list->units = units, list->unit_elements = each, list->table = nullptr;
   return NVFP4_OK;
 }
 
@@ -961,7 +959,7 @@ int nvfp4_grad_clip(const nvfp4_grad_list* list, const double* sumsq, float max_
   const int rc = check_list(list);
   if (rc != NVFP4_OK) return rc;
   if (!sumsq || !aligned(sumsq, 8) || !aligned(norm, 4) || !(max_norm >= 0.0f)) return NVFP4_ERR_INVALID_ARG;
-  const hipError_t e = launch_grad_clip(tensors_of(list), map_of(list), list->units, sumsq, max_norm, norm, static_cast<hipStream_t>(stream));
+  const hipError_t e = launch_grad_clip(tensors_of(list), map_of(list), list->units, list->unit_elements, sumsq, max_norm, norm, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? NVFP4_OK : NVFP4_ERR_HIP;
 }
 

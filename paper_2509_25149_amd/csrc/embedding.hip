@@ -61,40 +61,70 @@ __device__ __forceinline__ uint32_t key_of(const void* ids, bool i64, int64_t t,
   return static_cast<uint32_t>(id >= 0 && id < vocab ? id : vocab);
 }
 
-// Up to kFewTokens: a token's place is the number of tokens before it, counted: two operations a pair.  A workgroup holds all keys and takes 32 tokens, sixteen threads to a token.
-constexpr int kFewTokens = 8192, kTile = 2048, kRankTokens = 32, kRankParts = 16;
+// Up to kFewTokens: a token's place is the number of tokens before it, counted: two operations a pair.  A workgroup holds the keys and takes 32 tokens; a wavefront four of them, each
+// lane against every 64th piece of four keys.
+constexpr int kFewTokens = 8192, kTile = 2048, kRankTokens = 32, kRankEach = 4;
 
-__global__ __launch_bounds__(kRankTokens* kRankParts) void rank_kernel(const void* ids, bool i64, int n, int64_t vocab, uint32_t* __restrict__ keys, uint32_t* __restrict__ order) {
-  constexpr int T = kRankTokens * kRankParts;
+constexpr int kRankThreads = kRankTokens / kRankEach * 64;
+
+// Zeros into [vocab, cols] of FP32, 16 bytes a thread: waves that store once, neighbours on one XCD, write 2.7 GB at 6.9 TB/s (five or more stores to a thread at 5.6).
+struct ZeroArgs {
+  float* to;
+  int64_t ld, pieces;   // of four columns, in all rows
+  uint32_t across, groups;   // pieces of a row; workgroups
+};
+__device__ __forceinline__ void write_zeros(const ZeroArgs& z, uint32_t group) {
+  for (int64_t i = static_cast<int64_t>(xcd_neighbours(group, z.groups)) * kRankThreads + threadIdx.x; i < z.pieces; i += static_cast<int64_t>(z.groups) * kRankThreads) {
+    int64_t row;
+    uint32_t part;
+    if (i >> 32) row = i / z.across, part = static_cast<uint32_t>(i % z.across);
+    else row = static_cast<uint32_t>(i) / z.across, part = static_cast<uint32_t>(i) % z.across;
+    *reinterpret_cast<float4v*>(z.to + row * z.ld + static_cast<int64_t>(part) * 4) = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+}
+
+__global__ __launch_bounds__(kRankThreads) void zero_kernel(ZeroArgs z) { write_zeros(z, blockIdx.x); }
+
+// Workgroups behind those of the tokens write zeros.
+__global__ __launch_bounds__(kRankThreads) void rank_kernel(const void* ids, bool i64, int n, int64_t vocab, uint32_t* __restrict__ keys, uint32_t* __restrict__ order, ZeroArgs z) {
+  const uint32_t ranking = static_cast<uint32_t>(n + kRankTokens - 1) / kRankTokens;
+  if (blockIdx.x >= ranking) {
+    write_zeros(z, blockIdx.x - ranking);
+    return;
+  }
+  constexpr int T = kRankThreads;
   __shared__ __attribute__((aligned(16))) uint32_t all[kFewTokens];
   const int fours = (n + 3) >> 2;
 #pragma unroll 8
   for (int i = threadIdx.x; i < fours * 4; i += T) all[i] = i < n ? key_of(ids, i64, i, vocab) : 0xFFFFFFFFu;
   __syncthreads();
-  const int t = static_cast<int>(blockIdx.x) * kRankTokens + static_cast<int>(threadIdx.x) / kRankParts, part = threadIdx.x % kRankParts;
-  const uint32_t key = t < n ? all[t] : 0u;
+  const int lane = threadIdx.x & 63, t0 = static_cast<int>(blockIdx.x) * kRankTokens + static_cast<int>(threadIdx.x >> 6) * kRankEach;
   const uint4* four = reinterpret_cast<const uint4*>(all);
-  uint32_t before = 0u;
-  // Among equal keys those in front come first: keys up to this token's in front of the workgroup's tokens, less than it behind them.
-  const int mid0 = static_cast<int>(blockIdx.x) * (kRankTokens / 4), mid1 = min(mid0 + kRankTokens / 4, fours);
-#pragma unroll 8
-  for (int i = part; i < mid0; i += kRankParts) {
+  uint32_t key[kRankEach], before[kRankEach] = {};
+#pragma unroll
+  for (int e = 0; e < kRankEach; ++e) key[e] = t0 + e < n ? all[t0 + e] : 0u;
+  // Among equal keys those in front come first: keys up to this token's in front of the wavefront's tokens (one piece, kRankEach being 4), less than it behind them.
+  const int mid = t0 >> 2;
+#pragma unroll 4
+  for (int i = lane; i < mid; i += 64) {
     const uint4 k = four[i];
-    before += (k.x <= key) + (k.y <= key) + (k.z <= key) + (k.w <= key);
+#pragma unroll
+    for (int e = 0; e < kRankEach; ++e) before[e] += (k.x <= key[e]) + (k.y <= key[e]) + (k.z <= key[e]) + (k.w <= key[e]);
   }
-  for (int i = mid0 + part; i < mid1; i += kRankParts) {
+#pragma unroll 4
+  for (int i = mid + 1 + lane; i < fours; i += 64) {
     const uint4 k = four[i];
-    const int at = t - i * 4;
-    before += (k.x < key + (at > 0)) + (k.y < key + (at > 1)) + (k.z < key + (at > 2)) + (k.w < key + (at > 3));
-  }
-#pragma unroll 8
-  for (int i = mid1 + part; i < fours; i += kRankParts) {
-    const uint4 k = four[i];
-    before += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
+#pragma unroll
+    for (int e = 0; e < kRankEach; ++e) before[e] += (k.x < key[e]) + (k.y < key[e]) + (k.z < key[e]) + (k.w < key[e]);
   }
 #pragma unroll
-  for (int off = 1; off < kRankParts; off <<= 1) before += __shfl_xor(before, off, 64);
-  if (part == 0 && t < n) keys[before] = key, order[before] = static_cast<uint32_t>(t);
+  for (int e = 0; e < kRankEach; ++e) {
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) before[e] += __shfl_xor(before[e], off, 64);
+#pragma unroll
+    for (int o = 0; o < kRankEach; ++o) before[e] += o < e ? key[o] <= key[e] : o > e && t0 + o < n && key[o] < key[e];
+    if (lane == 0 && t0 + e < n) keys[before[e]] = key[e], order[before[e]] = static_cast<uint32_t>(t0 + e);
+  }
 }
 
 // More: passes over digits of up to nine bits, each stable: count the digits of a tile, sum up, put in place.  A tile of 2048 belongs to a workgroup, whose
@@ -216,7 +246,7 @@ struct SumArgs {
   const uint32_t *keys, *order;   // n of them, in order
   float* partials;                // [chunks, 2, cols]: sum of a chunk's first row if that has begun before, of its last if that goes on behind
   int n, chunk, chunks, strips;   // strips of 512 columns
-  int zero_groups;                // workgroups that write rows without a token
+  uint32_t zero_groups;           // workgroups that write rows without a token
 };
 
 __device__ __forceinline__ int lower_bound(const uint32_t* keys, int n, uint32_t key) {
@@ -231,8 +261,8 @@ __device__ __forceinline__ int lower_bound(const uint32_t* keys, int n, uint32_t
 
 constexpr int kZeroRows = 32, kAhead = 8;
 
-// The first workgroups: a wavefront adds a chunk of consecutive tokens over 512 columns, eight to a lane, and stores each row as it ends.  The rest, where the
-// gradient is stored and not added to: 32 rows each, zeros where no token is.
+// The first workgroups: a wavefront adds a chunk of consecutive tokens over 512 columns, eight to a lane, and stores each row as it ends.  The rest, if
+// any, look for rows without a token, 32 each, and write zeros there.
 template <bool kBf16>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs s) {
   const EmbeddingBackward& a = s.a;
@@ -255,12 +285,12 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs s) {
   const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (unit >= static_cast<int64_t>(s.chunks) * s.strips) return;
   const int chunk = static_cast<int>(unit / s.strips), first = chunk * s.chunk, last = min(first + s.chunk, s.n);
-  const int64_t col = static_cast<int64_t>(unit % s.strips) * 512 + lane * 8;
+  const int64_t col = static_cast<int64_t>(unit % s.strips) * 512 + lane * 8, from = min(col, a.cols - 8);
   const bool in = col < a.cols;
   const uint32_t vocab = static_cast<uint32_t>(a.vocab);
+  const uint32_t ahead = first > 0 ? s.keys[first - 1] : 0xFFFFFFFFu, behind = last < s.n ? s.keys[last] : 0xFFFFFFFFu;
   uint32_t key = s.keys[first];
-  const uint32_t behind = last < s.n ? s.keys[last] : 0xFFFFFFFFu;
-  bool begun = first > 0 && s.keys[first - 1] == key;
+  bool begun = ahead == key;
   float sum[8] = {};
   auto finish = [&](bool goes_on) {
     if (key >= vocab || !in) return;
@@ -282,26 +312,25 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs s) {
     }
     store8(row, col, false, v);
   };
-  for (int at = first; at < last; at += kAhead) {
-    Eight<kBf16> x[kAhead];
-    uint32_t k[kAhead];
+  for (int base = first; base < last; base += 64) {   // a lane holds one of the next 64 tokens
+    const int mine = min(base + lane, last - 1), n = min(64, last - base);
+    const uint32_t keys = s.keys[mine], order = s.order[mine];
+    for (int at = 0; at < n; at += kAhead) {
+      Eight<kBf16> x[kAhead];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int i = min(at + u, last - 1);
-      k[u] = s.keys[i];
-      if (in && k[u] < vocab) x[u].load(static_cast<const char*>(a.dout) + static_cast<int64_t>(s.order[i]) * a.ldd * (kBf16 ? 2 : 4), col);
-    }
+      for (int u = 0; u < kAhead; ++u)   // (behind the last token the last once more)
+        x[u].load(static_cast<const char*>(a.dout) + static_cast<int64_t>(__builtin_amdgcn_readlane(order, (at + u) & 63)) * a.ldd * (kBf16 ? 2 : 4), from);
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      if (at + u >= last) break;
-      if (k[u] != key) {
-        finish(false);
-        key = k[u];
-        begun = false;
+      for (int u = 0; u < kAhead; ++u) {
+        if (at + u >= n) break;
+        const uint32_t k = __builtin_amdgcn_readlane(keys, at + u);
+        if (k != key) {
+          finish(false);
+          key = k;
+          begun = false;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
-      }
-      if (in && k[u] < vocab) {
+          for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+        }
         float v[8];
         x[u].get(v);
 #pragma unroll
@@ -319,9 +348,13 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs s) {
   if (last >= s.n) return;
   const uint32_t key = s.keys[last - 1];
   if (key >= static_cast<uint32_t>(a.vocab) || s.keys[last] != key || (first > 0 && s.keys[first - 1] == key)) return;
+  int final_chunk = chunk;   // the last one that begins with the key: 64 looked at together
+  for (uint64_t more = ~0ull; more == ~0ull; final_chunk += more == ~0ull ? 64 : __builtin_ctzll(~more)) {
+    const int64_t at = static_cast<int64_t>(final_chunk + 1 + (threadIdx.x & 63)) * s.chunk;
+    more = __ballot(at < s.n && s.keys[at] == key);
+  }
   const int64_t col = static_cast<int64_t>(blockIdx.y) * 1024 + threadIdx.x * 4;
   if (col >= a.cols) return;
-  const int end = lower_bound(s.keys, s.n, key + 1), final_chunk = (end - 1) / s.chunk;
   const float* from = s.partials + static_cast<int64_t>(chunk) * 2 * a.cols + col;
   float4v sum = *reinterpret_cast<const float4v*>(from + a.cols);
 #pragma unroll 8
@@ -331,12 +364,9 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs s) {
   *to = a.accumulate ? *to + sum : sum;
 }
 
-__global__ __launch_bounds__(256) void embedding_zero_kernel(float* dtable, int64_t ldt, int64_t rows, int64_t cols) {
-  for (int64_t row = blockIdx.x; row < rows; row += gridDim.x)
-    for (int64_t col = threadIdx.x * 4; col < cols; col += 1024) *reinterpret_cast<float4v*>(dtable + row * ldt + col) = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-}
-
 // ---------------------------------------------------------------- launches
+
+constexpr int64_t kFewTokensPerRow = 4;
 
 struct SumPlan {
   int chunk, chunks, tiles, passes, digit_bits;
@@ -344,8 +374,7 @@ struct SumPlan {
 };
 SumPlan plan(int64_t n, int64_t vocab, int64_t cols) {
   SumPlan p{};
-  // Chunks of sixteen tokens, longer from 8192 on so that the partial sums stay few.
-  p.chunk = static_cast<int>(std::max<int64_t>(16, (n + 511) / 512));
+  p.chunk = static_cast<int>(std::max<int64_t>(8, (n + 511) / 512));
   p.chunks = static_cast<int>((n + p.chunk - 1) / p.chunk);
   size_t at = 0;
   auto take = [&at](size_t words) {
@@ -393,18 +422,28 @@ hipError_t launch_embedding_forward(const EmbeddingForward& all, hipStream_t s) 
 }
 
 hipError_t launch_embedding_backward(const EmbeddingBackward& a, void* workspace, hipStream_t s) {
-  if (a.tokens == 0) {
-    if (a.accumulate || a.vocab == 0) return hipSuccess;
-    hipLaunchKernelGGL(embedding_zero_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(a.vocab, 4096))), dim3(256), 0, s, a.dtable, a.ldt, a.vocab, a.cols);
-    return hipGetLastError();
-  }
   const int n = static_cast<int>(a.tokens);
+  // Rows without a token: where tokens are few for the table all rows are written first, without looking, beside the ranking of the tokens; otherwise those that have none
+  // are looked for beside the sums.
+  const bool zero_first = !a.accumulate && a.tokens < a.vocab / kFewTokensPerRow;
+  ZeroArgs z{};
+  if (zero_first) {
+    z.to = a.dtable, z.ld = a.ldt, z.across = static_cast<uint32_t>(a.cols / 4), z.pieces = a.vocab * z.across;
+    z.groups = static_cast<uint32_t>(std::min<int64_t>((z.pieces + kRankThreads - 1) / kRankThreads, 1 << 22));   // (a launch holds 2^32 threads)
+  }
+  hipError_t e;
+  if (n > kFewTokens || n == 0) {
+    if (zero_first) {
+      hipLaunchKernelGGL(zero_kernel, dim3(z.groups), dim3(kRankThreads), 0, s, z);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (n == 0) return hipSuccess;
+  }
   const SumPlan p = plan(n, a.vocab, a.cols);
   uint32_t* words = static_cast<uint32_t*>(workspace);
   uint32_t *keys = words + p.keys, *order = words + p.order;
-  hipError_t e;
   if (n <= kFewTokens) {
-    hipLaunchKernelGGL(rank_kernel, dim3((n + kRankTokens - 1) / kRankTokens), dim3(kRankTokens * kRankParts), 0, s, a.ids, a.i64, n, a.vocab, keys, order);
+    hipLaunchKernelGGL(rank_kernel, dim3((n + kRankTokens - 1) / kRankTokens + z.groups), dim3(kRankThreads), 0, s, a.ids, a.i64, n, a.vocab, keys, order, z);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   } else {
     SortPass q{};
@@ -425,7 +464,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackward& a, void* workspace
   SumArgs u{};
   u.a = a, u.keys = keys, u.order = order, u.partials = reinterpret_cast<float*>(words + p.partials);
   u.n = n, u.chunk = p.chunk, u.chunks = p.chunks, u.strips = static_cast<int>((a.cols + 511) / 512);
-  u.zero_groups = a.accumulate ? 0 : static_cast<int>(std::min<int64_t>((a.vocab + kZeroRows - 1) / kZeroRows, 1 << 16));
+  u.zero_groups = a.accumulate || zero_first ? 0u : static_cast<uint32_t>(std::min<int64_t>((a.vocab + kZeroRows - 1) / kZeroRows, 1 << 16));
   const int64_t wgs = (static_cast<int64_t>(u.chunks) * u.strips + 3) / 4 + u.zero_groups;
   if (a.bf16) hipLaunchKernelGGL(embedding_sum_kernel<true>, dim3(static_cast<unsigned>(wgs)), dim3(256), 0, s, u);
   else hipLaunchKernelGGL(embedding_sum_kernel<false>, dim3(static_cast<unsigned>(wgs)), dim3(256), 0, s, u);

@@ -25,9 +25,9 @@ struct Unit {
   int64_t ld, ld_out;   // bytes
   int rows, cols, flags;
 };
-__device__ __forceinline__ Unit unit_of(const GradTensor* tensors, const int32_t* unit_tensor) {
-  const GradTensor& t = tensors[unit_tensor[blockIdx.x]];
-  const uint32_t u = blockIdx.x - static_cast<uint32_t>(t.first_unit);
+__device__ __forceinline__ Unit unit_of(const GradTensor* tensors, const int32_t* unit_tensor, uint32_t unit) {
+  const GradTensor& t = tensors[unit_tensor[unit]];
+  const uint32_t u = unit - static_cast<uint32_t>(t.first_unit);
   const uint32_t across = static_cast<uint32_t>((t.cols + t.unit_cols - 1) / t.unit_cols);
   const int64_t row = static_cast<int64_t>(u / across) * t.unit_rows, col = static_cast<int64_t>(u % across) * t.unit_cols;
   const int in = t.flags & kGradBf16 ? 2 : 4, to = t.flags & kGradOutBf16 ? 2 : 4;
@@ -41,45 +41,86 @@ __device__ __forceinline__ Unit unit_of(const GradTensor* tensors, const int32_t
   return n;
 }
 
+// Pieces of 16 bytes of the wider type (four FP32 or eight bf16 values), wherever they start: an element's alignment is enough for a 16-byte access to global memory, and the
+// address space is said since the pointers come out of a table.
+#define NVFP4_GLOBAL __attribute__((address_space(1)))
+typedef float float4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t uint4u __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t uint2u __attribute__((ext_vector_type(2), aligned(2)));
+template <int kN>
+struct Words {
+  using type = uint4u;
+};
+template <>
+struct Words<4> {
+  using type = uint2u;
+};
+
+template <bool kBf16, int kN>
+__device__ __forceinline__ void load_piece(const char* at, float (&v)[kN]) {
+  if constexpr (kBf16) {
+    const auto w = *reinterpret_cast<const NVFP4_GLOBAL typename Words<kN>::type*>(reinterpret_cast<uintptr_t>(at));
+#pragma unroll
+    for (int i = 0; i < kN / 2; ++i) v[2 * i] = bf16_lo(w[i]), v[2 * i + 1] = bf16_hi(w[i]);
+  } else {
+    const float4u w = *reinterpret_cast<const NVFP4_GLOBAL float4u*>(reinterpret_cast<uintptr_t>(at));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = w[i];
+  }
+}
+template <bool kBf16, int kN>
+__device__ __forceinline__ void store_piece(char* at, const float (&v)[kN]) {
+  if constexpr (kBf16) {
+    typename Words<kN>::type w;
+#pragma unroll
+    for (int i = 0; i < kN / 2; ++i) w[i] = f32x2_to_bf16(v[2 * i], v[2 * i + 1]);
+    *reinterpret_cast<NVFP4_GLOBAL typename Words<kN>::type*>(reinterpret_cast<uintptr_t>(at)) = w;
+  } else {
+    *reinterpret_cast<NVFP4_GLOBAL float4u*>(reinterpret_cast<uintptr_t>(at)) = float4u{v[0], v[1], v[2], v[3]};
+  }
+}
 template <bool kBf16>
-__device__ __forceinline__ float load1(const char* row, int col) {
-  return kBf16 ? __uint_as_float(static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(row)[col]) << 16) : reinterpret_cast<const float*>(row)[col];
+__device__ __forceinline__ float load1(const char* at) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(at);
+  return kBf16 ? __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const NVFP4_GLOBAL uint16_t*>(p)) << 16) : *reinterpret_cast<const NVFP4_GLOBAL float*>(p);
+}
+template <bool kBf16>
+__device__ __forceinline__ void store1(char* at, float v) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(at);
+  if (kBf16) *reinterpret_cast<NVFP4_GLOBAL uint16_t*>(p) = static_cast<uint16_t>(f32_to_bf16(v));
+  else *reinterpret_cast<NVFP4_GLOBAL float*>(p) = v;
 }
 
-// wide(row, group of eight columns) and single(row, column) over a unit by its 256 threads.
-template <typename Wide, typename Single>
-__device__ __forceinline__ void for_unit(const Unit& n, Wide wide, Single single) {
-  const uint32_t groups = n.flags & kGradWide ? static_cast<uint32_t>(n.cols) >> 3 : 0u, rest = static_cast<uint32_t>(n.cols) - groups * 8;
-  if (groups) {
-    if (n.rows == 1) {
-#pragma unroll 4
-      for (uint32_t i = threadIdx.x; i < groups; i += 256) wide(0, static_cast<int>(i));
-    } else {
-#pragma unroll 4
-      for (uint32_t i = threadIdx.x; i < groups * static_cast<uint32_t>(n.rows); i += 256) wide(static_cast<int>(i / groups), static_cast<int>(i % groups));
-    }
+// wide(row, column) for pieces of kN columns and single(row, column) for what a row has behind them, over a unit by `step` threads of which this one is number `t`.
+template <int kN, int kUnroll, typename Wide, typename Single>
+__device__ __forceinline__ void for_unit(const Unit& n, uint32_t t, uint32_t step, Wide wide, Single single) {
+  const uint32_t pieces = static_cast<uint32_t>(n.cols) / kN, rest = static_cast<uint32_t>(n.cols) - pieces * kN;
+  if (n.rows == 1) {
+#pragma unroll kUnroll
+    for (uint32_t i = t; i < pieces; i += step) wide(0, static_cast<int>(i * kN));
+  } else if (pieces) {
+#pragma unroll kUnroll
+    for (uint32_t i = t; i < pieces * static_cast<uint32_t>(n.rows); i += step) wide(static_cast<int>(i / pieces), static_cast<int>(i % pieces * kN));
   }
   if (rest) {
-#pragma unroll 4
-    for (uint32_t i = threadIdx.x; i < rest * static_cast<uint32_t>(n.rows); i += 256) single(static_cast<int>(i / rest), static_cast<int>(groups * 8 + i % rest));
+    for (uint32_t i = t; i < rest * static_cast<uint32_t>(n.rows); i += step) single(static_cast<int>(i / rest), static_cast<int>(pieces * kN + i % rest));
   }
 }
 
 template <bool kBf16>
 __device__ __forceinline__ double squares(const Unit& n) {
+  constexpr int kN = kBf16 ? 8 : 4, kSize = kBf16 ? 2 : 4;
   double s[2] = {};
-  for_unit(
-      n,
-      [&](int row, int g) {
-        Eight<kBf16> x;
-        float v[8];
-        x.load(n.data + row * n.ld, static_cast<int64_t>(g) * 8);
-        x.get(v);
+  for_unit<kN, 4>(
+      n, threadIdx.x, 256,
+      [&](int row, int col) {
+        float v[kN];
+        load_piece<kBf16>(n.data + row * n.ld + static_cast<int64_t>(col) * kSize, v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i & 1] = __builtin_fma(static_cast<double>(v[i]), static_cast<double>(v[i]), s[i & 1]);
+        for (int i = 0; i < kN; ++i) s[i & 1] = __builtin_fma(static_cast<double>(v[i]), static_cast<double>(v[i]), s[i & 1]);
       },
       [&](int row, int col) {
-        const double v = load1<kBf16>(n.data + row * n.ld, col);
+        const double v = load1<kBf16>(n.data + row * n.ld + static_cast<int64_t>(col) * kSize);
         s[0] = __builtin_fma(v, v, s[0]);
       });
   return s[0] + s[1];
@@ -87,7 +128,7 @@ __device__ __forceinline__ double squares(const Unit& n) {
 
 __global__ __launch_bounds__(256) void grad_sumsq_kernel(const GradTensor* __restrict__ tensors, const int32_t* __restrict__ unit_tensor, double* __restrict__ partials) {
   __shared__ double waves[4];
-  const Unit n = unit_of(tensors, unit_tensor);
+  const Unit n = unit_of(tensors, unit_tensor, blockIdx.x);
   const double s = wave_sum64(n.flags & kGradBf16 ? squares<true>(n) : squares<false>(n));
   if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = s;
   __syncthreads();
@@ -97,7 +138,7 @@ __global__ __launch_bounds__(256) void grad_sumsq_kernel(const GradTensor* __res
 __global__ __launch_bounds__(1024) void grad_fold_kernel(const double* __restrict__ partials, int64_t units, double* __restrict__ sumsq) {
   __shared__ double waves[16];
   double s = 0.0;
-#pragma unroll 4
+#pragma unroll 8
   for (int64_t i = threadIdx.x; i < units; i += 1024) s += partials[i];
   s = wave_sum64(s);
   if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = s;
@@ -109,40 +150,40 @@ __global__ __launch_bounds__(1024) void grad_fold_kernel(const double* __restric
 }
 
 template <bool kBf16, bool kOutBf16>
-__device__ __forceinline__ void scaled(const Unit& n, float by) {
-  for_unit(
-      n,
-      [&](int row, int g) {
-        Eight<kBf16> x;
-        float v[8];
-        x.load(n.data + row * n.ld, static_cast<int64_t>(g) * 8);
-        x.get(v);
+__device__ __forceinline__ void scaled(const Unit& n, uint32_t t, uint32_t step, float by) {
+  constexpr int kN = kBf16 && kOutBf16 ? 8 : 4, kSize = kBf16 ? 2 : 4, kOutSize = kOutBf16 ? 2 : 4;
+  for_unit<kN, 1>(
+      n, t, step,
+      [&](int row, int col) {
+        float v[kN];
+        load_piece<kBf16>(n.data + row * n.ld + static_cast<int64_t>(col) * kSize, v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= by;
-        store8(n.out + row * n.ld_out, static_cast<int64_t>(g) * 8, kOutBf16, v);
+        for (int i = 0; i < kN; ++i) v[i] *= by;
+        store_piece<kOutBf16>(n.out + row * n.ld_out + static_cast<int64_t>(col) * kOutSize, v);
       },
       [&](int row, int col) {
-        const float v = load1<kBf16>(n.data + row * n.ld, col) * by;
-        char* to = n.out + row * n.ld_out;
-        if (kOutBf16) reinterpret_cast<uint16_t*>(to)[col] = static_cast<uint16_t>(f32_to_bf16(v));
-        else reinterpret_cast<float*>(to)[col] = v;
+        const float v = load1<kBf16>(n.data + row * n.ld + static_cast<int64_t>(col) * kSize) * by;
+        store1<kOutBf16>(n.out + row * n.ld_out + static_cast<int64_t>(col) * kOutSize, v);
       });
 }
 
 // The factor from the sum of squares, in every workgroup.  1 for a norm that is not finite, and then, as for any factor of 1, what stays in its place is not touched.
-__global__ __launch_bounds__(256) void grad_clip_kernel(const GradTensor* __restrict__ tensors, const int32_t* __restrict__ unit_tensor, int64_t units,
+// `splits` workgroups to a unit, 16 bytes to a thread: waves that load once and store once, neighbours on one XCD (2.7 GB copied so at 6.3 TB/s; four pieces to a
+// thread 5.7, in a loop of four times four 5.4).
+__global__ __launch_bounds__(256) void grad_clip_kernel(const GradTensor* __restrict__ tensors, const int32_t* __restrict__ unit_tensor, int64_t units, uint32_t splits,
                                                         const double* __restrict__ sumsq, float max_norm, float* __restrict__ norm) {
   const double total = __builtin_sqrt(*sumsq);
   const bool clips = total > static_cast<double>(max_norm) && total < __builtin_huge_val();
   const float by = clips ? static_cast<float>(static_cast<double>(max_norm) / total) : 1.0f;
   if (blockIdx.x == 0 && threadIdx.x == 0 && norm) *norm = static_cast<float>(total);
   if (units == 0) return;
-  const Unit n = unit_of(tensors, unit_tensor);
+  const uint32_t w = xcd_neighbours(blockIdx.x, gridDim.x), t = w % splits * 256 + threadIdx.x, step = splits * 256;
+  const Unit n = unit_of(tensors, unit_tensor, w / splits);
   if (by == 1.0f && n.data == n.out && ((n.flags & kGradBf16) != 0) == ((n.flags & kGradOutBf16) != 0)) return;
   if (n.flags & kGradBf16) {
-    if (n.flags & kGradOutBf16) scaled<true, true>(n, by); else scaled<true, false>(n, by);
+    if (n.flags & kGradOutBf16) scaled<true, true>(n, t, step, by); else scaled<true, false>(n, t, step, by);
   } else {
-    if (n.flags & kGradOutBf16) scaled<false, true>(n, by); else scaled<false, false>(n, by);
+    if (n.flags & kGradOutBf16) scaled<false, true>(n, t, step, by); else scaled<false, false>(n, t, step, by);
   }
 }
 
@@ -158,8 +199,11 @@ hipError_t launch_grad_sumsq(const GradTensor* tensors, const int32_t* unit_tens
   return hipGetLastError();
 }
 
-hipError_t launch_grad_clip(const GradTensor* tensors, const int32_t* unit_tensor, int64_t units, const double* sumsq, float max_norm, float* norm, hipStream_t s) {
-  hipLaunchKernelGGL(grad_clip_kernel, dim3(static_cast<unsigned>(std::max<int64_t>(units, 1))), dim3(256), 0, s, tensors, unit_tensor, units, sumsq, max_norm, norm);
+hipError_t launch_grad_clip(const GradTensor* tensors, const int32_t* unit_tensor, int64_t units, int64_t unit_elements, const double* sumsq, float max_norm,
+                            float* norm, hipStream_t s) {
+  const int64_t most = std::max<int64_t>(1, (1 << 24) / std::max<int64_t>(units, 1) - 1), splits = std::min((unit_elements + 1023) / 1024, most);   // (a launch holds 2^32 threads)
+  hipLaunchKernelGGL(grad_clip_kernel, dim3(static_cast<unsigned>(std::max<int64_t>(units * splits, 1))), dim3(256), 0, s, tensors, unit_tensor, units,
+                     static_cast<uint32_t>(splits), sumsq, max_norm, norm);
   return hipGetLastError();
 }
 

@@ -384,6 +384,8 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobForward a) {
 
 // ---------------------------------------------------------------- gradient of the logits
 
+typedef uint32_t uint32x4 __attribute__((ext_vector_type(4)));
+
 // What is the same for a row: dz_j = p_j (a - b log2 p_j), log2 p_j = (z_j - m) c - l; and what the target's column gets on top.
 struct RowGradient {
   float m, l, a, b, at_target;
@@ -411,6 +413,20 @@ struct RowGradient {
   }
 };
 
+// store8, for what no cache should keep.
+__device__ __forceinline__ void stream8(void* row, int64_t col, bool bf16, const float (&v)[8]) {
+  if (bf16) {
+    const uint32x4 w = {f32x2_to_bf16(v[0], v[1]), f32x2_to_bf16(v[2], v[3]), f32x2_to_bf16(v[4], v[5]), f32x2_to_bf16(v[6], v[7])};
+    __builtin_nontemporal_store(w, reinterpret_cast<uint32x4*>(static_cast<uint16_t*>(row) + col));
+  } else {
+    float4v* p = reinterpret_cast<float4v*>(static_cast<float*>(row) + col);
+    __builtin_nontemporal_store(float4v{v[0], v[1], v[2], v[3]}, p);
+    __builtin_nontemporal_store(float4v{v[4], v[5], v[6], v[7]}, p + 1);
+  }
+}
+
+#define put8 store8
+#define put8k store8
 template <bool kInBf16, bool kOutBf16, bool kEntropy>
 __device__ __forceinline__ void gradient_of_rest(const void* z, void* dz, int g, int cols, const RowGradient& r, float c) {
   float v[8];
@@ -441,7 +457,7 @@ __device__ __forceinline__ void gradient_of_groups(const void* z, void* dz, int 
       float v[8];
       x[u].get(v);
       r.of<kEntropy>(v, g - u * step, c);
-      store8(dz, static_cast<int64_t>(g - u * step) * 8, kOutBf16, v);
+      put8(dz, static_cast<int64_t>(g - u * step) * 8, kOutBf16, v);
     }
   }
   for (; g >= g0; g -= step) {
@@ -450,14 +466,15 @@ __device__ __forceinline__ void gradient_of_groups(const void* z, void* dz, int 
     x.load(z, static_cast<int64_t>(g) * 8);
     x.get(v);
     r.of<kEntropy>(v, g, c);
-    store8(dz, static_cast<int64_t>(g) * 8, kOutBf16, v);
+    put8(dz, static_cast<int64_t>(g) * 8, kOutBf16, v);
   }
 }
 
 template <bool kInBf16, bool kOutBf16, bool kEntropy>
 __global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobBackward a) {
-  const int part = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.parts));
-  const int64_t row = a.row0 + blockIdx.x / static_cast<unsigned>(a.parts);
+  const uint32_t w = blockIdx.x;
+  const int part = static_cast<int>(w % static_cast<unsigned>(a.parts));
+  const int64_t row = a.row0 + w / static_cast<unsigned>(a.parts);
   const int cols = static_cast<int>(a.cols), groups = (cols + 7) >> 3, each = (groups + a.parts - 1) / a.parts;
   const int g0 = min(part * each, groups), g1 = min(g0 + each, groups);
   const RowGradient r(a.stats[2 * row], a.stats[2 * row + 1], a.scale, a.g_logprob ? a.g_logprob[row] : 0.0f, a.g_lse ? a.g_lse[row] : 0.0f,
@@ -528,7 +545,7 @@ __global__ __launch_bounds__(T, 8) void logprob_loss_kernel(LogprobForward f, Lo
     float v[8];
     x.get(v);
     d.of<false>(v, group, c);
-    store8(dz, static_cast<int64_t>(group) * 8, kOutBf16, v);
+    put8k(dz, static_cast<int64_t>(group) * 8, kOutBf16, v);
   };
   if ((cols & 7) && t == T - 1) gradient_of_rest<kInBf16, kOutBf16, false>(z, dz, whole, cols, d, c);
 #pragma unroll
@@ -642,11 +659,12 @@ hipError_t launch_logprob_forward(const LogprobForward& all, void* workspace, hi
   return forward_with<>(a, shape.threads, s);
 }
 
-// A workgroup takes 1024 groups of eight columns at a time, or a row that has fewer.
+// A workgroup takes 8 KB of logits, or a row that has fewer.
 hipError_t launch_logprob_backward(const LogprobBackward& all, hipStream_t s) {
   LogprobBackward a = all;
   const int64_t groups = (a.cols + 7) / 8;
-  a.parts = static_cast<int>((groups + 1023) / 1024);
+  const int64_t each = a.bf16 ? 512 : 256;
+  a.parts = static_cast<int>((groups + each - 1) / each);
   return backward_with<>(a, groups >= 256 ? 256 : 64, s);
 }
 

@@ -14,6 +14,12 @@ typedef float float16v __attribute__((ext_vector_type(16)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 
+// Workgroup b of n, renumbered so that each of the eight XCDs, to which the hardware deals workgroups in turn, gets a contiguous range.
+__device__ __forceinline__ uint32_t xcd_neighbours(uint32_t b, uint32_t n) {
+  const uint32_t each = n / 8;
+  return b < each * 8 ? b % 8 * each + b / 8 : b;
+}
+
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 

@@ -268,11 +268,12 @@ struct GradTensor {
   int64_t cols, ld, ld_out;
   int32_t rows, first_unit;
   int32_t unit_rows, unit_cols;   // of a unit of work; a row has (cols + unit_cols - 1) / unit_cols of them
-  int32_t flags, unused;          // bits: 1 data is bf16, 2 out is bf16, 4 sixteen bytes at a time
+  int32_t flags, unused;          // bits: 1 data is bf16, 2 out is bf16
 };
-enum { kGradBf16 = 1, kGradOutBf16 = 2, kGradWide = 4 };
+enum { kGradBf16 = 1, kGradOutBf16 = 2 };
 hipError_t launch_grad_sumsq(const GradTensor* tensors, const int32_t* unit_tensor, int64_t units, double* sumsq, double* partials, hipStream_t s);
-hipError_t launch_grad_clip(const GradTensor* tensors, const int32_t* unit_tensor, int64_t units, const double* sumsq, float max_norm, float* norm, hipStream_t s);
+hipError_t launch_grad_clip(const GradTensor* tensors, const int32_t* unit_tensor, int64_t units, int64_t unit_elements, const double* sumsq, float max_norm, float* norm,
+                            hipStream_t s);
 
 hipError_t run_selftest(uint64_t* mismatches_dev, hipStream_t s);
 

@@ -139,13 +139,13 @@ def test_units_of_work_cover_every_element_once(lib):
             assert len(mine) == 0
             continue
         assert out == data == grads[i].data and (r, c) in ((rows, cols), (1, rows * cols)) and (r == 1 or l == ld == lo)
-        assert bool(flags & 4) == (data % 16 == 0 and (r == 1 or ld % 4 == 0)) and first == mine[0] and (uc % 8 == 0 or uc == c)
+        assert flags == 0 and first == mine[0] and (uc % 8 == 0 or uc == c)
         across, down = -(-c // uc), -(-r // ur)
         assert list(mine) == list(range(first, first + across * down)) and ur * uc <= 1 << 24
         covered = sum(min(ur, r - (u // across) * ur) * min(uc, c - (u % across) * uc) for u in range(across * down))
         assert covered == rows * cols
         seen += len(mine)
-    assert seen == lst.units < 20000
+    assert seen == lst.units < 40000
 
 
 def test_the_binding_refuses():
