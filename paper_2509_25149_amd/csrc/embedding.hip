@@ -56,9 +56,20 @@ __global__ __launch_bounds__(256) void embedding_forward_kernel(EmbeddingForward
 
 // ---------------------------------------------------------------- tokens in order of their ids
 // A key is the id, or the number of rows for an id outside the table: those come last and belong to no row.
-__device__ __forceinline__ uint32_t key_of(const void* ids, bool i64, int64_t t, int64_t vocab) {
-  const int64_t id = id_at(ids, i64, t);
-  return static_cast<uint32_t>(id >= 0 && id < vocab ? id : vocab);
+// kN of them, `step` tokens apart, asked for together; those behind the last token are not tokens (kNoKey).
+constexpr uint32_t kNoKey = 0xFFFFFFFFu;
+template <int kN, typename Id>
+__device__ __forceinline__ void keys_of(const Id* ids, int t, int step, int n, int64_t vocab, uint32_t (&key)[kN]) {
+  Id id[kN];
+#pragma unroll
+  for (int u = 0; u < kN; ++u) id[u] = ids[min(t + u * step, n - 1)];
+#pragma unroll
+  for (int u = 0; u < kN; ++u) key[u] = t + u * step >= n ? kNoKey : id[u] >= 0 && id[u] < vocab ? static_cast<uint32_t>(id[u]) : static_cast<uint32_t>(vocab);
+}
+template <int kN>
+__device__ __forceinline__ void keys_of(const void* ids, bool i64, int t, int step, int n, int64_t vocab, uint32_t (&key)[kN]) {
+  if (i64) keys_of(static_cast<const int64_t*>(ids), t, step, n, vocab, key);
+  else keys_of(static_cast<const int32_t*>(ids), t, step, n, vocab, key);
 }
 
 // Up to kFewTokens: a token's place is the number of tokens before it, counted: two operations a pair.  A workgroup holds the keys and takes 32 tokens; a wavefront four of them, each
@@ -95,8 +106,13 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(const void* ids, boo
   constexpr int T = kRankThreads;
   __shared__ __attribute__((aligned(16))) uint32_t all[kFewTokens];
   const int fours = (n + 3) >> 2;
-#pragma unroll 8
-  for (int i = threadIdx.x; i < fours * 4; i += T) all[i] = i < n ? key_of(ids, i64, i, vocab) : 0xFFFFFFFFu;
+  for (int base = 0; base < n; base += T * 8) {
+    uint32_t k[8];
+    keys_of(ids, i64, base + static_cast<int>(threadIdx.x), T, n, vocab, k);
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (base + u * T < fours * 4) all[base + u * T + threadIdx.x] = k[u];
+  }
   __syncthreads();
   const int lane = threadIdx.x & 63, t0 = static_cast<int>(blockIdx.x) * kRankTokens + static_cast<int>(threadIdx.x >> 6) * kRankEach;
   const uint4* four = reinterpret_cast<const uint4*>(all);
@@ -139,14 +155,28 @@ struct SortPass {
   bool i64, first;
 };
 
-__device__ __forceinline__ uint32_t sort_key(const SortPass& p, int i) { return p.first ? key_of(p.ids, p.i64, i, p.vocab) : p.keys[i]; }
+// Eight keys of a thread, `step` apart; kNoKey behind the last.
+__device__ __forceinline__ void sort_keys(const SortPass& p, int i, int step, uint32_t (&key)[8]) {
+  if (p.first) {
+    keys_of(p.ids, p.i64, i, step, p.n, p.vocab, key);
+  } else {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) key[u] = p.keys[min(i + u * step, p.n - 1)];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (i + u * step >= p.n) key[u] = kNoKey;
+  }
+}
 
 __global__ __launch_bounds__(256) void sort_count_kernel(SortPass p) {
   __shared__ uint32_t count[kMostDigits];
   for (int d = threadIdx.x; d < p.digits; d += 256) count[d] = 0u;
   __syncthreads();
-  const int base = static_cast<int>(blockIdx.x) * kTile;
-  for (int i = threadIdx.x; i < kTile && base + i < p.n; i += 256) atomicAdd(&count[(sort_key(p, base + i) >> p.shift) & (p.digits - 1)], 1u);
+  uint32_t key[8];
+  sort_keys(p, static_cast<int>(blockIdx.x) * kTile + static_cast<int>(threadIdx.x), 256, key);
+#pragma unroll
+  for (int u = 0; u < 8; ++u)
+    if (key[u] != kNoKey) atomicAdd(&count[(key[u] >> p.shift) & (p.digits - 1)], 1u);
   __syncthreads();
   for (int d = threadIdx.x; d < p.digits; d += 256) p.counts[static_cast<int64_t>(d) * p.tiles + blockIdx.x] = count[d];
 }
@@ -194,12 +224,13 @@ __global__ __launch_bounds__(256) void sort_place_kernel(SortPass p) {
   for (int d = threadIdx.x; d < 4 * kMostDigits; d += 256) next[0][d] = 0u;
   __syncthreads();
   const int base = static_cast<int>(blockIdx.x) * kTile + wave * 512;
-  uint32_t key[8];
+  uint32_t key[8], order[8];
+  sort_keys(p, base + lane, 64, key);
 #pragma unroll
   for (int r = 0; r < 8; ++r) {
     const int i = base + r * 64 + lane;
-    key[r] = i < p.n ? sort_key(p, i) : 0u;
-    if (i < p.n) atomicAdd(&next[wave][(key[r] >> p.shift) & (p.digits - 1)], 1u);
+    order[r] = p.first ? static_cast<uint32_t>(i) : p.order[min(i, p.n - 1)];
+    if (key[r] != kNoKey) atomicAdd(&next[wave][(key[r] >> p.shift) & (p.digits - 1)], 1u);
   }
   __syncthreads();
   for (int d = threadIdx.x; d < p.digits; d += 256) {
@@ -215,8 +246,7 @@ __global__ __launch_bounds__(256) void sort_place_kernel(SortPass p) {
   volatile uint32_t* mine = next[wave];   // (a wavefront's own: its LDS operations are done in order)
 #pragma unroll
   for (int r = 0; r < 8; ++r) {
-    const int i = base + r * 64 + lane;
-    const bool in = i < p.n;
+    const bool in = key[r] != kNoKey;
     const uint32_t digit = (key[r] >> p.shift) & (p.digits - 1);
     uint64_t same = __ballot(in);
 #pragma unroll
@@ -235,7 +265,7 @@ __global__ __launch_bounds__(256) void sort_place_kernel(SortPass p) {
     __builtin_amdgcn_wave_barrier();
     if (in) {
       p.to_keys[to] = key[r];
-      p.to_order[to] = p.first ? static_cast<uint32_t>(i) : p.order[i];
+      p.to_order[to] = order[r];
     }
   }
 }
@@ -288,7 +318,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs s) {
   const int64_t col = static_cast<int64_t>(unit % s.strips) * 512 + lane * 8, from = min(col, a.cols - 8);
   const bool in = col < a.cols;
   const uint32_t vocab = static_cast<uint32_t>(a.vocab);
-  const uint32_t ahead = first > 0 ? s.keys[first - 1] : 0xFFFFFFFFu, behind = last < s.n ? s.keys[last] : 0xFFFFFFFFu;
+  const uint32_t ahead = first > 0 ? s.keys[first - 1] : kNoKey, behind = last < s.n ? s.keys[last] : kNoKey;
   uint32_t key = s.keys[first];
   bool begun = ahead == key;
   float sum[8] = {};
@@ -357,7 +387,7 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs s) {
   if (col >= a.cols) return;
   const float* from = s.partials + static_cast<int64_t>(chunk) * 2 * a.cols + col;
   float4v sum = *reinterpret_cast<const float4v*>(from + a.cols);
-#pragma unroll 8
+#pragma unroll 16
   for (int c = 1; c <= final_chunk - chunk; ++c) sum += *reinterpret_cast<const float4v*>(from + static_cast<int64_t>(c) * 2 * a.cols);
   float4v* to = reinterpret_cast<float4v*>(a.dtable + static_cast<int64_t>(key) * a.ldt + col);
   sum = a.scale * sum;

@@ -175,8 +175,8 @@ struct TopShared {
   float group[kMostThreads / 64][64];
   uint64_t best[kMostThreads / 64];
   uint64_t found[kCandidates];
-  uint16_t threads[kMostThreads];
-  uint32_t bound, n_threads, n_found;
+  uint8_t lanes[kMostThreads / 64][64];
+  uint32_t n_found;
 };
 
 // Eight values of a group, those past the end of the row at -infinity.
@@ -210,41 +210,51 @@ __device__ __forceinline__ uint64_t best_of_share(const void* row, int g0, int g
 
 // The k best of groups [g0, g1) to emit(rank, place).  `own`: the largest value that this thread has seen in sum_of_groups.
 // The k-th largest of 64 maxima over disjoint columns bounds the k-th best from below; only threads whose maximum reaches it hold candidates, some
-// k of them, and their columns are read once more by the whole workgroup.  Candidates take their rank by counting the better ones.
+// k of them, and their wavefront reads their columns once more.  Candidates take their rank by counting the better ones.
 // Where fewer than k values are above -infinity the first columns at -infinity follow.
 // Where too many reach the bound (rows that are equal nearly everywhere) each thread keeps the best of its share, and the best of those is taken k times over.
 template <bool kBf16, typename Emit>
 __device__ __forceinline__ void take_best(const void* row, int g0, int g1, int cols, float own, int k, TopShared& s, Emit emit) {
   const int t = threadIdx.x, T = blockDim.x, waves = T >> 6;
-  s.group[t >> 6][t & 63] = own;
-  if (t == 0) s.n_threads = s.n_found = 0u;
+  const int wave = t >> 6, lane = t & 63;
+  s.group[wave][lane] = own;
+  if (t == 0) s.n_found = 0u;
   __syncthreads();
-  if (t < 64) {
-    float m = s.group[0][t];
-    for (int w = 1; w < waves; ++w) m = __builtin_fmaxf(m, s.group[w][t]);
-    int better = 0;
-#pragma unroll 8
-    for (int i = 0; i < 64; ++i) {
-      const float o = __shfl(m, i, 64);
-      better += o > m || (o == m && i < t);
-    }
-    if (better == k - 1) s.bound = order_of(m);   // (kLowest, above -infinity, for groups of nothing else)
-  }
-  __syncthreads();
-  const uint32_t bound = s.bound;
-  if (order_of(own) >= bound) s.threads[atomicAdd(&s.n_threads, 1u)] = static_cast<uint16_t>(t);
-  __syncthreads();
-  const int turns = (g1 - g0 + T - 1) / T, items = static_cast<int>(s.n_threads) * turns;
-  for (int i = t; i < items; i += T) {
-    const int g = g0 + s.threads[i / turns] + i % turns * T;
-    if (g >= g1) continue;
-    float v[8];
-    group_of<kBf16>(row, g, cols, v);
+  float m = s.group[0][lane];   // (kLowest, above -infinity, for groups of nothing else)
+  for (int w = 1; w < waves; ++w) m = __builtin_fmaxf(m, s.group[w][lane]);
+  int better = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (g * 8 + j < cols && order_of(v[j]) >= bound) {
-        const uint32_t at = atomicAdd(&s.n_found, 1u);
-        if (at < kCandidates) s.found[at] = place(v[j], g * 8 + j);
+  for (int i = 0; i < 64; ++i) better += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(m), i)) > m;
+  uint32_t bound = better < k ? order_of(m) : ~0u;
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) bound = min(bound, static_cast<uint32_t>(__shfl_xor(bound, off, 64)));
+  const bool holds = order_of(own) >= bound;
+  const uint64_t holders = __ballot(holds);
+  if (holds) s.lanes[wave][__popcll(holders & ((uint64_t{1} << lane) - 1))] = static_cast<uint8_t>(lane);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const int turns = (g1 - g0 + T - 1) / T, items = __popcll(holders) * turns;
+  for (int i0 = lane; i0 < items; i0 += 4 * 64) {   // four groups of eight columns asked for together
+    Eight<kBf16> x[4];
+    int g[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + u * 64;
+      g[u] = i < items ? g0 + wave * 64 + s.lanes[wave][i / turns] + i % turns * T : g1;
+      if (g[u] < min(g1, cols >> 3)) x[u].load(row, static_cast<int64_t>(g[u]) * 8);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (g[u] >= g1) continue;
+      float v[8];
+      if (g[u] < cols >> 3) x[u].get(v);
+      else rest_of_row<kBf16>(row, g[u], cols, v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (g[u] * 8 + j < cols && order_of(v[j]) >= bound) {
+          const uint32_t at = atomicAdd(&s.n_found, 1u);
+          if (at < kCandidates) s.found[at] = place(v[j], g[u] * 8 + j);
+        }
       }
     }
   }
@@ -350,35 +360,40 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobForward a) {
     const float4v v = *reinterpret_cast<const float4v*>(a.partial + (row * parts + (t & 63)) * 4);
     mine = Sum{v[0], v[1], v[2]};
   }
-  const Sum all = wave_join<kEntropy>(mine, c);
-  const RowStats r(all);
-  if (t == 0) write_row(a, row, all, r, at_target, counted);
   if constexpr (kTop) {
     __shared__ uint64_t best[kMostParts * kMostTop], found[kMostParts * kMostTop];
-    __shared__ uint64_t bound;
     __shared__ int n_found;
-    const int n = parts * k;
+    const int n = parts * k, lane = t & 63;
+#pragma unroll 4
     for (int i = t; i < n; i += 256) best[i] = a.best[row * n + i];
-    if (t == 0) bound = 0ull, n_found = 0;
+    if (t == 0) n_found = 0;
+    const Sum all = wave_join<kEntropy>(mine, c);
+    const RowStats r(all);
+    if (t == 0) write_row(a, row, all, r, at_target, counted);
     __syncthreads();
-    if (t < parts) {   // with j = ceil(k / parts), the ceil(k / j)-th largest of the pieces' j-th: so many pieces have j each that reach it
-      const int j = (k + parts - 1) / parts, at = (k + j - 1) / j - 1;
-      const uint64_t mine = best[t * k + j - 1];
-      int better = 0;
-      for (int i = 0; i < parts; ++i) better += best[i * k + j - 1] > mine || (best[i * k + j - 1] == mine && i < t);
-      if (better == at) bound = mine;
-    }
-    __syncthreads();
+    // With j = ceil(k / parts), the ceil(k / j)-th largest of the pieces' j-th bounds the k-th best: so many pieces have j each that reach it.
+    const int j = (k + parts - 1) / parts, enough = (k + j - 1) / j;
+    const uint64_t jth = lane < parts ? best[lane * k + j - 1] : 0ull;
+    int better = 0;
+#pragma unroll 8
+    for (int i = 0; i < parts; ++i) better += best[i * k + j - 1] > jth;
+    const uint64_t in = __ballot(lane < parts && better < enough);
+    uint64_t bound = in >> lane & 1 ? jth : ~0ull;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) bound = min(bound, static_cast<uint64_t>(__shfl_xor(static_cast<unsigned long long>(bound), off, 64)));
     for (int i = t; i < n; i += 256)
       if (best[i] >= bound && best[i] != 0ull) found[atomicAdd(&n_found, 1)] = best[i];
     __syncthreads();
     for (int i = t; i < n_found; i += 256) {
       const uint64_t p = found[i];
-      int better = 0;
+      int ahead = 0;
 #pragma unroll 8
-      for (int j = 0; j < n_found; ++j) better += found[j] > p;
-      if (better < k) write_alternative(a, row, better, p, r);
+      for (int o = 0; o < n_found; ++o) ahead += found[o] > p;
+      if (ahead < k) write_alternative(a, row, ahead, p, r);
     }
+  } else {
+    const Sum all = wave_join<kEntropy>(mine, c);
+    if (t == 0) write_row(a, row, all, RowStats(all), at_target, counted);
   }
 }
 
@@ -413,9 +428,11 @@ struct RowGradient {
   }
 };
 
-// store8, for what no cache should keep.
-__device__ __forceinline__ void stream8(void* row, int64_t col, bool bf16, const float (&v)[8]) {
-  if (bf16) {
+template <bool kStream>
+__device__ __forceinline__ void put8(void* row, int64_t col, bool bf16, const float (&v)[8]) {
+  if (!kStream) {
+    store8(row, col, bf16, v);
+  } else if (bf16) {
     const uint32x4 w = {f32x2_to_bf16(v[0], v[1]), f32x2_to_bf16(v[2], v[3]), f32x2_to_bf16(v[4], v[5]), f32x2_to_bf16(v[6], v[7])};
     __builtin_nontemporal_store(w, reinterpret_cast<uint32x4*>(static_cast<uint16_t*>(row) + col));
   } else {
@@ -425,8 +442,6 @@ __device__ __forceinline__ void stream8(void* row, int64_t col, bool bf16, const
   }
 }
 
-#define put8 store8
-#define put8k store8
 template <bool kInBf16, bool kOutBf16, bool kEntropy>
 __device__ __forceinline__ void gradient_of_rest(const void* z, void* dz, int g, int cols, const RowGradient& r, float c) {
   float v[8];
@@ -443,7 +458,8 @@ __device__ __forceinline__ void gradient_of_rest(const void* z, void* dz, int g,
 }
 
 // Groups [g0, g1) of a row by the workgroup's threads, from the end to the front.
-template <bool kInBf16, bool kOutBf16, bool kEntropy>
+// kStream: results that no cache should keep.
+template <bool kInBf16, bool kOutBf16, bool kEntropy, bool kStream>
 __device__ __forceinline__ void gradient_of_groups(const void* z, void* dz, int g0, int g1, int cols, const RowGradient& r, float c) {
   const int step = blockDim.x, whole = min(g1, cols >> 3);
   if (whole < g1 && threadIdx.x == 0) gradient_of_rest<kInBf16, kOutBf16, kEntropy>(z, dz, whole, cols, r, c);
@@ -457,7 +473,7 @@ __device__ __forceinline__ void gradient_of_groups(const void* z, void* dz, int 
       float v[8];
       x[u].get(v);
       r.of<kEntropy>(v, g - u * step, c);
-      put8(dz, static_cast<int64_t>(g - u * step) * 8, kOutBf16, v);
+      put8<kStream>(dz, static_cast<int64_t>(g - u * step) * 8, kOutBf16, v);
     }
   }
   for (; g >= g0; g -= step) {
@@ -466,7 +482,7 @@ __device__ __forceinline__ void gradient_of_groups(const void* z, void* dz, int 
     x.load(z, static_cast<int64_t>(g) * 8);
     x.get(v);
     r.of<kEntropy>(v, g, c);
-    put8(dz, static_cast<int64_t>(g) * 8, kOutBf16, v);
+    put8<kStream>(dz, static_cast<int64_t>(g) * 8, kOutBf16, v);
   }
 }
 
@@ -479,7 +495,7 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobBackward a
   const int g0 = min(part * each, groups), g1 = min(g0 + each, groups);
   const RowGradient r(a.stats[2 * row], a.stats[2 * row + 1], a.scale, a.g_logprob ? a.g_logprob[row] : 0.0f, a.g_lse ? a.g_lse[row] : 0.0f,
                       kEntropy ? a.g_entropy[row] : 0.0f, kEntropy ? a.entropy[row] : 0.0f, a.targets ? index_at(a.targets, a.i64, row) : -1, cols);
-  gradient_of_groups<kInBf16, kOutBf16, kEntropy>(static_cast<const char*>(a.z) + row * a.ld * (kInBf16 ? 2 : 4),
+  gradient_of_groups<kInBf16, kOutBf16, kEntropy, false>(static_cast<const char*>(a.z) + row * a.ld * (kInBf16 ? 2 : 4),
                                                   static_cast<char*>(a.dz) + row * a.ldd * (kOutBf16 ? 2 : 4), g0, g1, cols, r, a.scale * kLog2E);
 }
 
@@ -500,7 +516,7 @@ __device__ __forceinline__ void add_groups(Sum& a, const Eight<kBf16> (&x)[kN], 
   add<false>(a, v, c);
 }
 
-template <int T, bool kInBf16, bool kOutBf16>
+template <int T, bool kInBf16, bool kOutBf16, bool kStream>
 __global__ __launch_bounds__(T, 8) void logprob_loss_kernel(LogprobForward f, LogprobBackward b) {
   constexpr int kRegisters = kInBf16 ? kKeepRegisters : kKeepRegisters / 2, kLds = kInBf16 ? kKeepLds : kKeepLds / 2;
   __shared__ Sum sums[T / 64];
@@ -545,7 +561,7 @@ __global__ __launch_bounds__(T, 8) void logprob_loss_kernel(LogprobForward f, Lo
     float v[8];
     x.get(v);
     d.of<false>(v, group, c);
-    put8k(dz, static_cast<int64_t>(group) * 8, kOutBf16, v);
+    put8<kStream>(dz, static_cast<int64_t>(group) * 8, kOutBf16, v);
   };
   if ((cols & 7) && t == T - 1) gradient_of_rest<kInBf16, kOutBf16, false>(z, dz, whole, cols, d, c);
 #pragma unroll
@@ -554,7 +570,7 @@ __global__ __launch_bounds__(T, 8) void logprob_loss_kernel(LogprobForward f, Lo
 #pragma unroll
   for (int u = kLds - 1; u >= 0; --u)
     if (first + u * T < whole) store(kept[u * T + t], first + u * T);
-  gradient_of_groups<kInBf16, kOutBf16, false>(z, dz, 0, again, again * 8, d, c);
+  gradient_of_groups<kInBf16, kOutBf16, false, kStream>(z, dz, 0, again, again * 8, d, c);
 }
 
 // ---------------------------------------------------------------- launches
@@ -567,13 +583,13 @@ constexpr int64_t kCUs = 256;
 struct ForwardShape {
   int parts, threads;
 };
-ForwardShape forward_shape(int64_t rows, int64_t cols) {
+// A row to a workgroup, but for few long rows, which are cut into pieces (us on the GPU without / with pieces: 1 x 131072 11.5 / 5.6, 64 x 131072 12 / 9, 100 x 131072 12 / 11, 1 to 100 x 50257
+// 6.9 / 5.8 to 8.7, where the second launch costs the host 3 more).  Threads by the bytes of a row; the best alternatives are looked for by 256 at least.
+ForwardShape forward_shape(int64_t rows, int64_t cols, bool bf16, bool top) {
   const int64_t groups = (cols + 7) / 8;
-  if (rows < 2 * kCUs && groups > 512) {
-    const int64_t parts = std::min<int64_t>({kMostParts, 4 * kCUs / std::max<int64_t>(rows, 1), groups / 256});
-    if (parts > 1) return {static_cast<int>(parts), 256};
-  }
-  return {1, groups >= 2048 ? 512 : groups >= 512 ? 256 : 64};
+  if (rows < 96 && groups >= 8192) return {static_cast<int>(std::min<int64_t>(kMostParts, 4 * kCUs / std::max<int64_t>(rows, 1))), 256};
+  const int64_t bytes = cols * (bf16 ? 2 : 4);
+  return {1, bytes <= (top ? 2 << 10 : 16 << 10) ? 64 : bytes <= 64 << 10 || (rows >= kCUs && rows < 8 * kCUs) ? 256 : 512};
 }
 
 template <bool... kFlags>
@@ -624,13 +640,13 @@ int loss_threads(int64_t rows, int64_t cols, bool bf16) {
   return bytes <= 8 << 10 ? 64 : bytes <= 36 << 10 ? 256 : bytes <= (rows >= 8 * kCUs ? 72 << 10 : 160 << 10) ? 512 : 1024;
 }
 
-template <int T>
+template <int T, bool kStream>
 hipError_t loss_of(const LogprobForward& f, const LogprobBackward& b, hipStream_t s) {
   const int64_t most = rows_at_once(T);
   LogprobForward p = f;
   for (p.row0 = 0; p.row0 < f.rows; p.row0 += most) {
     const unsigned rows = static_cast<unsigned>(std::min(most, f.rows - p.row0));
-#define NVFP4_LOSS(I, O) hipLaunchKernelGGL((logprob_loss_kernel<T, I, O>), dim3(rows), dim3(T), 0, s, p, b)
+#define NVFP4_LOSS(I, O) hipLaunchKernelGGL((logprob_loss_kernel<T, I, O, kStream>), dim3(rows), dim3(T), 0, s, p, b)
     if (f.bf16) {
       if (b.out_bf16) NVFP4_LOSS(true, true); else NVFP4_LOSS(true, false);
     } else {
@@ -646,13 +662,13 @@ hipError_t loss_of(const LogprobForward& f, const LogprobBackward& b, hipStream_
 }  // namespace
 
 size_t logprob_workspace_bytes(int64_t rows, int64_t cols, int top) {
-  const int parts = forward_shape(rows, cols).parts;
+  const int parts = forward_shape(rows, cols, true, false).parts;
   return parts == 1 ? 0 : static_cast<size_t>(rows) * static_cast<size_t>(parts) * (16 + 8 * static_cast<size_t>(top));
 }
 
 hipError_t launch_logprob_forward(const LogprobForward& all, void* workspace, hipStream_t s) {
   LogprobForward a = all;
-  const ForwardShape shape = forward_shape(a.rows, a.cols);
+  const ForwardShape shape = forward_shape(a.rows, a.cols, a.bf16, a.top > 0);
   a.parts = shape.parts;
   a.partial = static_cast<float*>(workspace);
   a.best = reinterpret_cast<uint64_t*>(a.partial + (a.parts > 1 ? a.rows * a.parts * 4 : 0));
@@ -669,9 +685,12 @@ hipError_t launch_logprob_backward(const LogprobBackward& all, hipStream_t s) {
 }
 
 hipError_t launch_logprob_with_gradient(const LogprobForward& f, const LogprobBackward& b, void* workspace, hipStream_t s) {
-  if (forward_shape(f.rows, f.cols).parts == 1) {
+  if (forward_shape(f.rows, f.cols, f.bf16, false).parts == 1) {
     const int threads = loss_threads(f.rows, f.cols, f.bf16);
-    return threads == 64 ? loss_of<64>(f, b, s) : threads == 256 ? loss_of<256>(f, b, s) : threads == 512 ? loss_of<512>(f, b, s) : loss_of<1024>(f, b, s);
+    return threads == 64    ? loss_of<64, false>(f, b, s)
+           : threads == 256 ? loss_of<256, false>(f, b, s)
+           : threads == 512 ? (f.bf16 ? loss_of<512, true>(f, b, s) : loss_of<512, false>(f, b, s))
+                            : (f.bf16 ? loss_of<1024, true>(f, b, s) : loss_of<1024, false>(f, b, s));
   }
   const hipError_t e = launch_logprob_forward(f, workspace, s);
   return e == hipSuccess ? launch_logprob_backward(b, s) : e;
