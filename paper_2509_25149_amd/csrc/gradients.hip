@@ -152,7 +152,7 @@ __global__ __launch_bounds__(1024) void grad_fold_kernel(const double* __restric
 template <bool kBf16, bool kOutBf16>
 __device__ __forceinline__ void scaled(const Unit& n, uint32_t t, uint32_t step, float by) {
   constexpr int kN = kBf16 && kOutBf16 ? 8 : 4, kSize = kBf16 ? 2 : 4, kOutSize = kOutBf16 ? 2 : 4;
-  for_unit<kN, 1>(
+  for_unit<kN, 4>(
       n, t, step,
       [&](int row, int col) {
         float v[kN];
@@ -168,8 +168,10 @@ __device__ __forceinline__ void scaled(const Unit& n, uint32_t t, uint32_t step,
 }
 
 // The factor from the sum of squares, in every workgroup.  1 for a norm that is not finite, and then, as for any factor of 1, what stays in its place is not touched.
-// `splits` workgroups to a unit, 16 bytes to a thread: waves that load once and store once, neighbours on one XCD (2.7 GB copied so at 6.3 TB/s; four pieces to a
-// thread 5.7, in a loop of four times four 5.4).
+// `splits` workgroups to a unit, so that each has 4096 elements: short waves, neighbours on one XCD.  (A plain copy of 2.7 GB is fastest with 16 bytes to a thread, 6.3 TB/s against 5.7 with
+// four times that and 5.4 in a loop; but here three loads in turn lead to the data.  us for norm and clipping of 210 million FP32 values / 30 million bf16 with 1024, 2048, 4096, 8192 elements
+// to a workgroup: 474 / 51, 437 / 36, 444 / 31, 461 / 31.)
+constexpr int64_t kClipElements = 4096;
 __global__ __launch_bounds__(256) void grad_clip_kernel(const GradTensor* __restrict__ tensors, const int32_t* __restrict__ unit_tensor, int64_t units, uint32_t splits,
                                                         const double* __restrict__ sumsq, float max_norm, float* __restrict__ norm) {
   const double total = __builtin_sqrt(*sumsq);
@@ -201,7 +203,7 @@ hipError_t launch_grad_sumsq(const GradTensor* tensors, const int32_t* unit_tens
 
 hipError_t launch_grad_clip(const GradTensor* tensors, const int32_t* unit_tensor, int64_t units, int64_t unit_elements, const double* sumsq, float max_norm,
                             float* norm, hipStream_t s) {
-  const int64_t most = std::max<int64_t>(1, (1 << 24) / std::max<int64_t>(units, 1) - 1), splits = std::min((unit_elements + 1023) / 1024, most);   // (a launch holds 2^32 threads)
+  const int64_t most = std::max<int64_t>(1, (1 << 24) / std::max<int64_t>(units, 1) - 1), splits = std::min((unit_elements + kClipElements - 1) / kClipElements, most);   // (a launch holds 2^32 threads)
   hipLaunchKernelGGL(grad_clip_kernel, dim3(static_cast<unsigned>(std::max<int64_t>(units * splits, 1))), dim3(256), 0, s, tensors, unit_tensor, units,
                      static_cast<uint32_t>(splits), sumsq, max_norm, norm);
   return hipGetLastError();
