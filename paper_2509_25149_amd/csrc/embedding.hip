@@ -394,9 +394,107 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs s) {
   *to = a.accumulate ? *to + sum : sum;
 }
 
+// ---------------------------------------------------------------- few tokens
+// Up to kCountedTokens there is no sorting and, but for a large table's zeros, one launch: a workgroup takes a token and 2048 columns, compares all ids with the token's, and goes on if it is
+// the first one of its id: the others' places are bits in order, and a wavefront adds their rows over its 512 columns.  Tokens that are all the same are added by a few
+// wavefronts one after the other, which is why this ends at 256 of them.  (Ids by Zipf's law, us so / sorted, called from Python: 16 tokens, 700 rows of 256 8.7 / 15.6, 3000 of 5120
+// 14.8 / 17.2; 128 tokens 9.4 / 16.0 and 18 / 18; 512 tokens 17 / 15 and 27 / 20.)
+// The rest of the workgroups, if any, look for rows without a token, 64 each, and write zeros there.
+constexpr int kCountedTokens = 256, kCountedZeroRows = 64;
+
+template <bool kBf16, int kN>
+__device__ __forceinline__ void add_listed(const EmbeddingBackward& a, const uint16_t* list, int n, int64_t col, float (&sum)[8]) {
+  for (int i = 0; i < n; i += kN) {
+    Eight<kBf16> x[kN];
+#pragma unroll
+    for (int u = 0; u < kN; ++u)   // (behind the last one the last once more)
+      x[u].load(static_cast<const char*>(a.dout) + static_cast<int64_t>(list[min(i + u, n - 1)]) * a.ldd * (kBf16 ? 2 : 4), col);
+#pragma unroll
+    for (int u = 0; u < kN; ++u) {
+      if (i + u >= n) break;
+      float v[8];
+      x[u].get(v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] += v[j];
+    }
+  }
+}
+
+template <bool kBf16>
+__global__ __launch_bounds__(256) void embedding_few_kernel(EmbeddingBackward a, int n, uint32_t across, uint32_t zero_groups) {
+  __shared__ uint64_t same[kCountedTokens / 64];
+  __shared__ uint16_t list[kCountedTokens];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t sums = static_cast<uint32_t>(n) * across;
+  uint32_t key[1] = {kNoKey};
+  if (n > 0) keys_of(a.ids, a.i64, static_cast<int>(threadIdx.x), 1, n, a.vocab, key);
+  if (blockIdx.x >= sums) {
+    uint32_t* present = reinterpret_cast<uint32_t*>(same);
+    for (int64_t row0 = static_cast<int64_t>(blockIdx.x - sums) * kCountedZeroRows; row0 < a.vocab; row0 += static_cast<int64_t>(zero_groups) * kCountedZeroRows) {
+      __syncthreads();
+      if (threadIdx.x < 2) present[threadIdx.x] = 0u;
+      __syncthreads();
+      const uint32_t r = key[0] - static_cast<uint32_t>(row0);
+      if (r < kCountedZeroRows) atomicOr(&present[r >> 5], 1u << (r & 31));
+      __syncthreads();
+      const int64_t left = a.vocab - row0;
+      const uint64_t there = left < 64 ? (uint64_t{1} << left) - 1 : ~uint64_t{0};
+      for (uint64_t absent = there & ~(static_cast<uint64_t>(present[1]) << 32 | present[0]); absent; absent &= absent - 1) {
+        float* to = a.dtable + (row0 + __builtin_ctzll(absent)) * a.ldt;
+        for (int64_t col = threadIdx.x * 4; col < a.cols; col += 1024) *reinterpret_cast<float4v*>(to + col) = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+      }
+    }
+    return;
+  }
+  const int t = static_cast<int>(blockIdx.x / across);
+  uint32_t mine[1];
+  keys_of(a.ids, a.i64, t, 1, n, a.vocab, mine);
+  if (mine[0] >= static_cast<uint32_t>(a.vocab)) return;
+  const uint64_t mask = __ballot(key[0] == mine[0]);
+  if (lane == 0) same[wave] = mask;
+  __syncthreads();
+  uint64_t m = lane < kCountedTokens / 64 ? same[lane] : 0ull;
+  const int word = t >> 6;
+  if (__ballot(lane < word ? m != 0 : lane == word && (m & ((uint64_t{1} << (t & 63)) - 1)) != 0)) return;   // not the first one
+  int before = __popcll(m), total;
+#pragma unroll
+  for (int off = 1; off < kCountedTokens / 64; off <<= 1) {
+    const int o = __shfl_up(before, off, 64);
+    if (lane >= off) before += o;
+  }
+  total = __builtin_amdgcn_readlane(before, kCountedTokens / 64 - 1);
+  before -= __popcll(m);
+  const int64_t col = static_cast<int64_t>(blockIdx.x % across) * 2048 + threadIdx.x * 8, from = min(col, a.cols - 8);
+  float sum[8] = {};
+  if (total == 1) {
+    Eight<kBf16> x;
+    x.load(static_cast<const char*>(a.dout) + static_cast<int64_t>(t) * a.ldd * (kBf16 ? 2 : 4), from);
+    x.get(sum);
+  } else {
+    if (wave == 0)
+      for (; m; m &= m - 1) list[before++] = static_cast<uint16_t>(lane * 64 + __builtin_ctzll(m));
+    __syncthreads();
+    if (total <= 8) add_listed<kBf16, 8>(a, list, total, from, sum);
+    else add_listed<kBf16, 16>(a, list, total, from, sum);
+  }
+  if (col >= a.cols) return;
+  float* row = a.dtable + static_cast<int64_t>(mine[0]) * a.ldt;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sum[i] *= a.scale;
+  if (a.accumulate) {
+    Eight<false> old;
+    float o[8];
+    old.load(row, col);
+    old.get(o);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] += o[i];
+  }
+  store8(row, col, false, sum);
+}
+
 // ---------------------------------------------------------------- launches
 
-constexpr int64_t kFewTokensPerRow = 4;
+constexpr int64_t kFewTokensPerRow = 4, kZeroFirstBytes = 8 << 20;
 
 struct SumPlan {
   int chunk, chunks, tiles, passes, digit_bits;
@@ -430,7 +528,7 @@ SumPlan plan(int64_t n, int64_t vocab, int64_t cols) {
 
 }  // namespace
 
-size_t embedding_workspace_bytes(int64_t tokens, int64_t vocab, int64_t cols) { return tokens ? plan(tokens, vocab, cols).bytes : 0; }
+size_t embedding_workspace_bytes(int64_t tokens, int64_t vocab, int64_t cols) { return tokens > kCountedTokens ? plan(tokens, vocab, cols).bytes : 0; }
 
 hipError_t launch_embedding_forward(const EmbeddingForward& all, hipStream_t s) {
   EmbeddingForward a = all;
@@ -453,21 +551,25 @@ hipError_t launch_embedding_forward(const EmbeddingForward& all, hipStream_t s) 
 
 hipError_t launch_embedding_backward(const EmbeddingBackward& a, void* workspace, hipStream_t s) {
   const int n = static_cast<int>(a.tokens);
-  // Rows without a token: where tokens are few for the table all rows are written first, without looking, beside the ranking of the tokens; otherwise those that have none
-  // are looked for beside the sums.
-  const bool zero_first = !a.accumulate && a.tokens < a.vocab / kFewTokensPerRow;
+  // Rows without a token: where tokens are few for the table all rows are written first, without looking; otherwise those that have none are looked for beside the sums.
+  const bool few = n <= kCountedTokens, zero_first = !a.accumulate && (few ? a.vocab * a.cols * 4 > kZeroFirstBytes : a.tokens < a.vocab / kFewTokensPerRow);
   ZeroArgs z{};
   if (zero_first) {
     z.to = a.dtable, z.ld = a.ldt, z.across = static_cast<uint32_t>(a.cols / 4), z.pieces = a.vocab * z.across;
     z.groups = static_cast<uint32_t>(std::min<int64_t>((z.pieces + kRankThreads - 1) / kRankThreads, 1 << 22));   // (a launch holds 2^32 threads)
   }
   hipError_t e;
-  if (n > kFewTokens || n == 0) {
-    if (zero_first) {
-      hipLaunchKernelGGL(zero_kernel, dim3(z.groups), dim3(kRankThreads), 0, s, z);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    if (n == 0) return hipSuccess;
+  if (zero_first && (few || n > kFewTokens)) {   // (otherwise in one launch with the ranking)
+    hipLaunchKernelGGL(zero_kernel, dim3(z.groups), dim3(kRankThreads), 0, s, z);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (few) {
+    const uint32_t across = static_cast<uint32_t>((a.cols + 2047) / 2048);
+    const uint32_t zeros = a.accumulate || zero_first ? 0u : static_cast<uint32_t>(std::min<int64_t>((a.vocab + kCountedZeroRows - 1) / kCountedZeroRows, 1 << 16));
+    if (n * across + zeros == 0) return hipSuccess;
+    if (a.bf16) hipLaunchKernelGGL(embedding_few_kernel<true>, dim3(n * across + zeros), dim3(256), 0, s, a, n, across, zeros);
+    else hipLaunchKernelGGL(embedding_few_kernel<false>, dim3(n * across + zeros), dim3(256), 0, s, a, n, across, zeros);
+    return hipGetLastError();
   }
   const SumPlan p = plan(n, a.vocab, a.cols);
   uint32_t* words = static_cast<uint32_t*>(workspace);

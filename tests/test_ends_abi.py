@@ -41,16 +41,16 @@ def test_embedding_refuses(lib):
     assert fwd(n=-1) == -2 and fwd(n=1 << 30) == -2 and fwd(vocab=0) == -2 and fwd(vocab=(1 << 31) - 1) == -2 and fwd(cols=24) == -2 and fwd(cols=0) == -2
     assert fwd(cols=32784, ldt=32784, ldo=32784) == -2 and fwd(ldt=56) == -2 and fwd(ldt=68) == -2 and fwd(ldo=60) == -2
 
-    def bwd(dout=P, dt=1, ldd=64, ids=P, it=1, n=32, vocab=100, cols=64, scale=1.0, dtable=P, ldt=64, acc=0, ws=P, size=1 << 24):
+    def bwd(dout=P, dt=1, ldd=64, ids=P, it=1, n=2000, vocab=100, cols=64, scale=1.0, dtable=P, ldt=64, acc=0, ws=P, size=1 << 24):
         return lib.nvfp4_embedding_backward(dout, dt, ldd, ids, it, n, vocab, cols, scale, dtable, ldt, acc, ws, size, None)
     assert bwd(dout=None) == -1 and bwd(dout=P + 8) == -1 and bwd(dt=2) == -1 and bwd(ids=None) == -1 and bwd(ids=P + 4) == -1 and bwd(it=5) == -1
     assert bwd(dtable=None) == -1 and bwd(dtable=P + 4) == -1 and bwd(scale=float("nan")) == -1
     assert bwd(n=-1) == -2 and bwd(vocab=-1) == -2 and bwd(cols=40) == -2 and bwd(ldd=56) == -2 and bwd(ldt=63) == -2
-    need = nv.embedding_workspace_bytes(32, 100, 64)
+    need = nv.embedding_workspace_bytes(2000, 100, 64)
     assert bwd(ws=None) == -6 and bwd(size=need - 1) == -6 and bwd(ws=P + 8) == -6
     w = ctypes.c_size_t()
     assert lib.nvfp4_embedding_workspace_bytes(32, 100, 24, ctypes.addressof(w)) == -2 and lib.nvfp4_embedding_workspace_bytes(32, 100, 64, None) == -1
-    assert nv.embedding_workspace_bytes(0, 100, 64) == 0
+    assert nv.embedding_workspace_bytes(0, 100, 64) == 0 and nv.embedding_workspace_bytes(256, 100, 64) == 0 and nv.embedding_workspace_bytes(257, 100, 64) >= 2 * 257 * 4
 
 
 def test_logprob_refuses(lib):

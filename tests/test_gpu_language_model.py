@@ -85,7 +85,7 @@ class Clip:
 
 
 # (small, larger): calls with scratch memory, the second needing more of it
-CASES = {"embedding": (lambda s: Embedding(1040, 700, 272, s), lambda s: Embedding(9000, 3000, 528, s)), "logprob": (lambda s: LogProb(3, 70000, s), lambda s: LogProb(90, 131072, s)),
+CASES = {"embedding": (lambda s: Embedding(1240, 700, 272, s), lambda s: Embedding(9000, 3000, 528, s)), "logprob": (lambda s: LogProb(3, 70000, s), lambda s: LogProb(90, 131072, s)),
          "clip": (lambda s: Clip([5000, 70000, 3], s), lambda s: Clip([1 << 20] * 8, s))}
 
 
@@ -170,7 +170,7 @@ def test_the_binding_refuses_what_does_not_fit():
                  lambda: nv.nvfp4_embedding_forward(t, table, out=torch.zeros(4, 48, device="cuda")), lambda: nv.nvfp4_embedding_forward(t, table, scale=math.inf),
                  lambda: nv.nvfp4_embedding_backward(table[:4], t), lambda: nv.nvfp4_embedding_backward(table[:4], t, accumulate=True, vocab=10),
                  lambda: nv.nvfp4_embedding_backward(table[:4], t, dtable=table.bfloat16()), lambda: nv.nvfp4_embedding_backward(table[:5], t, 10),
-                 lambda: nv.nvfp4_embedding_backward(table[:4], t, 10, workspace=torch.empty(16, dtype=torch.uint8, device="cuda")),
+                 lambda: nv.nvfp4_embedding_backward(table[:1].expand(2000, 32).contiguous(), t.repeat(500), 10, workspace=torch.empty(16, dtype=torch.uint8, device="cuda")),
                  lambda: nv.nvfp4_grad_clip(nv.Gradients([f]), f, 1.0), lambda: nv.nvfp4_grad_clip(nv.Gradients([f]), torch.zeros(1, dtype=torch.float64, device="cuda"), -1.0),
                  lambda: nv.nvfp4_grad_sumsq(nv.Gradients([f]), out=f[:1])):
         with pytest.raises((ValueError, nv.NVFP4Error)):
