@@ -685,7 +685,7 @@ def _here(*tensors) -> None:
     device = _current_device()
     for t in tensors:
         if t is not None and t.get_device() != device:
-            raise ValueError(f"a tensor on {t.device}, with device {device} current")
+            raise ValueError(f"a tensor on {t.device}, with CUDA device {device} current")
 
 
 def _indices(t: torch.Tensor, n: Optional[int], what: str):
@@ -774,16 +774,24 @@ def nvfp4_logprob_forward(logits: torch.Tensor, targets: Optional[torch.Tensor] 
     _here(logits, targets)
     dt, zp, ld = _matrix(logits, "logits")
     (rows, cols), device = logits.shape, logits.device
-    if ld % 8 and rows == 1:
+    if ld % 8 and rows <= 1:
         ld = -(-cols // 8) * 8      # (a row alone may be of any length)
     kind, tp = (INDEX_I64, None) if targets is None else _indices(targets, rows, "targets")
     ws, ws_bytes, workspace = _scratch(workspace, logprob_workspace_bytes(rows, cols, top), device)
-    f32 = lambda *size: torch.empty(*size, dtype=torch.float32, device=device)
-    r = LogProbs(None if targets is None else f32(rows), f32(rows), f32(rows, 2), f32(rows) if entropy else None,
-                 torch.empty(rows, top, dtype=torch.int32, device=device) if top else None, f32(rows, top) if top else None)
-    _check(load_library().nvfp4_logprob_forward(zp, dt, ld, rows, cols, scale, tp, kind, *[None if t is None else t.data_ptr() for t in (r.logprob, r.stats, r.lse, r.entropy)],
-                                                top, *[None if t is None else t.data_ptr() for t in (r.top_index, r.top_logprob)], ws, ws_bytes, _stream()))
-    return r
+    f32, lp, hp, ip, vp = torch.float32, None, None, None, None
+    logprob = h = index = values = None
+    if targets is not None:
+        logprob = torch.empty(rows, dtype=f32, device=device)
+        lp = logprob.data_ptr()
+    lse, stats = torch.empty(rows, dtype=f32, device=device), torch.empty(rows, 2, dtype=f32, device=device)
+    if entropy:
+        h = torch.empty(rows, dtype=f32, device=device)
+        hp = h.data_ptr()
+    if top:
+        index, values = torch.empty(rows, top, dtype=torch.int32, device=device), torch.empty(rows, top, dtype=f32, device=device)
+        ip, vp = index.data_ptr(), values.data_ptr()
+    _check(load_library().nvfp4_logprob_forward(zp, dt, ld, rows, cols, scale, tp, kind, lp, stats.data_ptr(), lse.data_ptr(), hp, top, ip, vp, ws, ws_bytes, _stream()))
+    return LogProbs(logprob, lse, stats, h, index, values)
 
 
 def _dlogits(logits: torch.Tensor, dt: int, out_dtype: Optional[int], out: Optional[torch.Tensor]):
@@ -795,7 +803,7 @@ def _dlogits(logits: torch.Tensor, dt: int, out_dtype: Optional[int], out: Optio
     ot, op, ldd = _matrix(out, "out", (rows, cols))
     if out_dtype is not None and ot != out_dtype:
         raise ValueError("out must be of type out_dtype")
-    return out, ot, op, -(-cols // 8) * 8 if rows == 1 else ldd
+    return out, ot, op, -(-cols // 8) * 8 if rows <= 1 else ldd
 
 
 def nvfp4_logprob_backward(logits: torch.Tensor, targets: Optional[torch.Tensor], stats: torch.Tensor, g_logprob: Optional[torch.Tensor] = None,
@@ -809,7 +817,7 @@ def nvfp4_logprob_backward(logits: torch.Tensor, targets: Optional[torch.Tensor]
     kind, tp = (INDEX_I64, None) if targets is None else _indices(targets, rows, "targets")
     if stats.dtype != torch.float32 or stats.shape != (rows, 2) or not stats.is_contiguous():
         raise ValueError("stats must be what the forward pass gave: contiguous float32 [rows, 2]")
-    if ld % 8 and rows == 1:
+    if ld % 8 and rows <= 1:
         ld = -(-cols // 8) * 8
     g = [_vector(t, rows, what) for t, what in ((g_logprob, "g_logprob"), (g_lse, "g_lse"), (g_entropy, "g_entropy"), (entropy, "entropy"))]
     out, ot, op, ldd = _dlogits(logits, dt, out_dtype, out)
@@ -823,7 +831,7 @@ def nvfp4_logprob_with_gradient(logits: torch.Tensor, targets: torch.Tensor, g_l
     _here(logits, targets, g_logprob, out)
     dt, zp, ld = _matrix(logits, "logits")
     (rows, cols), device = logits.shape, logits.device
-    if ld % 8 and rows == 1:
+    if ld % 8 and rows <= 1:
         ld = -(-cols // 8) * 8
     kind, tp = _indices(targets, rows, "targets")
     gp = _vector(g_logprob, rows, "g_logprob")

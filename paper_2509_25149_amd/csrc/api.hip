@@ -728,6 +728,14 @@ void fill_backward(LogprobBackward& a, const void* logits, int dtype, int64_t ld
   a.bf16 = dtype == NVFP4_OUT_BF16, a.out_bf16 = d_dtype == NVFP4_OUT_BF16, a.i64 = index_type == NVFP4_INDEX_I64;
 }
 
+// A gradient written over the logits has their type and leading dimension.
+int check_dlogits(const void* logits, int dtype, int64_t ld, int64_t rows, int64_t cols, const void* dlogits, int d_dtype, int64_t ldd) {
+  if (!element_type(d_dtype)) return NVFP4_ERR_INVALID_ARG;
+  const int rc = check_tensor(dlogits, rows, cols, ldd, false);
+  if (rc != NVFP4_OK || dlogits != logits || rows == 0) return rc;
+  return d_dtype == dtype && (ldd == ld || rows == 1) ? NVFP4_OK : NVFP4_ERR_INVALID_ARG;
+}
+
 int64_t grad_elements(const nvfp4_grad& g) { return g.rows * g.cols; }
 size_t element_size(int dtype) { return dtype == NVFP4_OUT_BF16 ? 2 : 4; }
 
@@ -869,8 +877,7 @@ int nvfp4_logprob_backward(const void* logits, int dtype, int64_t ld, int64_t ro
                            int d_dtype, int64_t ldd, nvfp4_stream_t stream) {
   int rc = check_logits(logits, dtype, ld, rows, cols, scale, targets, index_type);
   if (rc != NVFP4_OK) return rc;
-  if (!element_type(d_dtype)) return NVFP4_ERR_INVALID_ARG;
-  rc = check_tensor(dlogits, rows, cols, ldd, false);
+  rc = check_dlogits(logits, dtype, ld, rows, cols, dlogits, d_dtype, ldd);
   if (rc != NVFP4_OK) return rc;
   if (rows && (!stats || (g_logprob && !targets) || (g_entropy && !entropy))) return NVFP4_ERR_INVALID_ARG;
   if (!aligned(stats, 4) || !aligned(g_logprob, 4) || !aligned(g_lse, 4) || !aligned(g_entropy, 4) || !aligned(entropy, 4)) return NVFP4_ERR_INVALID_ARG;
@@ -885,8 +892,7 @@ int nvfp4_logprob_with_gradient(const void* logits, int dtype, int64_t ld, int64
                                 size_t workspace_bytes, nvfp4_stream_t stream) {
   int rc = check_logits(logits, dtype, ld, rows, cols, scale, targets, index_type);
   if (rc != NVFP4_OK) return rc;
-  if (!element_type(d_dtype)) return NVFP4_ERR_INVALID_ARG;
-  rc = check_tensor(dlogits, rows, cols, ldd, false);
+  rc = check_dlogits(logits, dtype, ld, rows, cols, dlogits, d_dtype, ldd);
   if (rc != NVFP4_OK) return rc;
   if (rows && (!targets || !g_logprob || !stats)) return NVFP4_ERR_INVALID_ARG;
   if (!aligned(g_logprob, 4) || !aligned(logprob, 4) || !aligned(stats, 4) || !aligned(lse, 4)) return NVFP4_ERR_INVALID_ARG;

@@ -73,8 +73,8 @@ __device__ __forceinline__ void keys_of(const void* ids, bool i64, int t, int st
 }
 
 // Up to kFewTokens: a token's place is the number of tokens before it, counted: two operations a pair.  A workgroup holds the keys and takes 32 tokens; a wavefront four of them, each
-// lane against every 64th piece of four keys.
-constexpr int kFewTokens = 8192, kTile = 2048, kRankTokens = 32, kRankEach = 4;
+// lane against every 64th piece of four keys.  (us for the whole gradient of 8200 / 16384 tokens, 700 rows of 256, so 27 / 38 and by passes 33 / 33.)
+constexpr int kFewTokens = 12288, kTile = 2048, kRankTokens = 32, kRankEach = 4;
 
 constexpr int kRankThreads = kRankTokens / kRankEach * 64;
 
@@ -144,8 +144,8 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(const void* ids, boo
 }
 
 // More: passes over digits of up to nine bits, each stable: count the digits of a tile, sum up, put in place.  A tile of 2048 belongs to a workgroup, whose
-// wavefronts have 512 consecutive keys each.
-constexpr int kMostDigits = 512;
+// wavefronts have 512 consecutive keys each.  Counts of up to kFoldTiles tiles are summed up by every workgroup for itself, which saves a launch.
+constexpr int kMostDigits = 512, kFoldTiles = 32;
 struct SortPass {
   const void* ids;                      // first pass: keys are made from these
   const uint32_t *keys, *order;         // later ones
@@ -233,13 +233,50 @@ __global__ __launch_bounds__(256) void sort_place_kernel(SortPass p) {
     if (key[r] != kNoKey) atomicAdd(&next[wave][(key[r] >> p.shift) & (p.digits - 1)], 1u);
   }
   __syncthreads();
-  for (int d = threadIdx.x; d < p.digits; d += 256) {
-    uint32_t at = p.counts[static_cast<int64_t>(d) * p.tiles + blockIdx.x];
+  // Where this tile's first key of a digit goes: two digits to a thread.
+  uint32_t at[2] = {};
+  if (p.tiles > kFoldTiles) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int d = static_cast<int>(threadIdx.x) * 2 + e;
+      if (d < p.digits) at[e] = p.counts[static_cast<int64_t>(d) * p.tiles + blockIdx.x];
+    }
+  } else {
+    __shared__ uint32_t wave_total[4];
+    uint32_t total[2] = {};
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int d = static_cast<int>(threadIdx.x) * 2 + e;
+      if (d >= p.digits) continue;
+#pragma unroll 8
+      for (int i = 0; i < p.tiles; ++i) {
+        const uint32_t n = p.counts[d * p.tiles + i];
+        total[e] += n;
+        at[e] += i < static_cast<int>(blockIdx.x) ? n : 0u;
+      }
+    }
+    uint32_t up = total[0] + total[1];
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const uint32_t o = __shfl_up(up, off, 64);
+      if (lane >= off) up += o;
+    }
+    if (lane == 63) wave_total[wave] = up;
+    __syncthreads();
+    uint32_t before = up - total[0] - total[1];
+    for (int w = 0; w < wave; ++w) before += wave_total[w];
+    at[0] += before;
+    at[1] += before + total[0];
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int d = static_cast<int>(threadIdx.x) * 2 + e;
+    if (d >= p.digits) continue;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
       const uint32_t n = next[w][d];
-      next[w][d] = at;
-      at += n;
+      next[w][d] = at[e];
+      at[e] += n;
     }
   }
   __syncthreads();
@@ -587,8 +624,10 @@ hipError_t launch_embedding_backward(const EmbeddingBackward& a, void* workspace
       q.to_keys = keys, q.to_order = order;
       hipLaunchKernelGGL(sort_count_kernel, dim3(p.tiles), dim3(256), 0, s, q);
       if ((e = hipGetLastError()) != hipSuccess) return e;
-      hipLaunchKernelGGL(sort_scan_kernel, dim3(1), dim3(1024), 0, s, q.counts, p.tiles << p.digit_bits);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
+      if (p.tiles > kFoldTiles) {
+        hipLaunchKernelGGL(sort_scan_kernel, dim3(1), dim3(1024), 0, s, q.counts, p.tiles << p.digit_bits);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+      }
       hipLaunchKernelGGL(sort_place_kernel, dim3(p.tiles), dim3(256), 0, s, q);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }

@@ -70,15 +70,17 @@ def test_logprob_refuses(lib):
     w = ctypes.c_size_t()
     assert lib.nvfp4_logprob_workspace_bytes(1, 4, 5, ctypes.addressof(w)) == -2 and lib.nvfp4_logprob_workspace_bytes(1, 4, 4, None) == -1
 
-    def bwd(z=P, dt=1, ld=104, rows=4, cols=100, scale=1.0, t=P, it=1, st=P, g=P, gl=None, ge=None, h=None, dz=P, ot=1, ldd=104):
+    def bwd(z=P, dt=1, ld=104, rows=4, cols=100, scale=1.0, t=P, it=1, st=P, g=P, gl=None, ge=None, h=None, dz=2 * P, ot=1, ldd=104):
         return lib.nvfp4_logprob_backward(z, dt, ld, rows, cols, scale, t, it, st, g, gl, ge, h, dz, ot, ldd, None)
     assert bwd(z=None) == -1 and bwd(dz=None) == -1 and bwd(dz=P + 8) == -1 and bwd(ot=2) == -1 and bwd(st=None) == -1 and bwd(t=None) == -1 and bwd(ge=P) == -1
     assert bwd(g=P + 2) == -1 and bwd(gl=P + 2) == -1 and bwd(ge=P + 2, h=P) == -1 and bwd(ge=P, h=P + 2) == -1 and bwd(scale=-1.0) == -1
     assert bwd(ldd=96) == -2 and bwd(ldd=100) == -2 and bwd(ld=100) == -2 and bwd(cols=0) == -2
 
-    def both(z=P, dt=1, ld=104, rows=4, cols=100, scale=1.0, t=P, it=1, g=P, lp=P, st=P, lse=P, dz=P, ot=1, ldd=104, ws=None, size=0):
+    assert bwd(dz=P, ot=0) == -1 and bwd(dz=P, ldd=112) == -1                                # over the logits, but laid out otherwise
+
+    def both(z=P, dt=1, ld=104, rows=4, cols=100, scale=1.0, t=P, it=1, g=P, lp=P, st=P, lse=P, dz=2 * P, ot=1, ldd=104, ws=None, size=0):
         return lib.nvfp4_logprob_with_gradient(z, dt, ld, rows, cols, scale, t, it, g, lp, st, lse, dz, ot, ldd, ws, size, None)
-    assert both(z=None) == -1 and both(t=None) == -1 and both(g=None) == -1 and both(st=None) == -1 and both(dz=None) == -1 and both(ot=3) == -1 and both(lse=P + 2) == -1
+    assert both(dz=P, ot=0) == -1 and both(dz=P, ldd=112) == -1 and both(z=None) == -1 and both(t=None) == -1 and both(g=None) == -1 and both(st=None) == -1 and both(dz=None) == -1 and both(ot=3) == -1 and both(lse=P + 2) == -1
     assert both(ldd=96) == -2 and both(rows=-1) == -2 and both(rows=1, cols=131072, ld=131072, ldd=131072) == -6
 
 
