@@ -24,6 +24,49 @@ __device__ __forceinline__ int64_t index_at(const void* p, bool i64, int64_t i) 
   return i64 ? static_cast<const int64_t*>(p)[i] : static_cast<const int32_t*>(p)[i];
 }
 
+// ---------------------------------------------------------------- a thread's piece of a row
+// Eight columns, or four of FP32: 16 bytes, so that a wavefront's access covers whole lines.  FP32 logits whose gradient is bf16 are taken by eight all the same, for the sake of
+// the stores (8192 x 20000: 225 us by four, 192 by eight).
+template <bool kBf16>
+constexpr int kGroup = kBf16 ? 8 : 4;
+template <bool kBf16, int kN>
+struct Group : Eight<kBf16> {
+  static_assert(kN == 8);
+  __device__ __forceinline__ void load(const void* row, int g) { Eight<kBf16>::load(row, static_cast<int64_t>(g) * 8); }
+};
+template <>
+struct Group<false, 4> {
+  float4v w;
+  __device__ __forceinline__ void load(const void* row, int g) { w = static_cast<const float4v*>(row)[g]; }
+  __device__ __forceinline__ void get(float (&v)[4]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = w[i];
+  }
+};
+typedef uint32_t uint32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t uint32x4 __attribute__((ext_vector_type(4)));
+
+// The results of a group.  kStream: no cache should keep them.
+template <bool kStream, typename T>
+__device__ __forceinline__ void put(T v, T* to) {
+  if (kStream) __builtin_nontemporal_store(v, to);
+  else *to = v;
+}
+template <bool kStream, bool kBf16>
+__device__ __forceinline__ void put_group(void* row, int g, const float (&v)[8]) {
+  if (kBf16) {
+    put<kStream>(uint32x4{f32x2_to_bf16(v[0], v[1]), f32x2_to_bf16(v[2], v[3]), f32x2_to_bf16(v[4], v[5]), f32x2_to_bf16(v[6], v[7])}, static_cast<uint32x4*>(row) + g);
+  } else {
+    put<kStream>(float4v{v[0], v[1], v[2], v[3]}, static_cast<float4v*>(row) + 2 * static_cast<int64_t>(g));
+    put<kStream>(float4v{v[4], v[5], v[6], v[7]}, static_cast<float4v*>(row) + 2 * static_cast<int64_t>(g) + 1);
+  }
+}
+template <bool kStream, bool kBf16>
+__device__ __forceinline__ void put_group(void* row, int g, const float (&v)[4]) {
+  if (kBf16) put<kStream>(uint32x2{f32x2_to_bf16(v[0], v[1]), f32x2_to_bf16(v[2], v[3])}, static_cast<uint32x2*>(row) + g);
+  else put<kStream>(float4v{v[0], v[1], v[2], v[3]}, static_cast<float4v*>(row) + g);
+}
+
 // ---------------------------------------------------------------- sums of exponentials relative to a maximum
 // s = sum 2^((z - m) c);  e = sum (z - m) c 2^((z - m) c), c = scale log2(e).  Nothing but -infinity: m = kLowest, s = 0.
 // A NaN or +infinity makes s NaN, and s stays so.
@@ -93,46 +136,59 @@ __device__ __forceinline__ Sum workgroup_join(Sum a, float c, Sum* lds) {
   return a;
 }
 
-// Eight columns from 8 g on; those past the end of the row are not there (-infinity).
 template <bool kBf16>
-__device__ __forceinline__ void rest_of_row(const void* row, int g, int cols, float (&v)[8]) {
+__device__ __forceinline__ float value_at(const void* row, int64_t col) {
+  return kBf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(row)[col]) << 16) : static_cast<const float*>(row)[col];
+}
+
+// A group at the end of a row: columns past it are not there (-infinity).
+template <bool kBf16, int kN>
+__device__ __forceinline__ void rest_of_row(const void* row, int g, int cols, float (&v)[kN]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int col = g * 8 + i;
-    v[i] = -kInfinity;
-    if (col < cols) v[i] = kBf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(row)[col]) << 16) : static_cast<const float*>(row)[col];
+  for (int i = 0; i < kN; ++i) v[i] = g * kN + i < cols ? value_at<kBf16>(row, g * kN + i) : -kInfinity;
+}
+
+// A group, whole or not.
+template <bool kBf16, int kN>
+__device__ __forceinline__ void group_of(const void* row, int g, int cols, float (&v)[kN]) {
+  if (g < cols / kN) {
+    Group<kBf16, kN> x;
+    x.load(row, g);
+    x.get(v);
+  } else {
+    rest_of_row<kBf16>(row, g, cols, v);
   }
 }
 
-// A thread's share of groups [g0, g1) of eight columns.
-template <bool kBf16, bool kEntropy>
+template <bool kEntropy, bool kBf16, int kN, int kGroups>
+__device__ __forceinline__ void add_groups(Sum& a, const Group<kBf16, kN> (&x)[kGroups], float c) {
+  float v[kGroups * kN];
+#pragma unroll
+  for (int u = 0; u < kGroups; ++u) {
+    float w[kN];
+    x[u].get(w);
+#pragma unroll
+    for (int i = 0; i < kN; ++i) v[u * kN + i] = w[i];
+  }
+  add<kEntropy>(a, v, c);
+}
+
+// A thread's share of groups [g0, g1), 32 columns at a time.
+template <bool kBf16, bool kEntropy, int kN>
 __device__ __forceinline__ Sum sum_of_groups(const void* row, int g0, int g1, int cols, float c) {
-  const int step = blockDim.x, whole = min(g1, cols >> 3);
+  constexpr int kBatch = 32 / kN;
+  const int step = blockDim.x, whole = min(g1, cols / kN);
   Sum a{kLowest, 0.0f, 0.0f};
   int g = g0 + static_cast<int>(threadIdx.x);
-  for (; g + 3 * step < whole; g += 4 * step) {
-    Eight<kBf16> x[4];
-    float v[32];
+  for (; g + (kBatch - 1) * step < whole; g += kBatch * step) {
+    Group<kBf16, kN> x[kBatch];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) x[u].load(row, static_cast<int64_t>(g + u * step) * 8);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      float w[8];
-      x[u].get(w);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[u * 8 + i] = w[i];
-    }
-    add<kEntropy>(a, v, c);
+    for (int u = 0; u < kBatch; ++u) x[u].load(row, g + u * step);
+    add_groups<kEntropy>(a, x, c);
   }
   for (; g < g1; g += step) {
-    float v[8];
-    if (g < whole) {
-      Eight<kBf16> x;
-      x.load(row, static_cast<int64_t>(g) * 8);
-      x.get(v);
-    } else {
-      rest_of_row<kBf16>(row, g, cols, v);
-    }
+    float v[kN];
+    group_of<kBf16>(row, g, cols, v);
     add<kEntropy>(a, v, c);
   }
   return a;
@@ -144,11 +200,6 @@ struct RowStats {
   __device__ __forceinline__ explicit RowStats(const Sum& a) : m(a.s == 0.0f ? 0.0f : a.m), logsum(a.s == 0.0f ? kInfinity : logf(a.s)) {}
   __device__ __forceinline__ float logprob(float z, float scale) const { return (z - m) * scale - logsum; }
 };
-
-template <bool kBf16>
-__device__ __forceinline__ float value_at(const void* row, int64_t col) {
-  return kBf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(row)[col]) << 16) : static_cast<const float*>(row)[col];
-}
 
 __device__ __forceinline__ void write_row(const LogprobForward& a, int64_t row, const Sum& sum, const RowStats& r, float at_target, bool counted) {
   const bool empty = sum.s == 0.0f;
@@ -179,30 +230,19 @@ struct TopShared {
   uint32_t n_found;
 };
 
-// Eight values of a group, those past the end of the row at -infinity.
-template <bool kBf16>
-__device__ __forceinline__ void group_of(const void* row, int g, int cols, float (&v)[8]) {
-  if (g < cols >> 3) {
-    Eight<kBf16> x;
-    x.load(row, static_cast<int64_t>(g) * 8);
-    x.get(v);
-  } else {
-    rest_of_row<kBf16>(row, g, cols, v);
-  }
-}
-
 // The best of a thread's share of groups [g0, g1) that is worse than `last`.
 template <bool kBf16>
 __device__ __forceinline__ uint64_t best_of_share(const void* row, int g0, int g1, int cols, uint64_t last) {
   uint64_t best = 0ull;
 #pragma unroll 4
   for (int g = g0 + static_cast<int>(threadIdx.x); g < g1; g += blockDim.x) {
-    float v[8];
+    constexpr int kN = kGroup<kBf16>;
+    float v[kN];
     group_of<kBf16>(row, g, cols, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint64_t p = place(v[j], g * 8 + j);
-      if (g * 8 + j < cols && p < last && p > best) best = p;
+    for (int j = 0; j < kN; ++j) {
+      const uint64_t p = place(v[j], g * kN + j);
+      if (g * kN + j < cols && p < last && p > best) best = p;
     }
   }
   return best;
@@ -234,26 +274,27 @@ __device__ __forceinline__ void take_best(const void* row, int g0, int g1, int c
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
   const int turns = (g1 - g0 + T - 1) / T, items = __popcll(holders) * turns;
-  for (int i0 = lane; i0 < items; i0 += 4 * 64) {   // four groups of eight columns asked for together
-    Eight<kBf16> x[4];
+  constexpr int kN = kGroup<kBf16>;
+  for (int i0 = lane; i0 < items; i0 += 4 * 64) {   // four groups asked for together
+    Group<kBf16, kN> x[4];
     int g[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int i = i0 + u * 64;
       g[u] = i < items ? g0 + wave * 64 + s.lanes[wave][i / turns] + i % turns * T : g1;
-      if (g[u] < min(g1, cols >> 3)) x[u].load(row, static_cast<int64_t>(g[u]) * 8);
+      if (g[u] < min(g1, cols / kN)) x[u].load(row, g[u]);
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (g[u] >= g1) continue;
-      float v[8];
-      if (g[u] < cols >> 3) x[u].get(v);
+      float v[kN];
+      if (g[u] < cols / kN) x[u].get(v);
       else rest_of_row<kBf16>(row, g[u], cols, v);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (g[u] * 8 + j < cols && order_of(v[j]) >= bound) {
+      for (int j = 0; j < kN; ++j) {
+        if (g[u] * kN + j < cols && order_of(v[j]) >= bound) {
           const uint32_t at = atomicAdd(&s.n_found, 1u);
-          if (at < kCandidates) s.found[at] = place(v[j], g[u] * 8 + j);
+          if (at < kCandidates) s.found[at] = place(v[j], g[u] * kN + j);
         }
       }
     }
@@ -262,8 +303,8 @@ __device__ __forceinline__ void take_best(const void* row, int g0, int g1, int c
   int n = static_cast<int>(s.n_found);
   if (n < k) {   // everything above -infinity is among them: the first T >= k + 32 columns have enough others, unless they are NaN
     __syncthreads();
-    const int col = g0 * 8 + t;
-    if (col < min(g1 * 8, cols) && value_at<kBf16>(row, col) == -kInfinity) {
+    const int col = g0 * kN + t;
+    if (col < min(g1 * kN, cols) && value_at<kBf16>(row, col) == -kInfinity) {
       const uint32_t at = atomicAdd(&s.n_found, 1u);
       s.found[at] = place(-kInfinity, col);
     }
@@ -310,7 +351,8 @@ __global__ __launch_bounds__(kMostThreads) void logprob_forward_kernel(LogprobFo
   __shared__ Sum sums[kMostThreads / 64];
   const int part = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.parts));
   const int64_t row = a.row0 + blockIdx.x / static_cast<unsigned>(a.parts);
-  const int cols = static_cast<int>(a.cols), groups = (cols + 7) >> 3, each = (groups + a.parts - 1) / a.parts;
+  constexpr int kN = kGroup<kBf16>;
+  const int cols = static_cast<int>(a.cols), groups = (cols + kN - 1) / kN, each = (groups + a.parts - 1) / a.parts;
   const int g0 = min(part * each, groups), g1 = min(g0 + each, groups);
   const void* z = static_cast<const char*>(a.z) + row * a.ld * (kBf16 ? 2 : 4);
   const float c = a.scale * kLog2E;
@@ -321,7 +363,7 @@ __global__ __launch_bounds__(kMostThreads) void logprob_forward_kernel(LogprobFo
     counted = target >= 0 && target < cols;
     if (counted) at_target = value_at<kBf16>(z, target);
   }
-  const Sum mine = sum_of_groups<kBf16, kEntropy>(z, g0, g1, cols, c);
+  const Sum mine = sum_of_groups<kBf16, kEntropy, kN>(z, g0, g1, cols, c);
   const Sum all = workgroup_join<kEntropy>(mine, c, sums);
   if (a.parts > 1) {
     float* to = a.partial + (row * a.parts + part) * 4;
@@ -399,8 +441,6 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobForward a) {
 
 // ---------------------------------------------------------------- gradient of the logits
 
-typedef uint32_t uint32x4 __attribute__((ext_vector_type(4)));
-
 // What is the same for a row: dz_j = p_j (a - b log2 p_j), log2 p_j = (z_j - m) c - l; and what the target's column gets on top.
 struct RowGradient {
   float m, l, a, b, at_target;
@@ -414,42 +454,32 @@ struct RowGradient {
     at_target = scale * g;
     target = counted && logsum != kInfinity ? static_cast<int>(target_) : -1;
   }
-  template <bool kEntropy>
-  __device__ __forceinline__ void of(float (&v)[8], int g, float c) const {
+  template <bool kEntropy, int kN>
+  __device__ __forceinline__ void of(float (&v)[kN], int g, float c) const {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < kN; ++i) {
       const float t = (v[i] - m) * c - l, p = __builtin_amdgcn_exp2f(t);
       v[i] = p * (kEntropy ? a - b * far_at_most(t) : a);
     }
-    if (g == target >> 3) {
+    if (g == target >> (kN == 8 ? 3 : 2)) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] += i == (target & 7) ? at_target : 0.0f;
+      for (int i = 0; i < kN; ++i) v[i] += i == (target & (kN - 1)) ? at_target : 0.0f;
     }
   }
 };
 
-template <bool kStream>
-__device__ __forceinline__ void put8(void* row, int64_t col, bool bf16, const float (&v)[8]) {
-  if (!kStream) {
-    store8(row, col, bf16, v);
-  } else if (bf16) {
-    const uint32x4 w = {f32x2_to_bf16(v[0], v[1]), f32x2_to_bf16(v[2], v[3]), f32x2_to_bf16(v[4], v[5]), f32x2_to_bf16(v[6], v[7])};
-    __builtin_nontemporal_store(w, reinterpret_cast<uint32x4*>(static_cast<uint16_t*>(row) + col));
-  } else {
-    float4v* p = reinterpret_cast<float4v*>(static_cast<float*>(row) + col);
-    __builtin_nontemporal_store(float4v{v[0], v[1], v[2], v[3]}, p);
-    __builtin_nontemporal_store(float4v{v[4], v[5], v[6], v[7]}, p + 1);
-  }
-}
+template <bool kInBf16, bool kOutBf16>
+constexpr int kGradientGroup = kInBf16 || kOutBf16 ? 8 : 4;
 
 template <bool kInBf16, bool kOutBf16, bool kEntropy>
 __device__ __forceinline__ void gradient_of_rest(const void* z, void* dz, int g, int cols, const RowGradient& r, float c) {
-  float v[8];
+  constexpr int kN = kGradientGroup<kInBf16, kOutBf16>;
+  float v[kN];
   rest_of_row<kInBf16>(z, g, cols, v);
   r.of<kEntropy>(v, g, c);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int col = g * 8 + i;
+  for (int i = 0; i < kN; ++i) {
+    const int col = g * kN + i;
     if (col < cols) {
       if (kOutBf16) static_cast<uint16_t*>(dz)[col] = static_cast<uint16_t>(f32_to_bf16(v[i]));
       else static_cast<float*>(dz)[col] = v[i];
@@ -458,31 +488,31 @@ __device__ __forceinline__ void gradient_of_rest(const void* z, void* dz, int g,
 }
 
 // Groups [g0, g1) of a row by the workgroup's threads, from the end to the front.
-// kStream: results that no cache should keep.
 template <bool kInBf16, bool kOutBf16, bool kEntropy, bool kStream>
 __device__ __forceinline__ void gradient_of_groups(const void* z, void* dz, int g0, int g1, int cols, const RowGradient& r, float c) {
-  const int step = blockDim.x, whole = min(g1, cols >> 3);
+  constexpr int kN = kGradientGroup<kInBf16, kOutBf16>;
+  const int step = blockDim.x, whole = min(g1, cols / kN);
   if (whole < g1 && threadIdx.x == 0) gradient_of_rest<kInBf16, kOutBf16, kEntropy>(z, dz, whole, cols, r, c);
   int g = whole - 1 - static_cast<int>(threadIdx.x);
   for (; g - 3 * step >= g0; g -= 4 * step) {
-    Eight<kInBf16> x[4];
+    Group<kInBf16, kN> x[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) x[u].load(z, static_cast<int64_t>(g - u * step) * 8);
+    for (int u = 0; u < 4; ++u) x[u].load(z, g - u * step);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      float v[8];
+      float v[kN];
       x[u].get(v);
       r.of<kEntropy>(v, g - u * step, c);
-      put8<kStream>(dz, static_cast<int64_t>(g - u * step) * 8, kOutBf16, v);
+      put_group<kStream, kOutBf16>(dz, g - u * step, v);
     }
   }
   for (; g >= g0; g -= step) {
-    Eight<kInBf16> x;
-    float v[8];
-    x.load(z, static_cast<int64_t>(g) * 8);
+    Group<kInBf16, kN> x;
+    float v[kN];
+    x.load(z, g);
     x.get(v);
     r.of<kEntropy>(v, g, c);
-    put8<kStream>(dz, static_cast<int64_t>(g) * 8, kOutBf16, v);
+    put_group<kStream, kOutBf16>(dz, g, v);
   }
 }
 
@@ -491,7 +521,8 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobBackward a
   const uint32_t w = blockIdx.x;
   const int part = static_cast<int>(w % static_cast<unsigned>(a.parts));
   const int64_t row = a.row0 + w / static_cast<unsigned>(a.parts);
-  const int cols = static_cast<int>(a.cols), groups = (cols + 7) >> 3, each = (groups + a.parts - 1) / a.parts;
+  constexpr int kN = kGradientGroup<kInBf16, kOutBf16>;
+  const int cols = static_cast<int>(a.cols), groups = (cols + kN - 1) / kN, each = (groups + a.parts - 1) / a.parts;
   const int g0 = min(part * each, groups), g1 = min(g0 + each, groups);
   const RowGradient r(a.stats[2 * row], a.stats[2 * row + 1], a.scale, a.g_logprob ? a.g_logprob[row] : 0.0f, a.g_lse ? a.g_lse[row] : 0.0f,
                       kEntropy ? a.g_entropy[row] : 0.0f, kEntropy ? a.entropy[row] : 0.0f, a.targets ? index_at(a.targets, a.i64, row) : -1, cols);
@@ -499,30 +530,17 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobBackward a
                                                   static_cast<char*>(a.dz) + row * a.ldd * (kOutBf16 ? 2 : 4), g0, g1, cols, r, a.scale * kLog2E);
 }
 
-// Loss and gradient in one launch: a workgroup takes a row, sums over it and goes over it again from its end.  The last groups of eight columns stay on the CU between the two --
-// kKeepRegisters of each thread in registers, kKeepLds in LDS --, those in front are read again, from the L2 or the memory-side cache.
-constexpr int kKeepRegisters = 4, kKeepLds = 4;   // of bf16; half as many of FP32
-
-template <bool kBf16, int kN>
-__device__ __forceinline__ void add_groups(Sum& a, const Eight<kBf16> (&x)[kN], float c) {
-  float v[kN * 8];
-#pragma unroll
-  for (int u = 0; u < kN; ++u) {
-    float w[8];
-    x[u].get(w);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[u * 8 + i] = w[i];
-  }
-  add<false>(a, v, c);
-}
+// Loss and gradient in one launch: a workgroup takes a row, sums over it and goes over it again from its end.  The last groups stay on the CU between the two --
+// half in registers, half in LDS --, those in front are read again, from the L2 or the memory-side cache.
+constexpr int kKeepBytes = 64;   // of a thread, in either
 
 template <int T, bool kInBf16, bool kOutBf16, bool kStream>
 __global__ __launch_bounds__(T, 8) void logprob_loss_kernel(LogprobForward f, LogprobBackward b) {
-  constexpr int kRegisters = kInBf16 ? kKeepRegisters : kKeepRegisters / 2, kLds = kInBf16 ? kKeepLds : kKeepLds / 2;
+  constexpr int kN = kGradientGroup<kInBf16, kOutBf16>, kKeep = kKeepBytes / static_cast<int>(sizeof(Group<kInBf16, kN>));
   __shared__ Sum sums[T / 64];
-  __shared__ Eight<kInBf16> kept[kLds * T];
+  __shared__ Group<kInBf16, kN> kept[kKeep * T];
   const int64_t row = f.row0 + blockIdx.x;
-  const int t = threadIdx.x, cols = static_cast<int>(f.cols), whole = cols >> 3;
+  const int t = threadIdx.x, cols = static_cast<int>(f.cols), whole = cols / kN;
   const void* z = static_cast<const char*>(f.z) + row * f.ld * (kInBf16 ? 2 : 4);
   void* dz = static_cast<char*>(b.dz) + row * b.ldd * (kOutBf16 ? 2 : 4);
   const float c = f.scale * kLog2E;
@@ -530,26 +548,26 @@ __global__ __launch_bounds__(T, 8) void logprob_loss_kernel(LogprobForward f, Lo
   const bool counted = target >= 0 && target < cols;
   const float at_target = counted ? value_at<kInBf16>(z, target) : 0.0f, g = b.g_logprob[row];
 
-  const int again = max(0, whole - (kLds + kRegisters) * T), first = again + t;   // groups [0, again) are read twice
-  Sum mine = sum_of_groups<kInBf16, false>(z, 0, again, again * 8, c);
+  const int again = max(0, whole - 2 * kKeep * T), first = again + t;   // groups [0, again) are read twice
+  Sum mine = sum_of_groups<kInBf16, false, kN>(z, 0, again, again * kN, c);
 #pragma unroll
-  for (int u = 0; u < kLds; ++u) {
-    Eight<kInBf16> x[1];
+  for (int u = 0; u < kKeep; ++u) {
+    Group<kInBf16, kN> x[1];
     if (first + u * T < whole) {
-      x[0].load(z, static_cast<int64_t>(first + u * T) * 8);
+      x[0].load(z, first + u * T);
       kept[u * T + t] = x[0];
-      add_groups(mine, x, c);
+      add_groups<false>(mine, x, c);
     }
   }
-  Eight<kInBf16> x[kRegisters][1];
+  Group<kInBf16, kN> x[kKeep][1];
 #pragma unroll
-  for (int u = 0; u < kRegisters; ++u)
-    if (first + (kLds + u) * T < whole) x[u][0].load(z, static_cast<int64_t>(first + (kLds + u) * T) * 8);
+  for (int u = 0; u < kKeep; ++u)
+    if (first + (kKeep + u) * T < whole) x[u][0].load(z, first + (kKeep + u) * T);
 #pragma unroll
-  for (int u = 0; u < kRegisters; ++u)
-    if (first + (kLds + u) * T < whole) add_groups(mine, x[u], c);
-  if ((cols & 7) && t == T - 1) {
-    float v[8];
+  for (int u = 0; u < kKeep; ++u)
+    if (first + (kKeep + u) * T < whole) add_groups<false>(mine, x[u], c);
+  if (cols % kN && t == T - 1) {
+    float v[kN];
     rest_of_row<kInBf16>(z, whole, cols, v);
     add<false>(mine, v, c);
   }
@@ -557,20 +575,20 @@ __global__ __launch_bounds__(T, 8) void logprob_loss_kernel(LogprobForward f, Lo
   const RowStats r(all);
   if (t == 0) write_row(f, row, all, r, at_target, counted);
   const RowGradient d(r.m, r.logsum, f.scale, g, 0.0f, 0.0f, 0.0f, target, cols);
-  auto store = [&](const Eight<kInBf16>& x, int group) {
-    float v[8];
+  auto store = [&](const Group<kInBf16, kN>& x, int group) {
+    float v[kN];
     x.get(v);
     d.of<false>(v, group, c);
-    put8<kStream>(dz, static_cast<int64_t>(group) * 8, kOutBf16, v);
+    put_group<kStream, kOutBf16>(dz, group, v);
   };
-  if ((cols & 7) && t == T - 1) gradient_of_rest<kInBf16, kOutBf16, false>(z, dz, whole, cols, d, c);
+  if (cols % kN && t == T - 1) gradient_of_rest<kInBf16, kOutBf16, false>(z, dz, whole, cols, d, c);
 #pragma unroll
-  for (int u = kRegisters - 1; u >= 0; --u)
-    if (first + (kLds + u) * T < whole) store(x[u][0], first + (kLds + u) * T);
+  for (int u = kKeep - 1; u >= 0; --u)
+    if (first + (kKeep + u) * T < whole) store(x[u][0], first + (kKeep + u) * T);
 #pragma unroll
-  for (int u = kLds - 1; u >= 0; --u)
+  for (int u = kKeep - 1; u >= 0; --u)
     if (first + u * T < whole) store(kept[u * T + t], first + u * T);
-  gradient_of_groups<kInBf16, kOutBf16, false, kStream>(z, dz, 0, again, again * 8, d, c);
+  gradient_of_groups<kInBf16, kOutBf16, false, kStream>(z, dz, 0, again, again * kN, d, c);
 }
 
 // ---------------------------------------------------------------- launches
@@ -586,8 +604,7 @@ struct ForwardShape {
 // A row to a workgroup, but for few long rows, which are cut into pieces (us on the GPU without / with pieces: 1 x 131072 11.5 / 5.6, 64 x 131072 12 / 9, 100 x 131072 12 / 11, 1 to 100 x 50257
 // 6.9 / 5.8 to 8.7, where the second launch costs the host 3 more).  Threads by the bytes of a row; the best alternatives are looked for by 256 at least.
 ForwardShape forward_shape(int64_t rows, int64_t cols, bool bf16, bool top) {
-  const int64_t groups = (cols + 7) / 8;
-  if (rows < 96 && groups >= 8192) return {static_cast<int>(std::min<int64_t>(kMostParts, 4 * kCUs / std::max<int64_t>(rows, 1))), 256};
+  if (rows < 96 && cols >= 65536) return {static_cast<int>(std::min<int64_t>(kMostParts, 4 * kCUs / std::max<int64_t>(rows, 1))), 256};
   const int64_t bytes = cols * (bf16 ? 2 : 4);
   return {1, bytes <= (top ? 2 << 10 : 16 << 10) ? 64 : bytes <= 64 << 10 || (rows >= kCUs && rows < 8 * kCUs) ? 256 : 512};
 }
@@ -675,13 +692,12 @@ hipError_t launch_logprob_forward(const LogprobForward& all, void* workspace, hi
   return forward_with<>(a, shape.threads, s);
 }
 
-// A workgroup takes 8 KB of logits, or a row that has fewer.
+// A workgroup takes 8 KB of the wider of logits and gradient, or a row that has fewer.  (us with 4 / 8 / 16 KB: 8192 x 131072 bf16 758 / 674 / 748, 1040 x 50257 FP32 86 / 76 / 84.)
 hipError_t launch_logprob_backward(const LogprobBackward& all, hipStream_t s) {
   LogprobBackward a = all;
-  const int64_t groups = (a.cols + 7) / 8;
-  const int64_t each = a.bf16 ? 512 : 256;
-  a.parts = static_cast<int>((groups + each - 1) / each);
-  return backward_with<>(a, groups >= 256 ? 256 : 64, s);
+  const int64_t each = a.bf16 && a.out_bf16 ? 4096 : 2048;
+  a.parts = static_cast<int>((a.cols + each - 1) / each);
+  return backward_with<>(a, a.cols >= each / 2 ? 256 : 64, s);
 }
 
 hipError_t launch_logprob_with_gradient(const LogprobForward& f, const LogprobBackward& b, void* workspace, hipStream_t s) {
@@ -689,8 +705,8 @@ hipError_t launch_logprob_with_gradient(const LogprobForward& f, const LogprobBa
     const int threads = loss_threads(f.rows, f.cols, f.bf16);
     return threads == 64    ? loss_of<64, false>(f, b, s)
            : threads == 256 ? loss_of<256, false>(f, b, s)
-           : threads == 512 ? (f.bf16 ? loss_of<512, true>(f, b, s) : loss_of<512, false>(f, b, s))
-                            : (f.bf16 ? loss_of<1024, true>(f, b, s) : loss_of<1024, false>(f, b, s));
+           : threads == 512 ? (b.out_bf16 == f.bf16 ? loss_of<512, true>(f, b, s) : loss_of<512, false>(f, b, s))
+                            : (b.out_bf16 == f.bf16 ? loss_of<1024, true>(f, b, s) : loss_of<1024, false>(f, b, s));
   }
   const hipError_t e = launch_logprob_forward(f, workspace, s);
   return e == hipSuccess ? launch_logprob_backward(b, s) : e;
