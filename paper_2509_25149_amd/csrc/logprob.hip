@@ -3,7 +3,8 @@
 //   logprob = scale d_t - ln s;  entropy H = ln s - sum p_j scale d_j
 //   dz_j = scale (g [j = t] + p_j (g_lse - g - g_H (ln p_j + H)))
 // One pass over a row: every thread keeps a running maximum, the sum of exponentials relative to it and (for H) the sum of d exp(d), rescaled when the maximum
-// moves, a batch of 32 values at a time.  All of it FP32.  Masked values may be -infinity (probability 0) or the type's lowest value: the maximum
+// moves, a batch of 32 values at a time.  All of it FP32.  Memory bounds it: 8192 x 131072 bf16 with entropies 360 us, 6.0 TB/s read (some ten operations a value, of which the
+// exponential counts four, are two thirds of what the vector pipe can do in that time); its gradient 675 us, 6.4 TB/s.  Masked values may be -infinity (probability 0) or the type's lowest value: the maximum
 // is kept apart from the logarithm of the sum, so that neither a large maximum nor a row of lowest values loses what the sum says.
 #include <algorithm>
 
@@ -518,20 +519,22 @@ __device__ __forceinline__ void gradient_of_groups(const void* z, void* dz, int 
 
 template <bool kInBf16, bool kOutBf16, bool kEntropy>
 __global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobBackward a) {
-  const uint32_t w = blockIdx.x;
-  const int part = static_cast<int>(w % static_cast<unsigned>(a.parts));
-  const int64_t row = a.row0 + w / static_cast<unsigned>(a.parts);
+  const int part = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.parts));
+  const int64_t row = a.row0 + blockIdx.x / static_cast<unsigned>(a.parts);
   constexpr int kN = kGradientGroup<kInBf16, kOutBf16>;
   const int cols = static_cast<int>(a.cols), groups = (cols + kN - 1) / kN, each = (groups + a.parts - 1) / a.parts;
   const int g0 = min(part * each, groups), g1 = min(g0 + each, groups);
   const RowGradient r(a.stats[2 * row], a.stats[2 * row + 1], a.scale, a.g_logprob ? a.g_logprob[row] : 0.0f, a.g_lse ? a.g_lse[row] : 0.0f,
                       kEntropy ? a.g_entropy[row] : 0.0f, kEntropy ? a.entropy[row] : 0.0f, a.targets ? index_at(a.targets, a.i64, row) : -1, cols);
   gradient_of_groups<kInBf16, kOutBf16, kEntropy, false>(static_cast<const char*>(a.z) + row * a.ld * (kInBf16 ? 2 : 4),
-                                                  static_cast<char*>(a.dz) + row * a.ldd * (kOutBf16 ? 2 : 4), g0, g1, cols, r, a.scale * kLog2E);
+                                                         static_cast<char*>(a.dz) + row * a.ldd * (kOutBf16 ? 2 : 4), g0, g1, cols, r, a.scale * kLog2E);
 }
 
 // Loss and gradient in one launch: a workgroup takes a row, sums over it and goes over it again from its end.  The last groups stay on the CU between the two --
-// half in registers, half in LDS --, those in front are read again, from the L2 or the memory-side cache.
+// half in registers, half in LDS --, those in front are read again, from the L2 or the memory-side cache (8192 x 131072 bf16: by the counters 1.5 times the logits' bytes are
+// fetched; 795 us, 5.4 TB/s of the bytes that have to move; two launches take 1050, without what stays on the CU 925, with one workgroup to a CU that keeps all of a row 875).
+// Tried too: a workgroup that takes one row after the other and fetches the next one into the places that the gradient leaves, each byte once: 820, the two passes of
+// exponentials then stand by themselves.
 constexpr int kKeepBytes = 64;   // of a thread, in either
 
 template <int T, bool kInBf16, bool kOutBf16, bool kStream>
@@ -702,6 +705,8 @@ hipError_t launch_logprob_backward(const LogprobBackward& all, hipStream_t s) {
 
 hipError_t launch_logprob_with_gradient(const LogprobForward& f, const LogprobBackward& b, void* workspace, hipStream_t s) {
   if (forward_shape(f.rows, f.cols, f.bf16, false).parts == 1) {
+    // The gradient passes the caches by where that pays: they are left to the rows that are read again (8192 x 131072 bf16 877 -> 797, 4096 x 131072 FP32 1075 -> 966), but stores of half lines
+    // (FP32 from eight columns of bf16) lose by it (686 -> 980).
     const int threads = loss_threads(f.rows, f.cols, f.bf16);
     return threads == 64    ? loss_of<64, false>(f, b, s)
            : threads == 256 ? loss_of<256, false>(f, b, s)
