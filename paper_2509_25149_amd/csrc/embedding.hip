@@ -408,36 +408,59 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs s) {
   finish(behind == key);
 }
 
-// Rows whose tokens reach over chunks: the chunk in which one begins adds up, in order, what the chunks have left of it.  A wavefront to a chunk and 256 columns.
+// What four wavefronts have of 512 (or 256) columns, in order; the first one gets the sum.
+template <int kN>
+__device__ __forceinline__ void add_wavefronts(float (&sum)[kN], float (*lds)[64][kN]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (wave > 0) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) lds[wave - 1][lane][i] = sum[i];
+  }
+  __syncthreads();
+  if (wave > 0) return;
+  for (int w = 0; w < 3; ++w) {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) sum[i] += lds[w][lane][i];
+  }
+}
+
+// Rows whose tokens reach over chunks: the workgroup of the chunk in which one begins adds up, in order, what the chunks have left of it, over 256 columns and a quarter of the chunks to
+// each wavefront.
 __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs s) {
+  __shared__ float others[3][64][4];
   const EmbeddingBackward& a = s.a;
   const int chunk = static_cast<int>(blockIdx.x), first = chunk * s.chunk, last = first + s.chunk;
   if (last >= s.n) return;
   const uint32_t key = s.keys[last - 1];
   if (key >= static_cast<uint32_t>(a.vocab) || s.keys[last] != key || (first > 0 && s.keys[first - 1] == key)) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int final_chunk = chunk;   // the last one that begins with the key: 64 looked at together
   for (uint64_t more = ~0ull; more == ~0ull; final_chunk += more == ~0ull ? 64 : __builtin_ctzll(~more)) {
-    const int64_t at = static_cast<int64_t>(final_chunk + 1 + (threadIdx.x & 63)) * s.chunk;
+    const int64_t at = static_cast<int64_t>(final_chunk + 1 + lane) * s.chunk;
     more = __ballot(at < s.n && s.keys[at] == key);
   }
-  const int64_t col = static_cast<int64_t>(blockIdx.y) * 1024 + threadIdx.x * 4;
-  if (col >= a.cols) return;
-  const float* from = s.partials + static_cast<int64_t>(chunk) * 2 * a.cols + col;
-  float4v sum = *reinterpret_cast<const float4v*>(from + a.cols);
+  const int64_t col = static_cast<int64_t>(blockIdx.y) * 256 + lane * 4;
+  const int parts = final_chunk - chunk + 1, each = (parts + 3) >> 2, p0 = wave * each, p1 = min(p0 + each, parts);
+  // (The chunk in which the row begins has left its part in the second place, the others in the first.)
+  const float* from = s.partials + static_cast<int64_t>(chunk) * 2 * a.cols + min(col, a.cols - 4);
+  float4v part = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 16
-  for (int c = 1; c <= final_chunk - chunk; ++c) sum += *reinterpret_cast<const float4v*>(from + static_cast<int64_t>(c) * 2 * a.cols);
+  for (int p = p0; p < p1; ++p) part += *reinterpret_cast<const float4v*>(from + (static_cast<int64_t>(p) * 2 + (p == 0 ? 1 : 0)) * a.cols);
+  float sum[4] = {part[0], part[1], part[2], part[3]};
+  add_wavefronts(sum, others);
+  if (wave > 0 || col >= a.cols) return;
   float4v* to = reinterpret_cast<float4v*>(a.dtable + static_cast<int64_t>(key) * a.ldt + col);
-  sum = a.scale * sum;
-  *to = a.accumulate ? *to + sum : sum;
+  const float4v v = a.scale * float4v{sum[0], sum[1], sum[2], sum[3]};
+  *to = a.accumulate ? *to + v : v;
 }
 
 // ---------------------------------------------------------------- few tokens
-// Up to kCountedTokens there is no sorting and, but for a large table's zeros, one launch: a workgroup takes a token and 2048 columns, compares all ids with the token's, and goes on if it is
-// the first one of its id: the others' places are bits in order, and a wavefront adds their rows over its 512 columns.  Tokens that are all the same are added by a few
-// wavefronts one after the other, which is why this ends at 256 of them.  (Ids by Zipf's law, us so / sorted, called from Python: 16 tokens, 700 rows of 256 8.7 / 15.6, 3000 of 5120
-// 14.8 / 17.2; 128 tokens 9.4 / 16.0 and 18 / 18; 512 tokens 17 / 15 and 27 / 20.)
+// Up to kCountedTokens there is no sorting and, but for a large table's zeros, one launch: a workgroup takes a token and 512 columns, compares all ids with the token's, and goes on if it is
+// the first one of its id: the others' places are bits in order, and each wavefront adds a quarter of their rows.  Tokens that are all the same are added by a few
+// workgroups, which is why this ends at 512 of them.  (Ids by Zipf's law, us so / sorted, called from Python: 16 tokens, 700 rows of 256 8.3 / 15.6, 3000 of 5120
+// 13.7 / 17.2; 128 tokens 8.3 / 16.0 and 15.2 / 18; 512 tokens 8.7 / 15.0 and 19 / 20; 512 times the same of 3000 rows of 5120 25 / 21.)
 // The rest of the workgroups, if any, look for rows without a token, 64 each, and write zeros there.
-constexpr int kCountedTokens = 256, kCountedZeroRows = 64;
+constexpr int kCountedTokens = 512, kCountedZeroRows = 64;
 
 template <bool kBf16, int kN>
 __device__ __forceinline__ void add_listed(const EmbeddingBackward& a, const uint16_t* list, int n, int64_t col, float (&sum)[8]) {
@@ -460,18 +483,24 @@ template <bool kBf16>
 __global__ __launch_bounds__(256) void embedding_few_kernel(EmbeddingBackward a, int n, uint32_t across, uint32_t zero_groups) {
   __shared__ uint64_t same[kCountedTokens / 64];
   __shared__ uint16_t list[kCountedTokens];
+  __shared__ float others[3][64][8];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint32_t sums = static_cast<uint32_t>(n) * across;
-  uint32_t key[1] = {kNoKey};
-  if (n > 0) keys_of(a.ids, a.i64, static_cast<int>(threadIdx.x), 1, n, a.vocab, key);
+  uint32_t key[kCountedTokens / 256];
+#pragma unroll
+  for (int u = 0; u < kCountedTokens / 256; ++u) key[u] = kNoKey;
+  if (n > 0) keys_of(a.ids, a.i64, static_cast<int>(threadIdx.x), 256, n, a.vocab, key);
   if (blockIdx.x >= sums) {
     uint32_t* present = reinterpret_cast<uint32_t*>(same);
     for (int64_t row0 = static_cast<int64_t>(blockIdx.x - sums) * kCountedZeroRows; row0 < a.vocab; row0 += static_cast<int64_t>(zero_groups) * kCountedZeroRows) {
       __syncthreads();
       if (threadIdx.x < 2) present[threadIdx.x] = 0u;
       __syncthreads();
-      const uint32_t r = key[0] - static_cast<uint32_t>(row0);
-      if (r < kCountedZeroRows) atomicOr(&present[r >> 5], 1u << (r & 31));
+#pragma unroll
+      for (int u = 0; u < kCountedTokens / 256; ++u) {
+        const uint32_t r = key[u] - static_cast<uint32_t>(row0);
+        if (r < kCountedZeroRows) atomicOr(&present[r >> 5], 1u << (r & 31));
+      }
       __syncthreads();
       const int64_t left = a.vocab - row0;
       const uint64_t there = left < 64 ? (uint64_t{1} << left) - 1 : ~uint64_t{0};
@@ -486,8 +515,11 @@ __global__ __launch_bounds__(256) void embedding_few_kernel(EmbeddingBackward a,
   uint32_t mine[1];
   keys_of(a.ids, a.i64, t, 1, n, a.vocab, mine);
   if (mine[0] >= static_cast<uint32_t>(a.vocab)) return;
-  const uint64_t mask = __ballot(key[0] == mine[0]);
-  if (lane == 0) same[wave] = mask;
+#pragma unroll
+  for (int u = 0; u < kCountedTokens / 256; ++u) {
+    const uint64_t mask = __ballot(key[u] == mine[0]);
+    if (lane == 0) same[u * 4 + wave] = mask;   // tokens 256 u + 64 wave on
+  }
   __syncthreads();
   uint64_t m = lane < kCountedTokens / 64 ? same[lane] : 0ull;
   const int word = t >> 6;
@@ -500,9 +532,10 @@ __global__ __launch_bounds__(256) void embedding_few_kernel(EmbeddingBackward a,
   }
   total = __builtin_amdgcn_readlane(before, kCountedTokens / 64 - 1);
   before -= __popcll(m);
-  const int64_t col = static_cast<int64_t>(blockIdx.x % across) * 2048 + threadIdx.x * 8, from = min(col, a.cols - 8);
+  const int64_t col = static_cast<int64_t>(blockIdx.x % across) * 512 + lane * 8, from = min(col, a.cols - 8);
   float sum[8] = {};
   if (total == 1) {
+    if (wave > 0) return;
     Eight<kBf16> x;
     x.load(static_cast<const char*>(a.dout) + static_cast<int64_t>(t) * a.ldd * (kBf16 ? 2 : 4), from);
     x.get(sum);
@@ -510,10 +543,12 @@ __global__ __launch_bounds__(256) void embedding_few_kernel(EmbeddingBackward a,
     if (wave == 0)
       for (; m; m &= m - 1) list[before++] = static_cast<uint16_t>(lane * 64 + __builtin_ctzll(m));
     __syncthreads();
-    if (total <= 8) add_listed<kBf16, 8>(a, list, total, from, sum);
-    else add_listed<kBf16, 16>(a, list, total, from, sum);
+    const int each = (total + 3) >> 2, first = wave * each, count = min(each, total - first);
+    if (each <= 4) add_listed<kBf16, 4>(a, list + first, count, from, sum);
+    else add_listed<kBf16, 16>(a, list + first, count, from, sum);
+    add_wavefronts(sum, others);
   }
-  if (col >= a.cols) return;
+  if (wave > 0 || col >= a.cols) return;
   float* row = a.dtable + static_cast<int64_t>(mine[0]) * a.ldt;
 #pragma unroll
   for (int i = 0; i < 8; ++i) sum[i] *= a.scale;
@@ -600,7 +635,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackward& a, void* workspace
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (few) {
-    const uint32_t across = static_cast<uint32_t>((a.cols + 2047) / 2048);
+    const uint32_t across = static_cast<uint32_t>((a.cols + 511) / 512);
     const uint32_t zeros = a.accumulate || zero_first ? 0u : static_cast<uint32_t>(std::min<int64_t>((a.vocab + kCountedZeroRows - 1) / kCountedZeroRows, 1 << 16));
     if (n * across + zeros == 0) return hipSuccess;
     if (a.bf16) hipLaunchKernelGGL(embedding_few_kernel<true>, dim3(n * across + zeros), dim3(256), 0, s, a, n, across, zeros);
@@ -639,7 +674,7 @@ hipError_t launch_embedding_backward(const EmbeddingBackward& a, void* workspace
   if (a.bf16) hipLaunchKernelGGL(embedding_sum_kernel<true>, dim3(static_cast<unsigned>(wgs)), dim3(256), 0, s, u);
   else hipLaunchKernelGGL(embedding_sum_kernel<false>, dim3(static_cast<unsigned>(wgs)), dim3(256), 0, s, u);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (u.chunks > 1) hipLaunchKernelGGL(embedding_join_kernel, dim3(u.chunks, static_cast<unsigned>((a.cols + 1023) / 1024)), dim3(256), 0, s, u);
+  if (u.chunks > 1) hipLaunchKernelGGL(embedding_join_kernel, dim3(u.chunks, static_cast<unsigned>((a.cols + 255) / 256)), dim3(256), 0, s, u);
   return hipGetLastError();
 }
 

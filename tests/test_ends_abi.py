@@ -50,7 +50,7 @@ def test_embedding_refuses(lib):
     assert bwd(ws=None) == -6 and bwd(size=need - 1) == -6 and bwd(ws=P + 8) == -6
     w = ctypes.c_size_t()
     assert lib.nvfp4_embedding_workspace_bytes(32, 100, 24, ctypes.addressof(w)) == -2 and lib.nvfp4_embedding_workspace_bytes(32, 100, 64, None) == -1
-    assert nv.embedding_workspace_bytes(0, 100, 64) == 0 and nv.embedding_workspace_bytes(256, 100, 64) == 0 and nv.embedding_workspace_bytes(257, 100, 64) >= 2 * 257 * 4
+    assert nv.embedding_workspace_bytes(0, 100, 64) == 0 and nv.embedding_workspace_bytes(512, 100, 64) == 0 and nv.embedding_workspace_bytes(513, 100, 64) >= 2 * 513 * 4
 
 
 def test_logprob_refuses(lib):
