@@ -490,7 +490,7 @@ int nvfp4_logprob_backward(const void* logits, int dtype, int64_t ld, int64_t ro
 
 /*
  * Both for a loss whose gradient by the log probabilities is known beforehand (a mean over tokens): the same results as nvfp4_logprob_forward and
- * nvfp4_logprob_backward with g_logprob, with the logits read from memory once where they allow it.  stats must not be NULL; workspace: nvfp4_logprob_workspace_bytes with top = 0.
+ * nvfp4_logprob_backward with g_logprob, with the logits read from memory once where they allow it.  logprob, stats and lse may be NULL; workspace: nvfp4_logprob_workspace_bytes with top = 0.
  */
 int nvfp4_logprob_with_gradient(const void* logits, int dtype, int64_t ld, int64_t rows, int64_t cols, float scale, const void* targets, int index_type,
                                 const float* g_logprob, float* logprob, float* stats, float* lse, void* dlogits, int d_dtype, int64_t ldd, void* workspace,

@@ -754,7 +754,7 @@ def nvfp4_embedding_backward(dout: torch.Tensor, ids: torch.Tensor, vocab: Optio
 class LogProbs(NamedTuple):
     logprob: Optional[torch.Tensor]       # of the targets, float32 [rows]
     lse: torch.Tensor                     # float32 [rows]
-    stats: torch.Tensor                   # float32 [rows, 2], for nvfp4_logprob_backward
+    stats: Optional[torch.Tensor] = None          # float32 [rows, 2], for nvfp4_logprob_backward
     entropy: Optional[torch.Tensor] = None
     top_index: Optional[torch.Tensor] = None      # int32 [rows, top]
     top_logprob: Optional[torch.Tensor] = None    # float32 [rows, top]
@@ -769,8 +769,8 @@ def logprob_workspace_bytes(rows: int, cols: int, top: int = 0) -> int:
 
 
 def nvfp4_logprob_forward(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, scale: float = 1.0, entropy: bool = False, top: int = 0,
-                          workspace: Optional[torch.Tensor] = None) -> LogProbs:
-    """ln softmax(scale * logits) at the targets (0 where a target is outside the row), with what else is asked for: see LogProbs."""
+                          for_backward: bool = False, workspace: Optional[torch.Tensor] = None) -> LogProbs:
+    """ln softmax(scale * logits) at the targets (0 where a target is outside the row), with what else is asked for: see LogProbs.  for_backward: stats too."""
     _here(logits, targets)
     dt, zp, ld = _matrix(logits, "logits")
     (rows, cols), device = logits.shape, logits.device
@@ -778,19 +778,22 @@ def nvfp4_logprob_forward(logits: torch.Tensor, targets: Optional[torch.Tensor] 
         ld = -(-cols // 8) * 8      # (a row alone may be of any length)
     kind, tp = (INDEX_I64, None) if targets is None else _indices(targets, rows, "targets")
     ws, ws_bytes, workspace = _scratch(workspace, logprob_workspace_bytes(rows, cols, top), device)
-    f32, lp, hp, ip, vp = torch.float32, None, None, None, None
-    logprob = h = index = values = None
+    f32, lp, sp, hp, ip, vp = torch.float32, None, None, None, None, None
+    logprob = stats = h = index = values = None
     if targets is not None:
         logprob = torch.empty(rows, dtype=f32, device=device)
         lp = logprob.data_ptr()
-    lse, stats = torch.empty(rows, dtype=f32, device=device), torch.empty(rows, 2, dtype=f32, device=device)
+    lse = torch.empty(rows, dtype=f32, device=device)
+    if for_backward:
+        stats = torch.empty(rows, 2, dtype=f32, device=device)
+        sp = stats.data_ptr()
     if entropy:
         h = torch.empty(rows, dtype=f32, device=device)
         hp = h.data_ptr()
     if top:
         index, values = torch.empty(rows, top, dtype=torch.int32, device=device), torch.empty(rows, top, dtype=f32, device=device)
         ip, vp = index.data_ptr(), values.data_ptr()
-    _check(load_library().nvfp4_logprob_forward(zp, dt, ld, rows, cols, scale, tp, kind, lp, stats.data_ptr(), lse.data_ptr(), hp, top, ip, vp, ws, ws_bytes, _stream()))
+    _check(load_library().nvfp4_logprob_forward(zp, dt, ld, rows, cols, scale, tp, kind, lp, sp, lse.data_ptr(), hp, top, ip, vp, ws, ws_bytes, _stream()))
     return LogProbs(logprob, lse, stats, h, index, values)
 
 
@@ -837,11 +840,10 @@ def nvfp4_logprob_with_gradient(logits: torch.Tensor, targets: torch.Tensor, g_l
     gp = _vector(g_logprob, rows, "g_logprob")
     out, ot, op, ldd = _dlogits(logits, dt, out_dtype, out)
     ws, ws_bytes, workspace = _scratch(workspace, logprob_workspace_bytes(rows, cols), device)
-    logprob, lse = torch.empty(rows, dtype=torch.float32, device=device), torch.empty(rows, dtype=torch.float32, device=device)
-    stats = torch.empty(rows, 2, dtype=torch.float32, device=device)
-    _check(load_library().nvfp4_logprob_with_gradient(zp, dt, ld, rows, cols, scale, tp, kind, gp, logprob.data_ptr(), stats.data_ptr(), lse.data_ptr(), op, ot, ldd,
-                                                      ws, ws_bytes, _stream()))
-    return LogProbs(logprob, lse, stats, dlogits=out)
+    logprob, lse = torch.empty_like(g_logprob), torch.empty_like(g_logprob)
+    _check(load_library().nvfp4_logprob_with_gradient(zp, dt, ld, rows, cols, scale, tp, kind, gp, logprob.data_ptr(), None, lse.data_ptr(), op, ot, ldd, ws, ws_bytes,
+                                                      _stream()))
+    return LogProbs(logprob, lse, dlogits=out)
 
 
 class Gradients:

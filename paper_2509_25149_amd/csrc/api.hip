@@ -894,7 +894,7 @@ int nvfp4_logprob_with_gradient(const void* logits, int dtype, int64_t ld, int64
   if (rc != NVFP4_OK) return rc;
   rc = check_dlogits(logits, dtype, ld, rows, cols, dlogits, d_dtype, ldd);
   if (rc != NVFP4_OK) return rc;
-  if (rows && (!targets || !g_logprob || !stats)) return NVFP4_ERR_INVALID_ARG;
+  if (rows && (!targets || !g_logprob)) return NVFP4_ERR_INVALID_ARG;
   if (!aligned(g_logprob, 4) || !aligned(logprob, 4) || !aligned(stats, 4) || !aligned(lse, 4)) return NVFP4_ERR_INVALID_ARG;
   rc = check_workspace(workspace, workspace_bytes, logprob_workspace_bytes(rows, cols, 0));
   if (rc != NVFP4_OK) return rc;

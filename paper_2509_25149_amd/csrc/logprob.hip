@@ -683,7 +683,8 @@ hipError_t loss_of(const LogprobForward& f, const LogprobBackward& b, hipStream_
 
 size_t logprob_workspace_bytes(int64_t rows, int64_t cols, int top) {
   const int parts = forward_shape(rows, cols, true, false).parts;
-  return parts == 1 ? 0 : static_cast<size_t>(rows) * static_cast<size_t>(parts) * (16 + 8 * static_cast<size_t>(top));
+  // The pieces' sums, their best, and room for the statistics between the two passes of nvfp4_logprob_with_gradient.
+  return parts == 1 ? 0 : static_cast<size_t>(rows) * (static_cast<size_t>(parts) * (16 + 8 * static_cast<size_t>(top)) + 8);
 }
 
 hipError_t launch_logprob_forward(const LogprobForward& all, void* workspace, hipStream_t s) {
@@ -713,8 +714,11 @@ hipError_t launch_logprob_with_gradient(const LogprobForward& f, const LogprobBa
            : threads == 512 ? (b.out_bf16 == f.bf16 ? loss_of<512, true>(f, b, s) : loss_of<512, false>(f, b, s))
                             : (b.out_bf16 == f.bf16 ? loss_of<1024, true>(f, b, s) : loss_of<1024, false>(f, b, s));
   }
-  const hipError_t e = launch_logprob_forward(f, workspace, s);
-  return e == hipSuccess ? launch_logprob_backward(b, s) : e;
+  LogprobForward forward = f;
+  LogprobBackward backward = b;
+  if (!f.stats) backward.stats = forward.stats = static_cast<float*>(workspace) + f.rows * forward_shape(f.rows, f.cols, f.bf16, false).parts * 4;
+  const hipError_t e = launch_logprob_forward(forward, workspace, s);
+  return e == hipSuccess ? launch_logprob_backward(backward, s) : e;
 }
 
 }  // namespace nvfp4

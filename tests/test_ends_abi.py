@@ -80,7 +80,7 @@ def test_logprob_refuses(lib):
 
     def both(z=P, dt=1, ld=104, rows=4, cols=100, scale=1.0, t=P, it=1, g=P, lp=P, st=P, lse=P, dz=2 * P, ot=1, ldd=104, ws=None, size=0):
         return lib.nvfp4_logprob_with_gradient(z, dt, ld, rows, cols, scale, t, it, g, lp, st, lse, dz, ot, ldd, ws, size, None)
-    assert both(dz=P, ot=0) == -1 and both(dz=P, ldd=112) == -1 and both(z=None) == -1 and both(t=None) == -1 and both(g=None) == -1 and both(st=None) == -1 and both(dz=None) == -1 and both(ot=3) == -1 and both(lse=P + 2) == -1
+    assert both(dz=P, ot=0) == -1 and both(dz=P, ldd=112) == -1 and both(z=None) == -1 and both(t=None) == -1 and both(g=None) == -1 and both(st=P + 2) == -1 and both(dz=None) == -1 and both(ot=3) == -1 and both(lse=P + 2) == -1
     assert both(ldd=96) == -2 and both(rows=-1) == -2 and both(rows=1, cols=131072, ld=131072, ldd=131072) == -6
 
 

@@ -67,7 +67,7 @@ class LogProb:
         self.z, self.t = logits_of(rows, cols, seed)
 
     def run(self):
-        r = nv.nvfp4_logprob_forward(self.z, self.t, entropy=True, top=5)
+        r = nv.nvfp4_logprob_forward(self.z, self.t, entropy=True, top=5, for_backward=True)
         g = torch.full_like(r.logprob, -0.25)
         return [r.logprob, r.lse, r.entropy, r.top_index, r.top_logprob, nv.nvfp4_logprob_backward(self.z, self.t, r.stats, g_logprob=g, g_entropy=g, entropy=r.entropy),
                 nv.nvfp4_logprob_with_gradient(self.z, self.t, g).dlogits]

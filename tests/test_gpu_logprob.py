@@ -42,8 +42,9 @@ def check_forward(out, z, scale, targets, top, entropy):
     m, logsum, p, logp, h = em.logits_statistics(z64, scale)
     rel = em.sum_error(z64, scale)[0]
     rows, cols = z64.shape
-    bm.within(out.stats[:, 0], m, np.zeros(rows))
-    bm.within(out.stats[:, 1], logsum, rel + 2 * em.U * np.abs(logsum) + em.U)
+    if out.stats is not None:
+        bm.within(out.stats[:, 0], m, np.zeros(rows))
+        bm.within(out.stats[:, 1], logsum, rel + 2 * em.U * np.abs(logsum) + em.U)
     lse = scale * m + logsum
     bm.within(out.lse, lse, rel + em.U * (2 * np.abs(scale * m) + 3 * np.abs(logsum) + 2 * np.abs(lse)) + em.U)
     at = lambda col: (logp[np.arange(rows)[:, None], col], rel[:, None] + em.U * (4 * np.abs(logp + logsum[:, None]) + 4 * np.abs(logsum)[:, None] + 2 * np.abs(logp))[
@@ -72,10 +73,10 @@ def check_forward(out, z, scale, targets, top, entropy):
 def test_forward(rows, cols, dt, it, scale, entropy, top, kind):
     z = logits(rows, cols, rows + cols, dt, 8, kind)
     t, top = targets_of(rows, cols, 1), min(top, cols)
-    out = nv.nvfp4_logprob_forward(z, em.index(t, it), scale=scale, entropy=entropy, top=top)
+    out = nv.nvfp4_logprob_forward(z, em.index(t, it), scale=scale, entropy=entropy, top=top, for_backward=True)
     check_forward(out, z, scale, t, top, entropy)
     again = nv.nvfp4_logprob_forward(z, None, scale=scale, entropy=entropy, top=top)
-    assert again.logprob is None and all(torch.equal(a, b) for a, b in zip(out[1:6], again[1:6]) if a is not None)
+    assert again.logprob is None and again.stats is None and all(torch.equal(getattr(out, f), getattr(again, f)) for f in ("lse", "entropy", "top_index", "top_logprob") if getattr(out, f) is not None)
 
 
 def check_gradient(dz, z, scale, targets, g, g_lse, g_entropy, dtype):
@@ -92,7 +93,7 @@ def test_backward(rows, cols, dt, ot, it, scale, which, kind):
     z = logits(rows, cols, rows * 7 + cols, dt, 8, kind)
     t = targets_of(rows, cols, 2)
     g, gl, ge = (torch.as_tensor(r.standard_normal(rows).astype(np.float32)).cuda() if c in which else None for c in "gle")
-    fwd = nv.nvfp4_logprob_forward(z, em.index(t, it), scale=scale, entropy=True)
+    fwd = nv.nvfp4_logprob_forward(z, em.index(t, it), scale=scale, entropy=True, for_backward=True)
     args = dict(g_logprob=g, g_lse=gl, g_entropy=ge, entropy=fwd.entropy if ge is not None else None, scale=scale)
     tt = em.index(t, it) if g is not None else None
     dz = nv.nvfp4_logprob_backward(z, tt, fwd.stats, out_dtype=OUT[ot], **args)
@@ -137,7 +138,7 @@ def test_rows_that_masks_leave_nothing_of(rows, cols, dt):
     z[4, 1::2] = lowest
     t = np.full(rows, 5)
     t[2] = cols - 1
-    out = nv.nvfp4_logprob_forward(z, em.index(t, I64), entropy=True, top=3)
+    out = nv.nvfp4_logprob_forward(z, em.index(t, I64), entropy=True, top=3, for_backward=True)
     lp, h, idx, tl = bm.f64(out.logprob), bm.f64(out.entropy), out.top_index.cpu().numpy(), bm.f64(out.top_logprob)
     assert np.isneginf(lp[0]) and np.isneginf(bm.f64(out.lse)[0]) and h[0] == 0 and list(idx[0]) == [0, 1, 2] and np.all(np.isneginf(tl[0]))
     assert abs(lp[1] + np.log(cols)) <= 1e-5 and abs(h[1] - np.log(cols)) <= 1e-5 and list(idx[1]) == [0, 1, 2] and np.all(np.abs(tl[1] + np.log(cols)) <= 1e-5)
@@ -160,7 +161,7 @@ def test_trouble_shows_in_its_row_and_nowhere_else(rows, cols):
     clean = nv.nvfp4_logprob_forward(z, None, entropy=True, top=2)
     z[1, 7], z[2, cols - 1] = torch.nan, torch.inf
     t = torch.zeros(rows, dtype=I64, device="cuda")
-    out = nv.nvfp4_logprob_forward(z, t, entropy=True, top=2)
+    out = nv.nvfp4_logprob_forward(z, t, entropy=True, top=2, for_backward=True)
     for v in (out.logprob, out.lse, out.entropy):
         assert bool(torch.isnan(v[1:3]).all()) and bool(torch.isfinite(v[0]).all()) and bool(torch.isfinite(v[3:]).all())
     assert int(out.top_index[2, 0]) == cols - 1 and 7 not in out.top_index[1].tolist() and torch.equal(out.top_index[3:], clean.top_index[3:])
@@ -194,7 +195,7 @@ def test_gradients_agree_with_differences():
         m, logsum, p, logp, h = em.logits_statistics(z, scale)
         return (w[0] * logp[np.arange(rows), t] + w[1] * (scale * m + logsum) + w[2] * h).sum()
     x = bm.tensor(z, F32, pad_of(cols))
-    fwd = nv.nvfp4_logprob_forward(x, em.index(t, I64), scale=scale, entropy=True)
+    fwd = nv.nvfp4_logprob_forward(x, em.index(t, I64), scale=scale, entropy=True, for_backward=True)
     g = [torch.as_tensor(v).cuda() for v in w]
     dz = bm.f64(nv.nvfp4_logprob_backward(x, em.index(t, I64), fwd.stats, g_logprob=g[0], g_lse=g[1], g_entropy=g[2], entropy=fwd.entropy, scale=scale))
     for _ in range(4):
@@ -229,7 +230,7 @@ def test_offsets_beyond_2_to_the_31():
     z = torch.zeros(rows, cols, device="cuda", dtype=BF16)
     z[-1, -1] = 20.0
     t = torch.full((rows,), cols - 1, dtype=I64, device="cuda")
-    out = nv.nvfp4_logprob_forward(z, t, entropy=True)
+    out = nv.nvfp4_logprob_forward(z, t, entropy=True, for_backward=True)
     s = np.exp(20.0) + cols - 1
     assert abs(float(out.logprob[-1]) - (20 - np.log(s))) <= 1e-5 and abs(float(out.logprob[0]) + np.log(cols)) <= 1e-5
     dz = nv.nvfp4_logprob_backward(z, t, out.stats, g_logprob=torch.ones(rows, device="cuda"), out=z)
