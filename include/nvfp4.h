@@ -460,7 +460,7 @@ int nvfp4_embedding_backward(const void* dout, int dtype, int64_t ldd, const voi
 
 /*
  * Log probabilities, with p = softmax(scale * logits) over each row:
- *   logits       [rows, cols] of type dtype;  scale  > 0 and finite: the reciprocal of a temperature
+ *   logits       [rows, cols] of type dtype;  scale  > 0 and at most 2^127: the reciprocal of a temperature
  *   targets      token numbers [rows], or NULL
  *   logprob      FP32 [rows]: ln p[target], 0 where the target is outside [0, cols); or NULL
  *   stats        FP32 [rows, 2]: the row's largest logit m, and ln sum exp(scale (logit - m)), for nvfp4_logprob_backward; or NULL.  They are kept apart because their

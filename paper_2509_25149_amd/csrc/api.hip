@@ -707,7 +707,8 @@ int check_embedding(int64_t tokens, int64_t vocab, int64_t cols) {
 bool logits_shape(int64_t rows, int64_t cols) { return rows >= 0 && rows <= 0x7fffffff && cols > 0 && cols < 0x40000000; }
 
 int check_logits(const void* logits, int dtype, int64_t ld, int64_t rows, int64_t cols, float scale, const void* targets, int index_type) {
-  if (!element_type(dtype) || !index_kind(index_type) || !is_finite(scale) || !(scale > 0.0f)) return NVFP4_ERR_INVALID_ARG;
+  // (2^127 at most: exponents are taken to base 2, and the scale's 1.44 times stay finite)
+  if (!element_type(dtype) || !index_kind(index_type) || !(scale > 0.0f && scale <= 0x1p127f)) return NVFP4_ERR_INVALID_ARG;
   if (!logits_shape(rows, cols)) return NVFP4_ERR_BAD_SHAPE;
   const int rc = check_tensor(logits, rows, cols, ld, false);
   return rc == NVFP4_OK ? check_index(targets, index_type, rows, true) : rc;

@@ -95,6 +95,16 @@ def build(lib, grads, room=1 << 22, host=True):
     return rc, buf, lst
 
 
+def test_logprob_refuses_a_scale_whose_base_2_form_overflows(lib):
+    """The kernels work with scale * log2(e): infinite, it would make a NaN of the largest logit's distance 0.  No rows: nothing is read, whatever the answer."""
+    most = 2.0 ** 127
+    for scale, rc in ((3.4e38, -1), (2.4e38, -1), (float(np.nextafter(np.float32(most), np.float32(np.inf))), -1), (most, 0), (1e-45, 0)):
+        logits = (None, 1, 104, 0, 100, scale, None, 1)
+        assert lib.nvfp4_logprob_forward(*logits, None, None, None, None, 0, None, None, None, 0, None) == rc
+        assert lib.nvfp4_logprob_backward(*logits, None, None, None, None, None, None, 1, 104, None) == rc
+        assert lib.nvfp4_logprob_with_gradient(*logits, None, None, None, None, None, 1, 104, None, 0, None) == rc
+
+
 def test_the_list_of_gradients_refuses(lib):
     size = lambda *g: lib.nvfp4_grad_list_sizes((nv.GradStruct * len(g))(*g), len(g), None, None)
     assert size(grad()) == 0 and lib.nvfp4_grad_list_sizes(None, 1, None, None) == -1 and lib.nvfp4_grad_list_sizes(None, -1, None, None) == -1
