@@ -726,6 +726,8 @@ def _scratch(workspace: Optional[torch.Tensor], need: int, device):
     if workspace is None:
         return _workspace(device, need) if need else (None, 0, None)
     _here(workspace)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 

@@ -166,3 +166,13 @@ def test_the_binding_refuses():
                  lambda: nv.nvfp4_logprob_backward(x, i, x), lambda: nv.nvfp4_logprob_with_gradient(x, i, torch.zeros(4)), lambda: nv.Gradients([x])):
         with pytest.raises((ValueError, RuntimeError, AssertionError)):
             call()
+
+
+def test_a_workspace_that_is_no_plain_memory_is_refused(monkeypatch):
+    """An expanded view says more elements than it has memory for."""
+    monkeypatch.setattr(nv, "_here", lambda *tensors: None)
+    whole = torch.empty(64, dtype=torch.float32)
+    assert nv._scratch(whole, 256, whole.device)[:2] == (whole.data_ptr(), 256)
+    for bad in (torch.empty(1).expand(64), torch.empty(1, 8).expand(8, 8), whole[::2]):
+        with pytest.raises(ValueError):
+            nv._scratch(bad, 64, bad.device)
