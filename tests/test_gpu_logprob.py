@@ -10,7 +10,7 @@ from paper_2509_25149_amd import binding as nv
 pytestmark = pytest.mark.gpu
 F32, BF16, I32, I64 = torch.float32, torch.bfloat16, torch.int32, torch.int64
 OUT = {F32: nv.OUT_F32, BF16: nv.OUT_BF16}
-# one column and fewer than eight; whole and broken groups of eight; a wavefront, 256 and 512 threads to a row; pieces of a row (few rows, more than 4096 columns)
+# one column and fewer than eight; whole and broken groups of eight; a wavefront, 256 and 512 threads to a row; pieces of a row (one row of 65536 columns and more)
 SHAPES = [(1, 1), (2, 7), (3, 8), (5, 9), (4, 100), (3, 513), (9, 4096), (2, 4100), (1, 5000), (3, 50257), (1, 131072), (300, 5001), (515, 4097), (513, 20003), (1, 262147)]
 
 
