@@ -69,7 +69,18 @@ __device__ __forceinline__ void put_group(void* row, int g, const float (&v)[4])
 }
 
 // ---------------------------------------------------------------- sums of exponentials relative to a maximum
-// s = sum 2^((z - m) c);  e = sum (z - m) c 2^((z - m) c), c = scale log2(e).  Nothing but -infinity: m = kLowest, s = 0.
+// scale (z - m), to base e and to base 2.  Two logits may be further apart than FP32's largest number while a small scale makes the distance an ordinary one: with a scale below 1 half of
+// the distance is formed, and taken twice as often.  Halves lose nothing (but 2^-150 where a distance is below FP32's normal numbers), and the fused product costs what the difference does:
+// one operation.  At a scale of 1 and more a distance beyond FP32 is one after scaling too.
+struct Exponent {
+  float h, by, c;
+  __device__ __forceinline__ explicit Exponent(float scale) : h(scale < 1.0f ? 0.5f : 1.0f), by(scale < 1.0f ? 2.0f * scale : scale), c(by * kLog2E) {}
+  __device__ __forceinline__ float half(float z) const { return z * h; }   // (or the whole)
+  __device__ __forceinline__ float base2(float z, float half_m) const { return __builtin_fmaf(z, h, -half_m) * c; }
+  __device__ __forceinline__ float base_e(float z, float half_m) const { return __builtin_fmaf(z, h, -half_m) * by; }
+};
+
+// s = sum 2^t, e = sum t 2^t, t = scale (z - m) to base 2.  Nothing but -infinity: m = kLowest, s = 0.
 // A NaN or +infinity makes s NaN, and s stays so.
 struct Sum {
   float m, s, e;
@@ -78,15 +89,15 @@ struct Sum {
 __device__ __forceinline__ float far_at_most(float t) { return __builtin_fmaxf(t, kFar); }
 
 template <bool kEntropy>
-__device__ __forceinline__ void move_to(Sum& a, float m, float c) {
-  const float t = far_at_most((a.m - m) * c), f = __builtin_amdgcn_exp2f(t);
+__device__ __forceinline__ void move_to(Sum& a, float m, const Exponent& c) {
+  const float t = far_at_most(c.base2(a.m, c.half(m))), f = __builtin_amdgcn_exp2f(t);
   if (kEntropy) a.e = (a.e + a.s * t) * f;
   a.s *= f;
   a.m = m;
 }
 
 template <bool kEntropy>
-__device__ __forceinline__ void join(Sum& a, Sum b, float c) {
+__device__ __forceinline__ void join(Sum& a, Sum b, const Exponent& c) {
   const float m = __builtin_fmaxf(a.m, b.m);
   move_to<kEntropy>(a, m, c);
   move_to<kEntropy>(b, m, c);
@@ -95,15 +106,16 @@ __device__ __forceinline__ void join(Sum& a, Sum b, float c) {
 }
 
 template <bool kEntropy, int kN>
-__device__ __forceinline__ void add(Sum& a, const float (&v)[kN], float c) {
+__device__ __forceinline__ void add(Sum& a, const float (&v)[kN], const Exponent& c) {
   float m = v[0];
 #pragma unroll
   for (int i = 1; i < kN; ++i) m = __builtin_fmaxf(m, v[i]);
   move_to<kEntropy>(a, __builtin_fmaxf(a.m, m), c);
+  const float half_m = c.half(a.m);
   float s[4] = {}, e[4] = {};   // four chains: shorter ones lose less
 #pragma unroll
   for (int i = 0; i < kN; ++i) {
-    const float t = (v[i] - a.m) * c, p = __builtin_amdgcn_exp2f(t);
+    const float t = c.base2(v[i], half_m), p = __builtin_amdgcn_exp2f(t);
     s[i & 3] += p;
     if (kEntropy) e[i & 3] = __builtin_fmaf(p, far_at_most(t), e[i & 3]);
   }
@@ -112,7 +124,7 @@ __device__ __forceinline__ void add(Sum& a, const float (&v)[kN], float c) {
 }
 
 template <bool kEntropy>
-__device__ __forceinline__ Sum wave_join(Sum a, float c) {
+__device__ __forceinline__ Sum wave_join(Sum a, const Exponent& c) {
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) {
     Sum b;
@@ -126,7 +138,7 @@ __device__ __forceinline__ Sum wave_join(Sum a, float c) {
 
 // Of a workgroup's threads, the same in all of them.
 template <bool kEntropy>
-__device__ __forceinline__ Sum workgroup_join(Sum a, float c, Sum* lds) {
+__device__ __forceinline__ Sum workgroup_join(Sum a, const Exponent& c, Sum* lds) {
   a = wave_join<kEntropy>(a, c);
   const int waves = blockDim.x >> 6;
   if (waves == 1) return a;
@@ -162,7 +174,7 @@ __device__ __forceinline__ void group_of(const void* row, int g, int cols, float
 }
 
 template <bool kEntropy, bool kBf16, int kN, int kGroups>
-__device__ __forceinline__ void add_groups(Sum& a, const Group<kBf16, kN> (&x)[kGroups], float c) {
+__device__ __forceinline__ void add_groups(Sum& a, const Group<kBf16, kN> (&x)[kGroups], const Exponent& c) {
   float v[kGroups * kN];
 #pragma unroll
   for (int u = 0; u < kGroups; ++u) {
@@ -176,7 +188,7 @@ __device__ __forceinline__ void add_groups(Sum& a, const Group<kBf16, kN> (&x)[k
 
 // A thread's share of groups [g0, g1), 32 columns at a time.
 template <bool kBf16, bool kEntropy, int kN>
-__device__ __forceinline__ Sum sum_of_groups(const void* row, int g0, int g1, int cols, float c) {
+__device__ __forceinline__ Sum sum_of_groups(const void* row, int g0, int g1, int cols, const Exponent& c) {
   constexpr int kBatch = 32 / kN;
   const int step = blockDim.x, whole = min(g1, cols / kN);
   Sum a{kLowest, 0.0f, 0.0f};
@@ -199,15 +211,15 @@ __device__ __forceinline__ Sum sum_of_groups(const void* row, int g0, int g1, in
 struct RowStats {
   float m, logsum;
   __device__ __forceinline__ explicit RowStats(const Sum& a) : m(a.s == 0.0f ? 0.0f : a.m), logsum(a.s == 0.0f ? kInfinity : logf(a.s)) {}
-  __device__ __forceinline__ float logprob(float z, float scale) const { return (z - m) * scale - logsum; }
+  __device__ __forceinline__ float logprob(float z, const Exponent& c) const { return c.base_e(z, c.half(m)) - logsum; }
 };
 
-__device__ __forceinline__ void write_row(const LogprobForward& a, int64_t row, const Sum& sum, const RowStats& r, float at_target, bool counted) {
+__device__ __forceinline__ void write_row(const LogprobForward& a, int64_t row, const Sum& sum, const RowStats& r, const Exponent& c, float at_target, bool counted) {
   const bool empty = sum.s == 0.0f;
   if (a.stats) a.stats[2 * row] = r.m, a.stats[2 * row + 1] = r.logsum;
   if (a.lse) a.lse[row] = empty ? -kInfinity : r.m * a.scale + r.logsum;
   if (a.entropy) a.entropy[row] = empty ? 0.0f : r.logsum - kLn2 * (sum.e / sum.s);
-  if (a.logprob) a.logprob[row] = counted ? r.logprob(at_target, a.scale) : 0.0f;
+  if (a.logprob) a.logprob[row] = counted ? r.logprob(at_target, c) : 0.0f;
 }
 
 // ---------------------------------------------------------------- best alternatives
@@ -340,9 +352,9 @@ __device__ __forceinline__ void take_best(const void* row, int g0, int g1, int c
   }
 }
 
-__device__ __forceinline__ void write_alternative(const LogprobForward& a, int64_t row, int rank, uint64_t p, const RowStats& r) {
+__device__ __forceinline__ void write_alternative(const LogprobForward& a, int64_t row, int rank, uint64_t p, const RowStats& r, const Exponent& c) {
   a.top_index[row * a.top + rank] = column_of(p);
-  a.top_logprob[row * a.top + rank] = r.logprob(value_of(p), a.scale);
+  a.top_logprob[row * a.top + rank] = r.logprob(value_of(p), c);
 }
 
 // ---------------------------------------------------------------- forward
@@ -356,7 +368,7 @@ __global__ __launch_bounds__(kMostThreads) void logprob_forward_kernel(LogprobFo
   const int cols = static_cast<int>(a.cols), groups = (cols + kN - 1) / kN, each = (groups + a.parts - 1) / a.parts;
   const int g0 = min(part * each, groups), g1 = min(g0 + each, groups);
   const void* z = static_cast<const char*>(a.z) + row * a.ld * (kBf16 ? 2 : 4);
-  const float c = a.scale * kLog2E;
+  const Exponent c(a.scale);
   bool counted = false;
   float at_target = 0.0f;
   if (a.parts == 1 && threadIdx.x == 0 && a.targets) {   // (asked for ahead of the row)
@@ -377,10 +389,10 @@ __global__ __launch_bounds__(kMostThreads) void logprob_forward_kernel(LogprobFo
     return;
   }
   const RowStats r(all);
-  if (threadIdx.x == 0) write_row(a, row, all, r, at_target, counted);
+  if (threadIdx.x == 0) write_row(a, row, all, r, c, at_target, counted);
   if constexpr (kTop) {
     __shared__ TopShared s;
-    take_best<kBf16>(z, g0, g1, cols, mine.m, a.top, s, [&](int rank, uint64_t p) { write_alternative(a, row, rank, p, r); });
+    take_best<kBf16>(z, g0, g1, cols, mine.m, a.top, s, [&](int rank, uint64_t p) { write_alternative(a, row, rank, p, r, c); });
   }
 }
 
@@ -389,7 +401,7 @@ template <bool kBf16, bool kEntropy, bool kTop>
 __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobForward a) {
   const int64_t row = a.row0 + blockIdx.x;
   const int t = threadIdx.x, parts = a.parts, k = a.top;
-  const float c = a.scale * kLog2E;
+  const Exponent c(a.scale);
   const void* z = static_cast<const char*>(a.z) + row * a.ld * (kBf16 ? 2 : 4);
   bool counted = false;
   float at_target = 0.0f;
@@ -412,7 +424,7 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobForward a) {
     if (t == 0) n_found = 0;
     const Sum all = wave_join<kEntropy>(mine, c);
     const RowStats r(all);
-    if (t == 0) write_row(a, row, all, r, at_target, counted);
+    if (t == 0) write_row(a, row, all, r, c, at_target, counted);
     __syncthreads();
     // With j = ceil(k / parts), the ceil(k / j)-th largest of the pieces' j-th bounds the k-th best: so many pieces have j each that reach it.
     const int j = (k + parts - 1) / parts, enough = (k + j - 1) / j;
@@ -432,34 +444,34 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobForward a) {
       int ahead = 0;
 #pragma unroll 8
       for (int o = 0; o < n_found; ++o) ahead += found[o] > p;
-      if (ahead < k) write_alternative(a, row, ahead, p, r);
+      if (ahead < k) write_alternative(a, row, ahead, p, r, c);
     }
   } else {
     const Sum all = wave_join<kEntropy>(mine, c);
-    if (t == 0) write_row(a, row, all, RowStats(all), at_target, counted);
+    if (t == 0) write_row(a, row, all, RowStats(all), c, at_target, counted);
   }
 }
 
 // ---------------------------------------------------------------- gradient of the logits
 
-// What is the same for a row: dz_j = p_j (a - b log2 p_j), log2 p_j = (z_j - m) c - l; and what the target's column gets on top.
+// What is the same for a row: dz_j = p_j (a - b log2 p_j), log2 p_j = scale (z_j - m) log2(e) - l; and what the target's column gets on top.
 struct RowGradient {
-  float m, l, a, b, at_target;
+  float half_m, l, a, b, at_target;
   int target;   // -1: none
-  __device__ __forceinline__ RowGradient(float m_, float logsum, float scale, float g, float g_lse, float g_entropy, float entropy, int64_t target_, int cols) {
+  __device__ __forceinline__ RowGradient(float half_m_, float logsum, float scale, float g, float g_lse, float g_entropy, float entropy, int64_t target_, int cols) {
     const bool counted = target_ >= 0 && target_ < cols;
     if (!counted) g = 0.0f;
-    m = m_, l = logsum * kLog2E;
+    half_m = half_m_, l = logsum * kLog2E;
     a = scale * (g_lse - g - (g_entropy != 0.0f ? g_entropy * entropy : 0.0f));
     b = scale * g_entropy * kLn2;
     at_target = scale * g;
     target = counted && logsum != kInfinity ? static_cast<int>(target_) : -1;
   }
   template <bool kEntropy, int kN>
-  __device__ __forceinline__ void of(float (&v)[kN], int g, float c) const {
+  __device__ __forceinline__ void of(float (&v)[kN], int g, const Exponent& c) const {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const float t = (v[i] - m) * c - l, p = __builtin_amdgcn_exp2f(t);
+      const float t = c.base2(v[i], half_m) - l, p = __builtin_amdgcn_exp2f(t);
       v[i] = p * (kEntropy ? a - b * far_at_most(t) : a);
     }
     if (g == target >> (kN == 8 ? 3 : 2)) {
@@ -473,7 +485,7 @@ template <bool kInBf16, bool kOutBf16>
 constexpr int kGradientGroup = kInBf16 || kOutBf16 ? 8 : 4;
 
 template <bool kInBf16, bool kOutBf16, bool kEntropy>
-__device__ __forceinline__ void gradient_of_rest(const void* z, void* dz, int g, int cols, const RowGradient& r, float c) {
+__device__ __forceinline__ void gradient_of_rest(const void* z, void* dz, int g, int cols, const RowGradient& r, const Exponent& c) {
   constexpr int kN = kGradientGroup<kInBf16, kOutBf16>;
   float v[kN];
   rest_of_row<kInBf16>(z, g, cols, v);
@@ -490,7 +502,7 @@ __device__ __forceinline__ void gradient_of_rest(const void* z, void* dz, int g,
 
 // Groups [g0, g1) of a row by the workgroup's threads, from the end to the front.
 template <bool kInBf16, bool kOutBf16, bool kEntropy, bool kStream>
-__device__ __forceinline__ void gradient_of_groups(const void* z, void* dz, int g0, int g1, int cols, const RowGradient& r, float c) {
+__device__ __forceinline__ void gradient_of_groups(const void* z, void* dz, int g0, int g1, int cols, const RowGradient& r, const Exponent& c) {
   constexpr int kN = kGradientGroup<kInBf16, kOutBf16>;
   const int step = blockDim.x, whole = min(g1, cols / kN);
   if (whole < g1 && threadIdx.x == 0) gradient_of_rest<kInBf16, kOutBf16, kEntropy>(z, dz, whole, cols, r, c);
@@ -524,10 +536,11 @@ __global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobBackward a
   constexpr int kN = kGradientGroup<kInBf16, kOutBf16>;
   const int cols = static_cast<int>(a.cols), groups = (cols + kN - 1) / kN, each = (groups + a.parts - 1) / a.parts;
   const int g0 = min(part * each, groups), g1 = min(g0 + each, groups);
-  const RowGradient r(a.stats[2 * row], a.stats[2 * row + 1], a.scale, a.g_logprob ? a.g_logprob[row] : 0.0f, a.g_lse ? a.g_lse[row] : 0.0f,
+  const Exponent c(a.scale);
+  const RowGradient r(c.half(a.stats[2 * row]), a.stats[2 * row + 1], a.scale, a.g_logprob ? a.g_logprob[row] : 0.0f, a.g_lse ? a.g_lse[row] : 0.0f,
                       kEntropy ? a.g_entropy[row] : 0.0f, kEntropy ? a.entropy[row] : 0.0f, a.targets ? index_at(a.targets, a.i64, row) : -1, cols);
   gradient_of_groups<kInBf16, kOutBf16, kEntropy, false>(static_cast<const char*>(a.z) + row * a.ld * (kInBf16 ? 2 : 4),
-                                                         static_cast<char*>(a.dz) + row * a.ldd * (kOutBf16 ? 2 : 4), g0, g1, cols, r, a.scale * kLog2E);
+                                                         static_cast<char*>(a.dz) + row * a.ldd * (kOutBf16 ? 2 : 4), g0, g1, cols, r, c);
 }
 
 // Loss and gradient in one launch: a workgroup takes a row, sums over it and goes over it again from its end.  The last groups stay on the CU between the two --
@@ -545,7 +558,7 @@ __global__ __launch_bounds__(T, 8) void logprob_loss_kernel(LogprobForward f, Lo
   const int t = threadIdx.x, cols = static_cast<int>(f.cols), whole = cols / kN;
   const void* z = static_cast<const char*>(f.z) + row * f.ld * (kInBf16 ? 2 : 4);
   void* dz = static_cast<char*>(b.dz) + row * b.ldd * (kOutBf16 ? 2 : 4);
-  const float c = f.scale * kLog2E;
+  const Exponent c(f.scale);
   const int64_t target = index_at(f.targets, f.i64, row);
   const bool counted = target >= 0 && target < cols;
   const float at_target = counted ? value_at<kInBf16>(z, target) : 0.0f, g = b.g_logprob[row];
@@ -575,8 +588,8 @@ __global__ __launch_bounds__(T, 8) void logprob_loss_kernel(LogprobForward f, Lo
   }
   const Sum all = workgroup_join<false>(mine, c, sums);
   const RowStats r(all);
-  if (t == 0) write_row(f, row, all, r, at_target, counted);
-  const RowGradient d(r.m, r.logsum, f.scale, g, 0.0f, 0.0f, 0.0f, target, cols);
+  if (t == 0) write_row(f, row, all, r, c, at_target, counted);
+  const RowGradient d(c.half(r.m), r.logsum, f.scale, g, 0.0f, 0.0f, 0.0f, target, cols);
   auto store = [&](const Group<kInBf16, kN>& x, int group) {
     float v[kN];
     x.get(v);
