@@ -482,6 +482,7 @@ int nvfp4_logprob_forward(const void* logits, int dtype, int64_t ld, int64_t row
 /*
  * Gradient of the logits from those of logprob, lse and entropy (FP32 [rows]; each may be NULL):
  *   dlogits[j] = scale (g_logprob [j = target] + p[j] (g_lse - g_logprob - g_entropy (ln p[j] + entropy)))
+ * The three gradients' sum is FP32; scale times it may be beyond that where p makes a number of it again, and p = 0 gives 0 (up to products of 2^242).
  * A target outside [0, cols) takes no g_logprob.  stats, entropy (only with g_entropy) as the forward pass gave them; dlogits of type d_dtype.
  */
 int nvfp4_logprob_backward(const void* logits, int dtype, int64_t ld, int64_t rows, int64_t cols, float scale, const void* targets, int index_type,

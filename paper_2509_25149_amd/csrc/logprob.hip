@@ -455,28 +455,52 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobForward a) {
 // ---------------------------------------------------------------- gradient of the logits
 
 // What is the same for a row: dz_j = p_j (a - b log2 p_j), log2 p_j = scale (z_j - m) log2(e) - l; and what the target's column gets on top.
+// scale times a gradient may be beyond FP32 where p_j makes a number of it again, and p_j = 0 has to make 0.  So where scale times the largest of the gradients is above 2^116, a, b and the target's part
+// are held 2^-up of themselves, below 2^125 with all that is added up, and p_j is taken 2^up times by its exponent, which is no operation more at a column.  (The sum of the gradients that `a` holds is FP32 by
+// itself.  up is 140 at most; above 127, scale times gradient above 2^242, 0 may come out as NaN.)
+template <bool kEntropy>
 struct RowGradient {
-  float half_m, l, a, b, at_target;
-  int target;   // -1: none
+  float half_m, l, a, b, at_target;   // l and a for exponents raised by `up`
+  int target;                         // -1: none
+  int up;
   __device__ __forceinline__ RowGradient(float half_m_, float logsum, float scale, float g, float g_lse, float g_entropy, float entropy, int64_t target_, int cols) {
     const bool counted = target_ >= 0 && target_ < cols;
     if (!counted) g = 0.0f;
-    half_m = half_m_, l = logsum * kLog2E;
-    a = scale * (g_lse - g - (g_entropy != 0.0f ? g_entropy * entropy : 0.0f));
-    b = scale * g_entropy * kLn2;
+    float most = __builtin_fmaxf(__builtin_fabsf(g), __builtin_fabsf(g_lse));
+    if (kEntropy) most = __builtin_fmaxf(most, __builtin_fabsf(g_entropy));
+    up = __builtin_amdgcn_readfirstlane(max(0, exponent_of(scale) + exponent_of(most) - 115));   // (the same in a wavefront)
+    scale = __builtin_ldexpf(scale, -up);
+    const float raised = static_cast<float>(up);
+    half_m = half_m_, l = logsum * kLog2E - raised;
+    a = scale * (g_lse - g - (kEntropy && g_entropy != 0.0f ? g_entropy * entropy : 0.0f)), b = 0.0f;
+    if (kEntropy) {
+      b = scale * g_entropy * kLn2;
+      a = up ? a + b * raised : a;
+    }
     at_target = scale * g;
     target = counted && logsum != kInfinity ? static_cast<int>(target_) : -1;
   }
-  template <bool kEntropy, int kN>
+  // (128 for what is no number; it stays none)
+  static __device__ __forceinline__ int exponent_of(float v) { return static_cast<int>(__float_as_uint(v) >> 23 & 255u) - 127; }
+  // v: logits of group g, and then their gradients.
+  template <int kN>
   __device__ __forceinline__ void of(float (&v)[kN], int g, const Exponent& c) const {
+    const float raised = static_cast<float>(up);
+    float z[kN];
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
+      z[i] = v[i];
       const float t = c.base2(v[i], half_m) - l, p = __builtin_amdgcn_exp2f(t);
-      v[i] = p * (kEntropy ? a - b * far_at_most(t) : a);
+      v[i] = p * (kEntropy ? a - b * __builtin_fmaxf(t, kFar + raised) : a);
     }
     if (g == target >> (kN == 8 ? 3 : 2)) {
+      float at = z[0];
 #pragma unroll
-      for (int i = 0; i < kN; ++i) v[i] += i == (target & (kN - 1)) ? at_target : 0.0f;
+      for (int i = 1; i < kN; ++i) at = i == (target & (kN - 1)) ? z[i] : at;
+      const float t = c.base2(at, half_m) - (l + raised), p = __builtin_amdgcn_exp2f(t);
+      const float x = __builtin_ldexpf(p * (kEntropy ? (a - (up ? b * raised : 0.0f)) - b * far_at_most(t) : a) + at_target, up);
+#pragma unroll
+      for (int i = 0; i < kN; ++i) v[i] = i == (target & (kN - 1)) ? x : v[i];
     }
   }
 };
@@ -485,11 +509,11 @@ template <bool kInBf16, bool kOutBf16>
 constexpr int kGradientGroup = kInBf16 || kOutBf16 ? 8 : 4;
 
 template <bool kInBf16, bool kOutBf16, bool kEntropy>
-__device__ __forceinline__ void gradient_of_rest(const void* z, void* dz, int g, int cols, const RowGradient& r, const Exponent& c) {
+__device__ __forceinline__ void gradient_of_rest(const void* z, void* dz, int g, int cols, const RowGradient<kEntropy>& r, const Exponent& c) {
   constexpr int kN = kGradientGroup<kInBf16, kOutBf16>;
   float v[kN];
   rest_of_row<kInBf16>(z, g, cols, v);
-  r.of<kEntropy>(v, g, c);
+  r.of(v, g, c);
 #pragma unroll
   for (int i = 0; i < kN; ++i) {
     const int col = g * kN + i;
@@ -502,7 +526,7 @@ __device__ __forceinline__ void gradient_of_rest(const void* z, void* dz, int g,
 
 // Groups [g0, g1) of a row by the workgroup's threads, from the end to the front.
 template <bool kInBf16, bool kOutBf16, bool kEntropy, bool kStream>
-__device__ __forceinline__ void gradient_of_groups(const void* z, void* dz, int g0, int g1, int cols, const RowGradient& r, const Exponent& c) {
+__device__ __forceinline__ void gradient_of_groups(const void* z, void* dz, int g0, int g1, int cols, const RowGradient<kEntropy>& r, const Exponent& c) {
   constexpr int kN = kGradientGroup<kInBf16, kOutBf16>;
   const int step = blockDim.x, whole = min(g1, cols / kN);
   if (whole < g1 && threadIdx.x == 0) gradient_of_rest<kInBf16, kOutBf16, kEntropy>(z, dz, whole, cols, r, c);
@@ -515,7 +539,7 @@ __device__ __forceinline__ void gradient_of_groups(const void* z, void* dz, int 
     for (int u = 0; u < 4; ++u) {
       float v[kN];
       x[u].get(v);
-      r.of<kEntropy>(v, g - u * step, c);
+      r.of(v, g - u * step, c);
       put_group<kStream, kOutBf16>(dz, g - u * step, v);
     }
   }
@@ -524,20 +548,21 @@ __device__ __forceinline__ void gradient_of_groups(const void* z, void* dz, int 
     float v[kN];
     x.load(z, g);
     x.get(v);
-    r.of<kEntropy>(v, g, c);
+    r.of(v, g, c);
     put_group<kStream, kOutBf16>(dz, g, v);
   }
 }
 
+// (Eight wavefronts to a SIMD, which FP32 to bf16 with entropy has to be told: 8192 x 20000 164 us, with seven 172.)
 template <bool kInBf16, bool kOutBf16, bool kEntropy>
-__global__ __launch_bounds__(256) void logprob_backward_kernel(LogprobBackward a) {
+__global__ __launch_bounds__(256, 8) void logprob_backward_kernel(LogprobBackward a) {
   const int part = static_cast<int>(blockIdx.x % static_cast<unsigned>(a.parts));
   const int64_t row = a.row0 + blockIdx.x / static_cast<unsigned>(a.parts);
   constexpr int kN = kGradientGroup<kInBf16, kOutBf16>;
   const int cols = static_cast<int>(a.cols), groups = (cols + kN - 1) / kN, each = (groups + a.parts - 1) / a.parts;
   const int g0 = min(part * each, groups), g1 = min(g0 + each, groups);
   const Exponent c(a.scale);
-  const RowGradient r(c.half(a.stats[2 * row]), a.stats[2 * row + 1], a.scale, a.g_logprob ? a.g_logprob[row] : 0.0f, a.g_lse ? a.g_lse[row] : 0.0f,
+  const RowGradient<kEntropy> r(c.half(a.stats[2 * row]), a.stats[2 * row + 1], a.scale, a.g_logprob ? a.g_logprob[row] : 0.0f, a.g_lse ? a.g_lse[row] : 0.0f,
                       kEntropy ? a.g_entropy[row] : 0.0f, kEntropy ? a.entropy[row] : 0.0f, a.targets ? index_at(a.targets, a.i64, row) : -1, cols);
   gradient_of_groups<kInBf16, kOutBf16, kEntropy, false>(static_cast<const char*>(a.z) + row * a.ld * (kInBf16 ? 2 : 4),
                                                          static_cast<char*>(a.dz) + row * a.ldd * (kOutBf16 ? 2 : 4), g0, g1, cols, r, c);
@@ -589,11 +614,11 @@ __global__ __launch_bounds__(T, 8) void logprob_loss_kernel(LogprobForward f, Lo
   const Sum all = workgroup_join<false>(mine, c, sums);
   const RowStats r(all);
   if (t == 0) write_row(f, row, all, r, c, at_target, counted);
-  const RowGradient d(c.half(r.m), r.logsum, f.scale, g, 0.0f, 0.0f, 0.0f, target, cols);
+  const RowGradient<false> d(c.half(r.m), r.logsum, f.scale, g, 0.0f, 0.0f, 0.0f, target, cols);
   auto store = [&](const Group<kInBf16, kN>& x, int group) {
     float v[kN];
     x.get(v);
-    d.of<false>(v, group, c);
+    d.of(v, group, c);
     put_group<kStream, kOutBf16>(dz, group, v);
   };
   if (cols % kN && t == T - 1) gradient_of_rest<kInBf16, kOutBf16, false>(z, dz, whole, cols, d, c);

@@ -40,3 +40,33 @@ def test_differences_beyond_fp32_at_a_small_scale(rows, cols, dt, scale):
     one = nv.nvfp4_logprob_with_gradient(z, em.index(t, I64), g, scale=scale)
     base.check_forward(one, z, scale, t, 0, False)
     base.check_gradient(one.dlogits, z, scale, t, g, None, None, dt)
+
+
+@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("dt,ot", [(F32, F32), (BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("scale,size", [(2.0 ** 122, 1.0), (2.0 ** 127, 1.0), (2.0 ** 64, 2.0 ** 63), (1.0, 2.0 ** 126), (2.0 ** -100, 2.0 ** 126)])
+def test_gradients_near_the_end_of_fp32(rows, cols, dt, ot, scale, size):
+    """scale times a gradient may be beyond FP32 where p makes it small again, and a probability of 0 makes a 0 of it: columns masked by -infinity or the type's lowest value, or
+    far below the others.  The logits that count are k / scale apart, k up to 30."""
+    r = np.random.default_rng(cols)
+    v = np.full((rows, cols), -np.inf)
+    v[:, 4:8] = float(torch.finfo(dt).min) if scale >= 1 else -3e38
+    v[:, 8:12] = -256 / scale
+    v[:, 12:20] = -r.integers(3, 30, (rows, 8)) / scale
+    v[:, cols - 3] = -4 / scale
+    v[:, 2] = 0.0
+    z = bm.tensor(v, dt, base.pad_of(cols, 8))
+    t = np.full(rows, 2)
+    t[rows // 2] = -1
+    t[0] = 0                                                  # masked
+    g, gl, ge = (torch.full((rows,), a * size, device="cuda") for a in (3.0, 0.2, 0.25))
+    g[0] = 0.5 * size
+    out = nv.nvfp4_logprob_forward(z, em.index(t, I32), scale=scale, entropy=True, for_backward=True)
+    base.check_forward(out, z, scale, t, 0, True)
+    for use in ((g, None, None), (g, gl, ge), (None, None, ge)):
+        dz = nv.nvfp4_logprob_backward(z, em.index(t, I32), out.stats, g_logprob=use[0], g_lse=use[1], g_entropy=use[2], entropy=out.entropy, scale=scale, out_dtype=base.OUT[ot])
+        assert bool(torch.isfinite(dz).all())
+        base.check_gradient(dz, z, scale, t, *use, ot)
+    one = nv.nvfp4_logprob_with_gradient(z, em.index(t, I32), g, scale=scale, out_dtype=base.OUT[ot])
+    assert bool(torch.isfinite(one.dlogits).all())
+    base.check_gradient(one.dlogits, z, scale, t, g, None, None, ot)
