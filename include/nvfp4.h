@@ -524,7 +524,8 @@ int nvfp4_grad_list_build(const nvfp4_grad* tensors, int64_t n, void* table_host
 
 /*
  * nvfp4_grad_sumsq: *sumsq = the sum of all squares, binary64, in a fixed order; device memory, as is the workspace (16-byte aligned, nvfp4_grad_list_sizes bytes).
- * nvfp4_grad_clip:  norm = sqrt(*sumsq);  out = data * (norm > max_norm ? max_norm / norm : 1).  norm: device FP32, or NULL; max_norm >= 0, infinity for the norm alone.
+ * nvfp4_grad_clip:  norm = sqrt(*sumsq);  out = data * (norm > max_norm ? max_norm / norm : 1).  norm: device FP32, or NULL; max_norm >= 0, infinity for the norm alone.  (A finite norm
+ *                   beyond FP32 is written as infinity and clips all the same.)
  * Two calls, so that the sums of several lists or of other GPUs' shards can be added in between.  A norm that is not finite leaves the values as they are; a gradient in its place that needs no
  * clipping is not read.
  */

@@ -151,7 +151,7 @@ __global__ __launch_bounds__(1024) void grad_fold_kernel(const double* __restric
 }
 
 template <bool kBf16, bool kOutBf16>
-__device__ __forceinline__ void scaled(const Unit& n, uint32_t t, uint32_t step, float by) {
+__device__ __forceinline__ void scaled(const Unit& n, uint32_t t, uint32_t step, float by, int up) {
   constexpr int kN = kBf16 && kOutBf16 ? 8 : 4, kSize = kBf16 ? 2 : 4, kOutSize = kOutBf16 ? 2 : 4;
   for_unit<kN, 4>(
       n, t, step,
@@ -159,11 +159,11 @@ __device__ __forceinline__ void scaled(const Unit& n, uint32_t t, uint32_t step,
         float v[kN];
         load_piece<kBf16>(n.data + row * n.ld + static_cast<int64_t>(col) * kSize, v);
 #pragma unroll
-        for (int i = 0; i < kN; ++i) v[i] *= by;
+        for (int i = 0; i < kN; ++i) v[i] = __builtin_ldexpf(v[i] * by, up);
         store_piece<kOutBf16>(n.out + row * n.ld_out + static_cast<int64_t>(col) * kOutSize, v);
       },
       [&](int row, int col) {
-        const float v = load1<kBf16>(n.data + row * n.ld + static_cast<int64_t>(col) * kSize) * by;
+        const float v = __builtin_ldexpf(load1<kBf16>(n.data + row * n.ld + static_cast<int64_t>(col) * kSize) * by, up);
         store1<kOutBf16>(n.out + row * n.ld_out + static_cast<int64_t>(col) * kOutSize, v);
       });
 }
@@ -177,16 +177,19 @@ __global__ __launch_bounds__(256) void grad_clip_kernel(const GradTensor* __rest
                                                         const double* __restrict__ sumsq, float max_norm, float* __restrict__ norm) {
   const double total = __builtin_sqrt(*sumsq);
   const bool clips = total > static_cast<double>(max_norm) && total < __builtin_huge_val();
-  const float by = clips ? static_cast<float>(static_cast<double>(max_norm) / total) : 1.0f;
+  // A factor below FP32's normal numbers (a norm beyond 2^126 times the bound) would have too few bits, or none: it is by 2^up, by in [0.5, 1).
+  const double factor = clips ? static_cast<double>(max_norm) / total : 1.0;
+  const int up = factor < 0x1p-126 ? __builtin_amdgcn_frexp_exp(factor) : 0;
+  const float by = static_cast<float>(__builtin_ldexp(factor, -up));
   if (blockIdx.x == 0 && threadIdx.x == 0 && norm) *norm = static_cast<float>(total);
   if (units == 0) return;
   const uint32_t w = xcd_neighbours(blockIdx.x, gridDim.x), t = w % splits * 256 + threadIdx.x, step = splits * 256;
   const Unit n = unit_of(tensors, unit_tensor, w / splits);
-  if (by == 1.0f && n.data == n.out && ((n.flags & kGradBf16) != 0) == ((n.flags & kGradOutBf16) != 0)) return;
+  if (by == 1.0f && up == 0 && n.data == n.out && ((n.flags & kGradBf16) != 0) == ((n.flags & kGradOutBf16) != 0)) return;
   if (n.flags & kGradBf16) {
-    if (n.flags & kGradOutBf16) scaled<true, true>(n, t, step, by); else scaled<true, false>(n, t, step, by);
+    if (n.flags & kGradOutBf16) scaled<true, true>(n, t, step, by, up); else scaled<true, false>(n, t, step, by, up);
   } else {
-    if (n.flags & kGradOutBf16) scaled<false, true>(n, t, step, by); else scaled<false, false>(n, t, step, by);
+    if (n.flags & kGradOutBf16) scaled<false, true>(n, t, step, by, up); else scaled<false, false>(n, t, step, by, up);
   }
 }
 
