@@ -500,8 +500,8 @@ int nvfp4_logprob_with_gradient(const void* logits, int dtype, int64_t ld, int64
 /*
  * The gradients of a model, for their common norm and for clipping.
  *   data       [rows, cols] of type dtype, leading dimension ld (any, at least cols), aligned to its element
- *   out        where the clipped gradient goes, of type out_dtype, leading dimension ld_out; NULL: to data.  Results do not overlap each other or another tensor's data;
- *              equal places are refused
+ *   out        where the clipped gradient goes, of type out_dtype, leading dimension ld_out; NULL: to data.  Results overlap neither each other nor anything that is read, but
+ *              for the very place of their own data.  The list refuses what overlaps (of a tensor whose rows lie apart only its first element is looked at)
  * Any rows and cols, 0 included; a vector is one row.  At most 2^20 tensors and 2^40 elements.
  */
 typedef struct nvfp4_grad {

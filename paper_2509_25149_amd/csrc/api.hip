@@ -921,22 +921,32 @@ int nvfp4_grad_list_build(const nvfp4_grad* tensors, int64_t n, void* table_host
   const int64_t units = grad_units(tensors, n);
   if (!list || (n && !table_host) || !aligned(table_host, 8)) return NVFP4_ERR_INVALID_ARG;
   if (table_bytes < grad_table_bytes(n, units)) return NVFP4_ERR_WORKSPACE;
-  // No element is written for two tensors: first and last byte of each, in order (of one whose rows lie apart its first element, since others may lie between its rows).
+  // No element is written that another tensor has written or anything reads, but for its own value: first and last byte of each tensor's data and result, in order (of one whose rows lie apart its
+  // first element, since others may lie between its rows).  They are held in the table's memory.
   struct Range {
     uintptr_t first, end;
+    bool written;
   };
+  static_assert(2 * sizeof(Range) <= sizeof(GradTensor));
   Range* ranges = static_cast<Range*>(table_host);
-  int64_t written = 0;
+  int64_t count = 0;
+  auto add = [&](const nvfp4_grad& g, const void* at, int64_t ld, int dtype, bool written) {
+    const uintptr_t first = reinterpret_cast<uintptr_t>(at);
+    ranges[count++] = Range{first, first + (g.rows == 1 || ld == g.cols ? static_cast<size_t>(grad_elements(g)) : 1) * element_size(dtype), written};
+  };
   for (int64_t i = 0; i < n; ++i) {
     const nvfp4_grad& g = tensors[i];
     if (grad_elements(g) == 0) continue;
-    const uintptr_t first = reinterpret_cast<uintptr_t>(g.out ? g.out : g.data);
-    const bool whole = g.rows == 1 || (g.out ? g.ld_out : g.ld) == g.cols;
-    ranges[written++] = Range{first, first + (whole ? static_cast<size_t>(grad_elements(g)) : 1) * element_size(g.out_dtype)};
+    const bool in_place = !g.out || g.out == g.data;
+    add(g, g.data, g.ld, g.dtype, in_place);
+    if (!in_place) add(g, g.out, g.ld_out, g.out_dtype, true);
   }
-  std::sort(ranges, ranges + written, [](const Range& a, const Range& b) { return a.first < b.first; });
-  for (int64_t i = 1; i < written; ++i) {
-    if (ranges[i].first < ranges[i - 1].end) return NVFP4_ERR_INVALID_ARG;
+  std::sort(ranges, ranges + count, [](const Range& a, const Range& b) { return a.first < b.first; });
+  uintptr_t read = 0, written = 0;   // where the data and the results so far end
+  for (int64_t i = 0; i < count; ++i) {
+    if (ranges[i].first < written || (ranges[i].written && ranges[i].first < read)) return NVFP4_ERR_INVALID_ARG;
+    uintptr_t& end = ranges[i].written ? written : read;
+    end = std::max(end, ranges[i].end);
   }
   const int64_t each = unit_elements(tensors, n);
   GradTensor* t = static_cast<GradTensor*>(table_host);
