@@ -45,8 +45,10 @@ class LanguageModel:
         e = nv.nvfp4_embedding_forward(ids, self.table, scale=self.scale)
         y, saved = self.block.forward(torch.zeros_like(e), e)
         norm = nv.nvfp4_rmsnorm_forward(y, self.gamma)
-        logits = torch.mm(norm.y, self.table.t())
-        counted = ((targets >= 0) & (targets < self.table.shape[0])).sum().clamp_min(1)
+        vocab = self.table.shape[0]
+        logits = torch.empty(len(ids), -(-vocab // 8) * 8, dtype=norm.y.dtype, device=ids.device)[:, :vocab]     # rows at multiples of 8, as the log probabilities take them
+        torch.mm(norm.y, self.table.t(), out=logits)
+        counted = ((targets >= 0) & (targets < vocab)).sum().clamp_min(1)
         weight = (-1.0 / counted).expand(targets.shape).contiguous()
         out = nv.nvfp4_logprob_with_gradient(logits, targets, weight, out=logits)
         dlogits = out.dlogits
