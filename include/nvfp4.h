@@ -464,7 +464,7 @@ int nvfp4_embedding_backward(const void* dout, int dtype, int64_t ldd, const voi
  *   targets      token numbers [rows], or NULL
  *   logprob      FP32 [rows]: ln p[target], 0 where the target is outside [0, cols); or NULL
  *   stats        FP32 [rows, 2]: the row's largest logit m, and ln sum exp(scale (logit - m)), for nvfp4_logprob_backward; or NULL.  They are kept apart because their
- *                sum loses the second where the first is large.
+ *                sum loses the second where the first is large.  (0 and +infinity for a row of nothing but -infinity.)
  *   lse          FP32 [rows]: scale m + the logarithm; or NULL
  *   entropy      FP32 [rows]: -sum p ln p; or NULL
  *   top          0 to 32, at most cols: the `top` largest logits of each row in descending order, of equal ones those with the lowest columns:

@@ -850,7 +850,8 @@ def nvfp4_logprob_with_gradient(logits: torch.Tensor, targets: torch.Tensor, g_l
 
 class Gradients:
     """The gradients of a model as one list, laid out on the device once for all steps that use these tensors: float32 or bf16, contiguous of any shape, or
-    2-D with contiguous rows.  outs: where the clipped ones go (same shapes, any of the two types); default: in their place."""
+    2-D with contiguous rows.  outs: where the clipped ones go (same shapes, any of the two types); default: in their place.  Takes the host 1.6 us a tensor, and a copy to
+    the device that is waited for."""
     __slots__ = ("tensors", "outs", "desc", "ref", "table", "workspace_bytes", "device")
 
     def __init__(self, tensors, outs=None):

@@ -641,8 +641,10 @@ constexpr int64_t kCUs = 256;
 struct ForwardShape {
   int parts, threads;
 };
-// A row to a workgroup, but for few long rows, which are cut into pieces (us on the GPU without / with pieces: 1 x 131072 11.5 / 5.6, 64 x 131072 12 / 9, 100 x 131072 12 / 11, 1 to 100 x 50257
-// 6.9 / 5.8 to 8.7, where the second launch costs the host 3 more).  Threads by the bytes of a row; the best alternatives are looked for by 256 at least.
+// A row to a workgroup, but for few long rows, which are cut into pieces (us on the GPU, whole / in pieces, bf16 with entropy, 1, 16, 64 and 90 rows: of 50257 6.3 / 5.6, 6.7 / 6.9, 6.8 / 8.1, 6.8 / 8.6;
+// of 65536 7.3 / 5.6, 7.6 / 6.9, 8.1 / 8.1, 8.3 / 9.2; of 131072 11.2 / 5.6, 11.5 / 7.4, 12.1 / 9.2, 12.8 / 11.9.  With 20 alternatives, which are searched in every piece and then joined: of 65536
+// 11.2 / 12.7, 11.8 / 15.1, 11.9 / 15.4, 12.5 / 16.2; of 100000 14.1 / 12.5, 15.2 / 15.6, 15.2 / 17.0, 16.1 / 17.3; of 131072 16.3 / 12.6, 17.3 / 15.6, 18.3 / 17.0, 19.4 / 19.3.  The second launch costs the
+// host 3 more).  Threads by the bytes of a row; 64 where alternatives are looked for in up to 2 KB, which is as many as take_best needs for 32.
 ForwardShape forward_shape(int64_t rows, int64_t cols, bool bf16, bool top) {
   if (rows < 96 && cols >= 65536) return {static_cast<int>(std::min<int64_t>(kMostParts, 4 * kCUs / std::max<int64_t>(rows, 1))), 256};
   const int64_t bytes = cols * (bf16 ? 2 : 4);
@@ -691,7 +693,7 @@ hipError_t backward_with(const LogprobBackward& a, int threads, hipStream_t s) {
 
 // By bytes of a row, in whose second pass the part that stays on the CU counts, against rows in flight.  us for 8192 rows with 64 / 256 / 512 / 1024 threads: 8 KB 27 / 31 / 46 / 97,
 // 20 KB 91 / 69 / 75 / 124, 40 KB 185 / 135 / 126 / 169, 80 KB 368 / 295 / 252 / 245, 262 KB 1214 / 1123 / 1054 / 873; 1040 rows of 100 KB 72 / 57 / 55 / 61 (1040 of
-// them do not fit the chip's 512 places for 1024 threads), of 200 KB 147 / 139 / 120 / 108.
+// them do not fit the chip's 512 places for 1024 threads), of 200 KB 147 / 139 / 120 / 108.  (Of 131072 FP32 values, 524 KB, three quarters are read twice: by the counters 1.75 times their bytes.)
 int loss_threads(int64_t rows, int64_t cols, bool bf16) {
   const int64_t bytes = cols * (bf16 ? 2 : 4);
   return bytes <= 8 << 10 ? 64 : bytes <= 36 << 10 ? 256 : bytes <= (rows >= 8 * kCUs ? 72 << 10 : 160 << 10) ? 512 : 1024;
